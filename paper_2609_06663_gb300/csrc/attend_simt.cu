@@ -1,0 +1,225 @@
+// Attention of the decode step on CUDA cores: fp32 tensors, and bf16 ones with
+// ECOKV_FLAG_FORCE_SIMT.  Items and tiles as in attend.cuh, rows in groups of 64
+// (or of 16 where an item has no more).
+//
+// A CTA of 256 threads holds an item's queries, a tile of 128 keys and its values
+// in shared memory as fp32.  Thread (ty, tx) of 16 x 16 forms the scores of its rows
+// ty R .. ty R + R - 1 with the keys tx + 16 j, a row's maximum and sum are four
+// shuffles away, and the same thread then sums columns 4 tx .. and 64 + 4 tx .. of
+// its rows' outputs over the tile, which stay in registers through the item.
+
+#include <math.h>
+
+#include "attend.cuh"
+#include "ptx.cuh"
+
+namespace ecokv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRows = 64;    // rows a row tile
+constexpr int kPad = kD + 4; // floats a padded row: 16-byte reads of 8 consecutive rows meet all banks
+
+struct Smem {
+  float q[kRows][kPad];
+  float k[kKeys][kPad];
+  float v[kKeys][kD];
+  float p[kRows][kPad];
+  Item item;
+  int more;
+};
+
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                     __uint_as_float(w.y & 0xffff0000u));
+}
+
+// Offset of key j of the item in K and V, negative: none (a page number out of range).
+__device__ __forceinline__ int64_t key_offset(const AttendArgs& a, const Item& it, int j) {
+  if (it.source == 0) {
+    const int64_t r = (int64_t)it.row0 + j;
+    return (a.prefix.head_off ? 0 : (int64_t)it.head * a.prefix.head_stride) + r * a.prefix.row_stride;
+  }
+  const int page = a.cache.table[(int64_t)it.seq * a.cache.table_stride + (j >> a.page_shift)];
+  if (page < 0 || page >= a.cache.n_pages) {
+    note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)it.seq);
+    return -1;
+  }
+  return (int64_t)page * a.cache.page_stride + (int64_t)it.head * a.cache.head_stride +
+         (int64_t)(j & (a.cache.page_size - 1)) * a.cache.slot_stride;
+}
+
+template <typename T, int R>
+__device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const Item& it) {
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31, warp = tid >> 5;
+  const int rows = it.ntok * a.g;
+  // queries
+  for (int r = warp; r < 16 * R; r += kThreads / 32) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < rows) {
+      const int k = r / a.g;
+      v = load4(static_cast<const T*>(a.q) + (int64_t)(it.tok0 + k) * a.q_token +
+                (int64_t)(it.head * a.g + r - k * a.g) * a.q_head + lane * 4);
+    }
+    *reinterpret_cast<float4*>(&s.q[r][lane * 4]) = v;
+  }
+  float m[R], l[R], o[R][8];
+  int lim[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+    lim[r] = it.lim0 + (ty * R + r) / a.g * it.slope;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[r][c] = 0.f;
+  }
+  const T* K = static_cast<const T*>(it.source == 0 ? a.prefix.k : a.cache.k);
+  const T* V = static_cast<const T*>(it.source == 0 ? a.prefix.v : a.cache.v);
+  for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
+    __syncthreads();
+#pragma unroll 4
+    for (int i = 0; i < kKeys / (kThreads / 32); ++i) {
+      const int kk = warp + i * (kThreads / 32), j = t * kKeys + kk;
+      const int64_t at = j < it.vis ? key_offset(a, it, j) : -1;
+      float4 k4 = make_float4(0.f, 0.f, 0.f, 0.f), v4 = k4;
+      if (at >= 0) {
+        k4 = load4(K + at + lane * 4);
+        v4 = load4(V + at + lane * 4);
+      }
+      *reinterpret_cast<float4*>(&s.k[kk][lane * 4]) = k4;
+      *reinterpret_cast<float4*>(&s.v[kk][lane * 4]) = v4;
+    }
+    __syncthreads();
+    float x[R][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[r][c] = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < kD; e += 4) {
+      float4 q4[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(&s.q[ty * R + r][e]);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&s.k[tx + 16 * c][e]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          x[r][c] = fmaf(q4[r].x, k4.x, x[r][c]);
+          x[r][c] = fmaf(q4[r].y, k4.y, x[r][c]);
+          x[r][c] = fmaf(q4[r].z, k4.z, x[r][c]);
+          x[r][c] = fmaf(q4[r].w, k4.w, x[r][c]);
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        x[r][c] = t * kKeys + tx + 16 * c < lim[r] ? x[r][c] * a.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, x[r][c]);
+      }
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+      const float mn = fmaxf(m[r], mx), ref = mn == -INFINITY ? 0.f : mn;
+      const float corr = ptx::ex2(m[r] - ref);
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float p = ptx::ex2(x[r][c] - ref);
+        sum += p;
+        s.p[ty * R + r][tx + 16 * c] = p;
+      }
+      l[r] = fmaf(l[r], corr, sum);  // this thread's share of the row's sum
+      m[r] = mn;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[r][c] *= corr;
+    }
+    __syncwarp();  // (a row's sixteen threads are in one warp)
+#pragma unroll 2
+    for (int k0 = 0; k0 < kKeys; k0 += 4) {
+      float4 p4[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) p4[r] = *reinterpret_cast<const float4*>(&s.p[ty * R + r][k0]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float4 va = *reinterpret_cast<const float4*>(&s.v[k0 + k][4 * tx]);
+        const float4 vb = *reinterpret_cast<const float4*>(&s.v[k0 + k][64 + 4 * tx]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float p = k == 0 ? p4[r].x : k == 1 ? p4[r].y : k == 2 ? p4[r].z : p4[r].w;
+          o[r][0] = fmaf(p, va.x, o[r][0]);
+          o[r][1] = fmaf(p, va.y, o[r][1]);
+          o[r][2] = fmaf(p, va.z, o[r][2]);
+          o[r][3] = fmaf(p, va.w, o[r][3]);
+          o[r][4] = fmaf(p, vb.x, o[r][4]);
+          o[r][5] = fmaf(p, vb.y, o[r][5]);
+          o[r][6] = fmaf(p, vb.z, o[r][6]);
+          o[r][7] = fmaf(p, vb.w, o[r][7]);
+        }
+      }
+    }
+    __syncwarp();
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+    const int row = ty * R + r;
+    if (row < rows) {
+      const int k = row / a.g;
+      const bool first = it.tile0 == 0;
+      const size_t at = first ? first_row(a, it.source, 0, it.tok0 + k, it.head * a.g + row - k * a.g)
+                              : next_row(a, blockIdx.x, 0, row);
+      float* dst = (first ? a.first_o : a.next_o) + at * kD;
+      *reinterpret_cast<float4*>(dst + 4 * tx) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+      *reinterpret_cast<float4*>(dst + 64 + 4 * tx) = make_float4(o[r][4], o[r][5], o[r][6], o[r][7]);
+      if (tx == 0) (first ? a.first_ml : a.next_ml)[at] = make_float2(m[r], l[r]);
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_constant__ AttendArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  Smem& s = *reinterpret_cast<Smem*>(smem_raw);
+  const int lane = threadIdx.x & 31;
+  Walk w;
+  if (threadIdx.x < 32) w.begin(a, blockIdx.x, lane);
+  while (true) {
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      Item it;
+      const bool more = w.next(a, it);
+      if (lane == 0) {
+        s.item = it;
+        s.more = more ? 1 : 0;
+      }
+    }
+    __syncthreads();
+    if (s.more == 0) break;
+    const Item it = s.item;
+    if (it.ntok * a.g <= 16) item_rows<T, 1>(a, s, it);
+    else item_rows<T, 4>(a, s, it);
+  }
+}
+
+template <typename T>
+cudaError_t launch(const AttendArgs& a, cudaStream_t st) {
+  const cudaError_t e =
+      cudaFuncSetAttribute(attend_simt_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+  if (e != cudaSuccess) return e;
+  attend_simt_kernel<T><<<a.P, kThreads, sizeof(Smem), st>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attend_simt(const AttendArgs& a, ecokv_dtype dt, cudaStream_t st) {
+  return dt == ECOKV_F32 ? launch<float>(a, st) : launch<__nv_bfloat16>(a, st);
+}
+
+}  // namespace ecokv

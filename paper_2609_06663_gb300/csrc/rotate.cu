@@ -1,0 +1,468 @@
+// ecokv_rotate and ecokv_append: per-head RMS norm and rotary positions of query
+// and key rows, into rows of any strides or into the slots of a paged cache.
+//
+// A row is 128 elements, held by eight lanes of sixteen.  Lane c holds the pairs
+// of frequencies 8c .. 8c + 7 in either layout: elements 8c.. and rot/2 + 8c.. (half)
+// or 16c .. 16c + 15 (interleaved), so that a rotation stays within a lane, its loads
+// are 16 bytes wide, and the norm's sum is three shuffles away.  A group of eight
+// lanes takes one token and some of its heads: the sines and cosines of a token
+// are formed once per group.
+//
+// The angle.  position * inv_freq / 2 pi mod 1 is position * turns mod 2^64 with
+// turns = inv_freq / 2 pi in units of 2^-64: the product wraps as the angle does, so
+// the only error is the frequency's own (2^-53 relative) and the last rounding to
+// 24 bits.  In fp32 position * inv_freq alone would be off by 2^-24 of the
+// position, 0.008 rad at 131072.
+//
+// Bound by HBM: every row is read and written once.
+
+#include <math.h>
+#include <string.h>
+
+#include "attend.cuh"
+
+namespace ecokv {
+namespace {
+
+constexpr int kGroup = 8;                // lanes a row
+constexpr int kThreads = 256;
+constexpr int kGroups = kThreads / kGroup;
+
+struct RowSet {
+  const void* x;
+  void* y;
+  int64_t x_token, x_head, y_token, y_head;
+  const void* norm;
+  int heads;
+};
+
+struct RotateArgs {
+  ecokv_rotary r;          // rot_dim 0: no rotation
+  RowSet q, k, v;          // v: append only, copied
+  const int32_t* positions;
+  int tokens, per;         // per: heads (of q, k and v together) a group takes
+  int chunks;              // ceil(heads / per)
+  float eps;
+  // append
+  ecokv_pages cache;
+  const int32_t* starts;
+  int batch;
+  int page_shift;
+  unsigned* status;
+};
+
+template <typename T>
+struct Vec;  // 8 elements, in 16-byte pieces
+template <>
+struct Vec<__nv_bfloat16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = v; }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Vec<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    reinterpret_cast<float4*>(p)[0] = a;
+    reinterpret_cast<float4*>(p)[1] = b;
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    a = make_float4(f[0], f[1], f[2], f[3]);
+    b = make_float4(f[4], f[5], f[6], f[7]);
+  }
+};
+
+// Norm and rotation of one row; every lane of its group takes part.
+template <typename T, bool kInter>
+__device__ __forceinline__ void turn_row(Vec<T>& v0, Vec<T>& v1, const float (&cs)[8], const float (&sn)[8],
+                                         bool turned, bool norm, const Vec<T>& w0, const Vec<T>& w1, float eps) {
+  float a[8], b[8];
+  v0.get(a);
+  v1.get(b);
+  if (norm) {
+    float ss = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      ss = fmaf(a[i], a[i], ss);
+      s1 = fmaf(b[i], b[i], s1);
+    }
+    ss += s1;
+#pragma unroll
+    for (int o = 1; o < kGroup; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    const float inv = 1.f / sqrtf(ss * (1.f / kD) + eps);
+    float wa[8], wb[8];
+    w0.get(wa);
+    w1.get(wb);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      a[i] = a[i] * inv * wa[i];
+      b[i] = b[i] * inv * wb[i];
+    }
+  }
+  if (turned) {
+    if constexpr (kInter) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = a[2 * i], y = a[2 * i + 1], z = b[2 * i], t = b[2 * i + 1];
+        a[2 * i] = x * cs[i] - y * sn[i];
+        a[2 * i + 1] = y * cs[i] + x * sn[i];
+        b[2 * i] = z * cs[4 + i] - t * sn[4 + i];
+        b[2 * i + 1] = t * cs[4 + i] + z * sn[4 + i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = a[i], y = b[i];
+        a[i] = x * cs[i] - y * sn[i];
+        b[i] = y * cs[i] + x * sn[i];
+      }
+    }
+  }
+  v0.set(a);
+  v1.set(b);
+}
+
+// The sequence of token t and its slot's page and row; row -1: none.
+struct Slot {
+  int64_t page;
+  int row;
+};
+__device__ __forceinline__ Slot find_slot(const RotateArgs& a, int t, int lane) {
+  int b = t, i = 0, n = 1;
+  if (a.starts != nullptr) {
+    // b = how many of starts[1 .. batch] are <= t: a warp's lanes read 32 of them
+    // at a time for its four tokens
+    const int g = lane >> 3;
+    b = 0;
+    for (int j0 = 0; j0 < a.batch; j0 += 32) {
+      const int s = j0 + lane < a.batch ? a.starts[1 + j0 + lane] : 0x7fffffff;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int n_le = __popc(__ballot_sync(0xffffffffu, s <= __shfl_sync(0xffffffffu, t, k * 8)));
+        if (k == g) b += n_le;
+      }
+    }
+    b = min(b, a.batch - 1);
+    const int s0 = a.starts[b];
+    i = t - s0;
+    n = a.starts[b + 1] - s0;
+  }
+  const long long slot = (long long)a.cache.lengths[b] - n + i;
+  const long long col = slot >> a.page_shift;
+  int row = -1;
+  int64_t page = 0;
+  if (slot >= 0 && col < a.cache.table_stride && i >= 0 && i < n) {
+    page = a.cache.table[(int64_t)b * a.cache.table_stride + col];
+    if (page >= 0 && page < a.cache.n_pages) row = (int)(slot & (a.cache.page_size - 1));
+  }
+  if (row < 0 && a.status != nullptr) {
+    if (atomicCAS(a.status, 0u, (unsigned)ECOKV_ERR_DEVICE_INDEX) == 0u) a.status[1] = (unsigned)b;
+  }
+  return {page, row};
+}
+
+template <typename T, bool kInter, bool kAppend>
+__global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant__ RotateArgs a) {
+  const int lane = threadIdx.x & 31, c = threadIdx.x & (kGroup - 1);
+  const long long unit = (long long)blockIdx.x * kGroups + threadIdx.x / kGroup;
+  // whole warps stay: a warp's groups share shuffles; one past the end repeats the last unit without storing
+  const long long last = (long long)a.tokens * a.chunks - 1;
+  const bool live = unit <= last;
+  const long long u = live ? unit : last;
+  const int t = (int)(u / a.chunks), r0 = (int)(u - (long long)t * a.chunks) * a.per;
+  const int F8 = a.r.rot_dim >> 4;  // lanes whose elements turn
+  const bool turned = c < F8;
+  // this lane's two eights of elements
+  const int e0 = !kInter && turned ? 8 * c : 16 * c;
+  const int e1 = !kInter && turned ? 8 * c + 8 * F8 : 16 * c + 8;
+  Slot at{0, -1};
+  if constexpr (kAppend) at = find_slot(a, t, lane);
+  float cs[8], sn[8];
+  const int n_turn = a.q.heads + a.k.heads;
+  if (turned && r0 < n_turn) {
+    uint64_t pos[ECOKV_ROTARY_AXES];
+#pragma unroll
+    for (int x = 0; x < ECOKV_ROTARY_AXES; ++x)
+      pos[x] = x < a.r.axes ? (uint64_t)(int64_t)a.positions[(int64_t)x * a.tokens + t] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int f = 8 * c + i, ax = a.r.axis[f];
+      const uint64_t p = ax == 0 ? pos[0] : ax == 1 ? pos[1] : ax == 2 ? pos[2] : pos[3];
+      // the upper 32 bits as a signed fraction of a turn: -1/2 .. 1/2, in half turns
+      const int32_t ph = (int32_t)((p * a.r.turns[f] + 0x80000000ull) >> 32);
+      float s_, c_;
+      sincospif((float)ph * 4.656612873077393e-10f, &s_, &c_);
+      cs[i] = c_ * a.r.magnitude;
+      sn[i] = s_ * a.r.magnitude;
+    }
+  }
+  const int n_all = n_turn + (kAppend ? a.v.heads : 0);
+  const int r1 = min(r0 + a.per, n_all);
+#pragma unroll 1
+  for (int seg = 0; seg < (kAppend ? 3 : 2); ++seg) {
+    const RowSet& s = seg == 0 ? a.q : seg == 1 ? a.k : a.v;
+    const int base = seg == 0 ? 0 : seg == 1 ? a.q.heads : n_turn;
+    const int lo = max(r0, base) - base, hi = min(r1, base + s.heads) - base;
+    // (the groups of a warp differ in their rows: the loop runs as long as the longest of them)
+    const int steps = (int)__reduce_max_sync(0xffffffffu, (unsigned)max(hi - lo, 0));
+    if (steps == 0) continue;
+    const bool norm = s.norm != nullptr;
+    Vec<T> w0{}, w1{};
+    if (norm) {
+      w0.load(static_cast<const T*>(s.norm) + e0);
+      w1.load(static_cast<const T*>(s.norm) + e1);
+    }
+    const T* x = static_cast<const T*>(s.x) + (int64_t)t * s.x_token;
+    T* y = static_cast<T*>(s.y) + (int64_t)t * s.y_token;
+    int64_t y_head = s.y_head;
+    bool store = live;
+    if (kAppend && seg > 0) {
+      y = static_cast<T*>(seg == 1 ? a.cache.k : a.cache.v) + at.page * a.cache.page_stride +
+          (int64_t)at.row * a.cache.slot_stride;
+      y_head = a.cache.head_stride;
+      store = live && at.row >= 0;
+    }
+    constexpr int kB = sizeof(T) == 2 ? 4 : 2;  // rows whose loads are in flight together
+#pragma unroll 1
+    for (int j = 0; j < steps; j += kB) {
+      Vec<T> v0[kB], v1[kB];
+#pragma unroll
+      for (int k = 0; k < kB; ++k)
+        if (lo + j + k < hi) {
+          v0[k].load(x + (int64_t)(lo + j + k) * s.x_head + e0);
+          v1[k].load(x + (int64_t)(lo + j + k) * s.x_head + e1);
+        }
+#pragma unroll
+      for (int k = 0; k < kB; ++k) {
+        if (!kAppend || seg < 2) turn_row<T, kInter>(v0[k], v1[k], cs, sn, turned, norm, w0, w1, a.eps);
+        if (store && lo + j + k < hi) {
+          v0[k].store(y + (int64_t)(lo + j + k) * y_head + e0);
+          v1[k].store(y + (int64_t)(lo + j + k) * y_head + e1);
+        }
+      }
+    }
+  }
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+bool stride_ok(int64_t s, size_t e) { return ((uint64_t)s * e & 15u) == 0; }
+
+bool rotary_ok(const ecokv_rotary& r) {
+  if (r.rot_dim < 16 || r.rot_dim > kD || r.rot_dim % 16 != 0) return false;
+  if (r.layout != ECOKV_ROTARY_HALF && r.layout != ECOKV_ROTARY_INTERLEAVED) return false;
+  if (r.axes < 1 || r.axes > ECOKV_ROTARY_AXES || !isfinite(r.magnitude)) return false;
+  for (int f = 0; f < r.rot_dim / 2; ++f)
+    if (r.axis[f] >= r.axes) return false;
+  return true;
+}
+
+// A row set with heads is complete and aligned; out: whether y is used.
+bool rows_ok(const ecokv_rows* s, size_t e, bool out) {
+  if (s == nullptr) return true;
+  if (s->heads < 1 || s->heads > (1 << 16) || !s->x || !aligned16(s->x) || !aligned16(s->norm)) return false;
+  if (!stride_ok(s->x_token, e) || !stride_ok(s->x_head, e)) return false;
+  if (out && (!s->y || !aligned16(s->y) || !stride_ok(s->y_token, e) || !stride_ok(s->y_head, e))) return false;
+  return true;
+}
+
+RowSet row_set(const ecokv_rows* s) {
+  RowSet r{};
+  if (s == nullptr) return r;
+  r.x = s->x;
+  r.y = s->y;
+  r.x_token = s->x_token;
+  r.x_head = s->x_head;
+  r.y_token = s->y_token;
+  r.y_head = s->y_head;
+  r.norm = s->norm;
+  r.heads = s->heads;
+  return r;
+}
+
+template <typename T, bool kAppend>
+cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
+  const long long units = (long long)a.tokens * a.chunks;
+  const unsigned grid = (unsigned)((units + kGroups - 1) / kGroups);
+  if (a.r.rot_dim > 0 && a.r.layout == ECOKV_ROTARY_INTERLEAVED)
+    rotate_kernel<T, true, kAppend><<<grid, kThreads, 0, st>>>(a);
+  else
+    rotate_kernel<T, false, kAppend><<<grid, kThreads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+// Heads a group takes: one while that still leaves SMs without a warp, then as
+// many as keep every SM at its resident groups, so that a token's sines are
+// formed for as many rows as possible.
+void set_split(RotateArgs& a, int heads) {
+  const long long rows = (long long)a.tokens * heads;
+  const long long per = rows / (152ll * kGroups * 6);
+  a.per = (int)(per < 1 ? 1 : per > heads ? heads : per);
+  a.chunks = (heads + a.per - 1) / a.per;
+}
+
+ecokv_status common(RotateArgs& a, const ecokv_rotary* r, const int32_t* positions, int32_t tokens, float eps) {
+  if (tokens < 0 || !(eps >= 0.f) || !isfinite(eps)) return ECOKV_ERR_INVALID_ARG;
+  if (r != nullptr) {
+    if (!rotary_ok(*r) || positions == nullptr || ((uintptr_t)positions & 3u)) return ECOKV_ERR_INVALID_ARG;
+    a.r = *r;
+  }
+  a.positions = positions;
+  a.tokens = tokens;
+  a.eps = eps;
+  return ECOKV_OK;
+}
+
+bool too_many(int32_t tokens, long long heads) { return (long long)tokens * heads > (1ll << 31) * (kGroups / 2); }
+
+}  // namespace
+}  // namespace ecokv
+
+using namespace ecokv;
+
+extern "C" {
+
+ecokv_status ecokv_rotary_set(ecokv_rotary* r, int32_t rot_dim, int32_t layout, const double* inv_freq,
+                              float magnitude) {
+  if (r == nullptr || inv_freq == nullptr) return ECOKV_ERR_INVALID_ARG;
+  ecokv_rotary n;
+  memset(&n, 0, sizeof(n));
+  n.rot_dim = rot_dim;
+  n.layout = layout;
+  n.axes = 1;
+  n.magnitude = magnitude;
+  if (!rotary_ok(n)) return ECOKV_ERR_INVALID_ARG;
+  for (int f = 0; f < rot_dim / 2; ++f) {
+    if (!isfinite(inv_freq[f])) return ECOKV_ERR_INVALID_ARG;
+    const double turns = inv_freq[f] / 6.283185307179586476925;
+    const double x = (turns - floor(turns)) * 18446744073709551616.0;  // exact: a power of two
+    n.turns[f] = x >= 18446744073709551616.0 ? 0 : (uint64_t)x;
+  }
+  *r = n;
+  return ECOKV_OK;
+}
+
+ecokv_status ecokv_rotary_init(ecokv_rotary* r, int32_t rot_dim, int32_t layout, double base, int32_t scaling,
+                               double factor, int32_t original) {
+  if (r == nullptr || rot_dim < 16 || rot_dim > kD || rot_dim % 16 != 0) return ECOKV_ERR_INVALID_ARG;
+  if (!(base > 0.0) || base == 1.0 || !isfinite(base)) return ECOKV_ERR_INVALID_ARG;
+  if (scaling < ECOKV_ROTARY_NONE || scaling > ECOKV_ROTARY_YARN) return ECOKV_ERR_INVALID_ARG;
+  if (scaling != ECOKV_ROTARY_NONE && (!(factor > 0.0) || !isfinite(factor))) return ECOKV_ERR_INVALID_ARG;
+  if (scaling == ECOKV_ROTARY_YARN && original < 1) return ECOKV_ERR_INVALID_ARG;
+  double freq[kD / 2];
+  if (scaling == ECOKV_ROTARY_NTK) base *= pow(factor, rot_dim / (rot_dim - 2.0));
+  for (int f = 0; f < rot_dim / 2; ++f) freq[f] = pow(base, -2.0 * f / rot_dim);
+  float magnitude = 1.f;
+  if (scaling == ECOKV_ROTARY_LINEAR)
+    for (int f = 0; f < rot_dim / 2; ++f) freq[f] /= factor;
+  if (scaling == ECOKV_ROTARY_YARN) {
+    // pair whose wavelength is original / turns: original inv_freq = 2 pi turns
+    const double pi2 = 6.283185307179586476925, lb = 2.0 * log(base);
+    double lo = floor(rot_dim * log(original / (pi2 * 32.0)) / lb);
+    double hi = ceil(rot_dim * log(original / pi2) / lb);
+    lo = lo > 0.0 ? lo : 0.0;
+    hi = hi < rot_dim - 1.0 ? hi : rot_dim - 1.0;
+    const double width = hi - lo > 1e-3 ? hi - lo : 1e-3;
+    for (int f = 0; f < rot_dim / 2; ++f) {
+      double w = (f - lo) / width;
+      w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+      freq[f] = freq[f] / factor * w + freq[f] * (1.0 - w);
+    }
+    magnitude = (float)(0.1 * log(factor) + 1.0);
+  }
+  return ecokv_rotary_set(r, rot_dim, layout, freq, magnitude);
+}
+
+ecokv_status ecokv_rotary_sections(ecokv_rotary* r, const int32_t* counts, int32_t axes) {
+  if (r == nullptr || counts == nullptr || axes < 1 || axes > ECOKV_ROTARY_AXES) return ECOKV_ERR_INVALID_ARG;
+  if (r->rot_dim < 16 || r->rot_dim > kD || r->rot_dim % 16 != 0) return ECOKV_ERR_INVALID_ARG;
+  long long sum = 0;
+  for (int x = 0; x < axes; ++x) {
+    if (counts[x] < 0) return ECOKV_ERR_INVALID_ARG;
+    sum += counts[x];
+  }
+  if (sum != r->rot_dim / 2) return ECOKV_ERR_INVALID_ARG;
+  int f = 0;
+  for (int x = 0; x < axes; ++x)
+    for (int i = 0; i < counts[x]; ++i) r->axis[f++] = (uint8_t)x;
+  r->axes = axes;
+  return ECOKV_OK;
+}
+
+ecokv_status ecokv_rotate(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_rows* q, const ecokv_rows* k,
+                          const int32_t* positions, int32_t tokens, float eps, void* stream) {
+  if (dtype != ECOKV_F32 && dtype != ECOKV_BF16) return ECOKV_ERR_INVALID_ARG;
+  const size_t e = dtype == ECOKV_F32 ? 4 : 2;
+  if (!rows_ok(q, e, true) || !rows_ok(k, e, true)) return ECOKV_ERR_INVALID_ARG;
+  RotateArgs a{};
+  const ecokv_status st = common(a, r, positions, tokens, eps);
+  if (st != ECOKV_OK) return st;
+  a.q = row_set(q);
+  a.k = row_set(k);
+  const int heads = a.q.heads + a.k.heads;
+  if (too_many(tokens, heads)) return ECOKV_ERR_UNSUPPORTED;
+  if (tokens == 0 || heads == 0) return ECOKV_OK;
+  set_split(a, heads);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t err = dtype == ECOKV_F32 ? launch<float, false>(a, s) : launch<__nv_bfloat16, false>(a, s);
+  return err == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
+}
+
+ecokv_status ecokv_append(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_rows* q, const ecokv_rows* k,
+                          const ecokv_rows* v, const ecokv_pages* cache, const int32_t* positions,
+                          const int32_t* starts, int32_t tokens, int32_t batch, float eps, void* ws,
+                          size_t ws_bytes, void* stream) {
+  if (dtype != ECOKV_F32 && dtype != ECOKV_BF16) return ECOKV_ERR_INVALID_ARG;
+  const size_t e = dtype == ECOKV_F32 ? 4 : 2;
+  if (k == nullptr || v == nullptr || !rows_ok(q, e, true) || !rows_ok(k, e, false) || !rows_ok(v, e, false))
+    return ECOKV_ERR_INVALID_ARG;
+  if (k->heads != v->heads || v->norm != nullptr) return ECOKV_ERR_INVALID_ARG;
+  ecokv_status st = check_pages(cache, batch, dtype);
+  if (st != ECOKV_OK) return st;
+  if ((uintptr_t)starts & 3u || (starts == nullptr && tokens != batch)) return ECOKV_ERR_INVALID_ARG;
+  if (ws != nullptr && (!aligned16(ws) || ws_bytes < 256)) return ECOKV_ERR_WORKSPACE;
+  RotateArgs a{};
+  st = common(a, r, positions, tokens, eps);
+  if (st != ECOKV_OK) return st;
+  a.q = row_set(q);
+  a.k = row_set(k);
+  a.v = row_set(v);
+  const int heads = a.q.heads + a.k.heads + a.v.heads;
+  if (too_many(tokens, heads)) return ECOKV_ERR_UNSUPPORTED;
+  if (tokens == 0) return ECOKV_OK;
+  a.cache = *cache;
+  a.starts = starts;
+  a.batch = batch;
+  a.page_shift = __builtin_ctz((unsigned)cache->page_size);
+  a.status = static_cast<unsigned*>(ws);
+  set_split(a, heads);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t err = dtype == ECOKV_F32 ? launch<float, true>(a, s) : launch<__nv_bfloat16, true>(a, s);
+  return err == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,7 +1,8 @@
-"""ctypes binding of libecokv.so: the C ABI of include/ecokv.h under the same
-names, plus small helpers that allocate outputs with torch.  Argument
-marshalling only: every step of the eviction pass runs in the library's CUDA
-kernels, and there is no fallback.  Importing this module does not load the
+"""ctypes binding of libecokv.so: the C ABI of include/ecokv.h and
+include/ecokv_decode.h under the same names, plus small helpers that allocate
+outputs with torch.  Argument marshalling only: every step of the eviction pass
+and of the decode step runs in the library's CUDA kernels, and there is no
+fallback.  Importing this module does not load the
 library; the first call does, and raises if it is missing.
 """
 from __future__ import annotations
@@ -32,7 +33,12 @@ STATUS = {0: "ECOKV_OK", 1: "ECOKV_ERR_INVALID_ARG", 2: "ECOKV_ERR_UNSUPPORTED",
 EXPORTS = ("ecokv_params_default", "ecokv_check_params", "ecokv_workspace_size", "ecokv_score",
            "ecokv_select", "ecokv_compact", "ecokv_evict", "ecokv_device_status", "ecokv_status_string",
            "ecokv_evict_noalloc", "ecokv_set_stage_events", "ecokv_workspace_size_host", "ecokv_evict_host",
-           "ecokv_evict_adaptive", "ecokv_evict_layered", "ecokv_pyramid_budgets")
+           "ecokv_evict_adaptive", "ecokv_evict_layered", "ecokv_pyramid_budgets",
+           "ecokv_rotary_init", "ecokv_rotary_set", "ecokv_rotary_sections", "ecokv_rotate", "ecokv_append",
+           "ecokv_attend_workspace_size", "ecokv_attend")
+ROTARY_LAYOUT = {"half": 0, "interleaved": 1}
+ROTARY_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+HEAD_DIM = 128
 
 
 class EcokvError(RuntimeError):
@@ -56,6 +62,33 @@ class ecokv_params(ctypes.Structure):
 _lib = None
 _P = ctypes.POINTER(ecokv_params)
 _vp, _sz = ctypes.c_void_p, ctypes.c_size_t
+_i32, _i64 = ctypes.c_int32, ctypes.c_int64
+
+
+class ecokv_rotary(ctypes.Structure):
+    _fields_ = [("rot_dim", _i32), ("layout", _i32), ("axes", _i32), ("magnitude", ctypes.c_float),
+                ("turns", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+class ecokv_rows(ctypes.Structure):
+    _fields_ = [("x", _vp), ("y", _vp), ("x_token", _i64), ("x_head", _i64), ("y_token", _i64), ("y_head", _i64),
+                ("norm", _vp), ("heads", _i32)]
+
+
+class ecokv_pages(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("page_stride", _i64), ("head_stride", _i64), ("slot_stride", _i64),
+                ("n_pages", _i32), ("page_size", _i32), ("table", _vp), ("table_stride", _i32), ("lengths", _vp)]
+
+
+class ecokv_prefix(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("head_stride", _i64), ("row_stride", _i64), ("rows", _i32),
+                ("head_off", _vp)]
+
+
+class ecokv_attend_params(ctypes.Structure):
+    _fields_ = [("h_q", _i32), ("h_kv", _i32), ("d", _i32), ("tokens", _i32), ("batch", _i32),
+                ("scale", ctypes.c_float), ("q_token", _i64), ("q_head", _i64), ("out_token", _i64),
+                ("out_head", _i64), ("flags", ctypes.c_uint32), ("timeout_us", ctypes.c_uint32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -95,6 +128,25 @@ def lib() -> ctypes.CDLL:
         L.ecokv_pyramid_budgets.restype = ctypes.c_int
         L.ecokv_set_stage_events.argtypes = [ctypes.POINTER(_vp), ctypes.c_int]
         L.ecokv_set_stage_events.restype = ctypes.c_int
+        f32, rows = ctypes.c_float, ctypes.POINTER(ecokv_rows)
+        L.ecokv_rotary_init.argtypes = [ctypes.POINTER(ecokv_rotary), _i32, _i32, ctypes.c_double, _i32,
+                                        ctypes.c_double, _i32]
+        L.ecokv_rotary_init.restype = ctypes.c_int
+        L.ecokv_rotary_set.argtypes = [ctypes.POINTER(ecokv_rotary), _i32, _i32, _vp, f32]
+        L.ecokv_rotary_set.restype = ctypes.c_int
+        L.ecokv_rotary_sections.argtypes = [ctypes.POINTER(ecokv_rotary), _vp, _i32]
+        L.ecokv_rotary_sections.restype = ctypes.c_int
+        L.ecokv_rotate.argtypes = [ctypes.POINTER(ecokv_rotary), ctypes.c_int, rows, rows, _vp, _i32, f32, _vp]
+        L.ecokv_rotate.restype = ctypes.c_int
+        L.ecokv_append.argtypes = [ctypes.POINTER(ecokv_rotary), ctypes.c_int, rows, rows, rows,
+                                   ctypes.POINTER(ecokv_pages), _vp, _vp, _i32, _i32, f32, _vp, _sz, _vp]
+        L.ecokv_append.restype = ctypes.c_int
+        L.ecokv_attend_workspace_size.argtypes = [_i32, _i32, _i32, _i32, ctypes.c_int]
+        L.ecokv_attend_workspace_size.restype = _sz
+        L.ecokv_attend.argtypes = [ctypes.POINTER(ecokv_attend_params), ctypes.c_int, _vp,
+                                   ctypes.POINTER(ecokv_prefix), ctypes.POINTER(ecokv_pages), _vp, _vp, _vp, _vp,
+                                   _sz, _vp]
+        L.ecokv_attend.restype = ctypes.c_int
         L.ecokv_device_status.argtypes = [_vp, _vp]
         L.ecokv_device_status.restype = ctypes.c_int
         L.ecokv_status_string.argtypes = [ctypes.c_int]
@@ -204,6 +256,39 @@ def ecokv_set_stage_events(events) -> int:
     hs = [e.cuda_event if hasattr(e, "cuda_event") else int(e) for e in events]
     arr = (_vp * len(hs))(*hs)
     return lib().ecokv_set_stage_events(arr, len(hs))
+
+
+def ecokv_rotary_init(r, rot_dim, layout, base, scaling=0, factor=1.0, original=0) -> int:
+    return lib().ecokv_rotary_init(r, rot_dim, layout, base, scaling, factor, original)
+
+
+def ecokv_rotary_set(r, rot_dim, layout, inv_freq, magnitude=1.0) -> int:
+    """inv_freq: rot_dim / 2 radians a position, or None."""
+    f = None if inv_freq is None else (ctypes.c_double * len(inv_freq))(*inv_freq)
+    return lib().ecokv_rotary_set(r, rot_dim, layout, f, magnitude)
+
+
+def ecokv_rotary_sections(r, counts) -> int:
+    return lib().ecokv_rotary_sections(r, (_i32 * len(counts))(*counts), len(counts))
+
+
+def ecokv_rotate(r, dtype, q, k, positions, tokens, eps, stream=None) -> int:
+    return lib().ecokv_rotate(r, dtype, q, k, _ptr(positions), tokens, eps, _stream(stream))
+
+
+def ecokv_append(r, dtype, q, k, v, cache, positions, starts, tokens, batch, eps, ws=None, ws_bytes=0,
+                 stream=None) -> int:
+    return lib().ecokv_append(r, dtype, q, k, v, cache, _ptr(positions), _ptr(starts), tokens, batch, eps, _ptr(ws),
+                              ws_bytes, _stream(stream))
+
+
+def ecokv_attend_workspace_size(tokens, batch, h_q, h_kv, dtype) -> int:
+    return lib().ecokv_attend_workspace_size(tokens, batch, h_q, h_kv, dtype)
+
+
+def ecokv_attend(p, dtype, q, prefix, cache, starts, out, lse, ws, ws_bytes, stream=None) -> int:
+    return lib().ecokv_attend(p, dtype, _ptr(q), prefix, cache, _ptr(starts), _ptr(out), _ptr(lse), _ptr(ws),
+                              ws_bytes, _stream(stream))
 
 
 def ecokv_device_status(ws, stream=None) -> int:
@@ -358,3 +443,227 @@ def evict_noalloc(p, K, V, Qwin, want_scores=False, stream=None):
     _check(ecokv_evict_noalloc(p, dtype_code(K), K, V, Qwin, idx, Ko, Vo, S, lam, code, stream),
            "ecokv_evict_noalloc")
     return idx, Ko, Vo, S, lam, int(code.item())
+
+
+# ---------------------------------------------------------------- the decode step
+# A call runs on `stream` (a torch.cuda.Stream or a raw handle), by default on
+# torch's current one.  Tensors that are not given are allocated by the helper.
+def rotary(rot_dim=HEAD_DIM, base=10000.0, layout="half", scaling="none", factor=1.0, original=0, sections=None,
+           inv_freq=None, magnitude=1.0) -> ecokv_rotary:
+    """Rotary positions of a model, kept for its calls.  scaling: "none",
+    "linear", "ntk" or "yarn" (the last needs `original`); inv_freq: the caller's
+    own frequencies (with `magnitude`) in place of base and scaling; sections:
+    pairs each position axis turns (time, height, width ...), default one axis."""
+    r = ecokv_rotary()
+    lay = ROTARY_LAYOUT[layout]
+    if inv_freq is not None:
+        inv_freq = [float(f) for f in inv_freq]
+        if len(inv_freq) != rot_dim // 2:
+            raise ValueError(f"{len(inv_freq)} frequencies for {rot_dim // 2} pairs")
+        _check(ecokv_rotary_set(r, rot_dim, lay, inv_freq, magnitude), "ecokv_rotary_set")
+    else:
+        _check(ecokv_rotary_init(r, rot_dim, lay, base, ROTARY_SCALING[scaling], factor, original),
+               "ecokv_rotary_init")
+    if sections is not None:
+        _check(ecokv_rotary_sections(r, sections), "ecokv_rotary_sections")
+    return r
+
+
+def _dtype(*tensors) -> int:
+    """Their common dtype's code; all of them on one CUDA device."""
+    t = tensors[0]
+    code = dtype_code(t)
+    for x in tensors:
+        if x is not None:
+            if not x.is_cuda:
+                raise ValueError("CUDA tensors are wanted")
+            if x.dtype != t.dtype or x.device != t.device:
+                raise TypeError(f"{x.dtype} on {x.device} next to {t.dtype} on {t.device}")
+    return code
+
+
+def _ints(x, shape, what):
+    import torch
+    if x is None:
+        return None
+    if x.dtype != torch.int32 or not x.is_cuda or not x.is_contiguous() or (shape and tuple(x.shape) != shape):
+        raise ValueError(f"{what}: a contiguous int32 CUDA tensor{f' of shape {shape}' if shape else ''} is wanted")
+    return x.data_ptr()
+
+
+def _strides(x):
+    """Strides in elements; one that is never taken (an axis of one or none) counts as a row."""
+    return tuple(s if n > 1 else HEAD_DIM for n, s in zip(x.shape[:-1], x.stride())) + x.stride()[-1:]
+
+
+def _heads(x, what):
+    """Rows [tokens, heads, d]: their strides."""
+    s = _strides(x)
+    if x.dim() != 3 or x.shape[2] != HEAD_DIM or s[2] != 1:
+        raise ValueError(f"{what}: rows [tokens, heads, {HEAD_DIM}] with the last axis contiguous are wanted")
+    return s
+
+
+def _rows(x, y, norm, what):
+    sx = _heads(x, what)
+    r = ecokv_rows(x.data_ptr(), None, sx[0], sx[1], 0, 0, None, x.shape[1])
+    if y is not None:
+        sy = _heads(y, what)
+        if y.shape != x.shape:
+            raise ValueError(f"{what}: the output has another shape")
+        r.y, r.y_token, r.y_head = y.data_ptr(), sy[0], sy[1]
+    if norm is not None:
+        if norm.shape != (HEAD_DIM,) or norm.stride(0) != 1:
+            raise ValueError(f"{what}: norm weights [{HEAD_DIM}] are wanted")
+        r.norm = norm.data_ptr()
+    return r
+
+
+def _on(stream, t, *made):
+    """The raw stream to launch on; tensors made here are kept from reuse until it is done with them."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(t.device).cuda_stream
+    if isinstance(stream, int):
+        return stream
+    for x in made:
+        if x is not None:
+            x.record_stream(stream)
+    return stream.cuda_stream
+
+
+def rotate(rot, positions, q, k=None, q_norm=None, k_norm=None, eps=1e-6, q_out=None, k_out=None, stream=None):
+    """Run ecokv_rotate: norm (where weights are given) and rotary positions of
+    q and k [tokens, heads, 128].  rot: from rotary(), None for the norms alone;
+    positions int32 [axes, tokens] (or [tokens]).  Outputs may have any strides
+    (k_out a view of the [heads, tokens, 128] that the eviction pass reads) or be
+    the inputs.  Returns (q_out, k_out)."""
+    import torch
+    made = []
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        made.append(q_out)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        made.append(k_out)
+    dt = _dtype(q, k, q_norm, k_norm, q_out, k_out)
+    tokens = q.shape[0]
+    if k is not None and k.shape[0] != tokens:
+        raise ValueError("q and k have different numbers of tokens")
+    pos = _positions(rot, positions, tokens)
+    _check(lib().ecokv_rotate(rot, dt, _rows(q, q_out, q_norm, "q"),
+                              None if k is None else _rows(k, k_out, k_norm, "k"), pos, tokens, eps,
+                              _on(stream, q, *made)), "ecokv_rotate")
+    return q_out, k_out
+
+
+def _positions(rot, positions, tokens):
+    if rot is None:
+        return None
+    if positions is None:
+        raise ValueError("positions are wanted")
+    if positions.numel() != rot.axes * tokens or positions.shape[-1] != tokens:
+        raise ValueError(f"positions: [{rot.axes}, {tokens}] is wanted")
+    return _ints(positions, None, "positions")
+
+
+class PagedCache:
+    """A paged cache: k_pages, v_pages [n_pages, h_kv, page_size, 128] (views of
+    any strides, the same for both, the last axis contiguous), table int32
+    [batch, pages a sequence], lengths int32 [batch].  Holds its tensors; table and
+    lengths are read on the device by every call."""
+
+    def __init__(self, k_pages, v_pages, table, lengths):
+        _dtype(k_pages, v_pages)
+        s = _strides(k_pages)
+        if k_pages.dim() != 4 or k_pages.shape[3] != HEAD_DIM or s[3] != 1:
+            raise ValueError(f"pages [n_pages, h_kv, page_size, {HEAD_DIM}] with the last axis contiguous are wanted")
+        if v_pages.shape != k_pages.shape or _strides(v_pages) != s:
+            raise ValueError("k_pages and v_pages have different shapes or strides")
+        if table.dim() != 2 or tuple(lengths.shape) != (table.shape[0],):
+            raise ValueError("table [batch, pages a sequence] and lengths [batch] are wanted")
+        self.k_pages, self.v_pages, self.table, self.lengths = k_pages, v_pages, table, lengths
+        self.batch, self.h_kv = table.shape[0], k_pages.shape[1]
+        self.c = ecokv_pages(k_pages.data_ptr(), v_pages.data_ptr(), s[0], s[1], s[2], k_pages.shape[0],
+                             k_pages.shape[2], _ints(table, None, "table"), table.shape[1],
+                             _ints(lengths, None, "lengths"))
+
+
+class Prefix:
+    """The shared prefix of one layer: k, v [h_kv, rows, 128] as evict() returns a
+    layer, or [rows, 128] with head_off int32 [h_kv + 1] as evict_adaptive() does."""
+
+    def __init__(self, k, v, head_off=None):
+        _dtype(k, v)
+        s = _strides(k)
+        if k.dim() != (3 if head_off is None else 2) or k.shape[-1] != HEAD_DIM or s[-1] != 1:
+            raise ValueError(f"prefix: [h_kv, rows, {HEAD_DIM}], or [rows, {HEAD_DIM}] with head_off, is wanted")
+        if v.shape != k.shape or _strides(v) != s:
+            raise ValueError("k and v have different shapes or strides")
+        self.k, self.v, self.head_off = k, v, head_off
+        self.h_kv = k.shape[0] if head_off is None else head_off.shape[0] - 1
+        self.c = ecokv_prefix(k.data_ptr(), v.data_ptr(), s[0] if head_off is None else 0, s[-2], k.shape[-2],
+                              _ints(head_off, None, "head_off"))
+
+
+def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm=None, k_norm=None, eps=1e-6,
+           q_out=None, ws=None, stream=None):
+    """Run ecokv_append: k (normed, rotated) and v [tokens, h_kv, 128] into the
+    cache's slots, q (normed, rotated) to q_out, which is returned.  starts int32
+    [batch + 1]: None = one token a sequence.  ws: a workspace whose status word
+    takes device-side errors."""
+    import torch
+    made = None
+    if q is not None and q_out is None:
+        made = q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    dt = _dtype(k, v, cache.k_pages, q, q_norm, k_norm, q_out)
+    tokens = k.shape[0]
+    if v.shape != k.shape or k.shape[1] != cache.h_kv or (q is not None and q.shape[0] != tokens):
+        raise ValueError("k, v and q do not fit together or the cache")
+    _check(lib().ecokv_append(rotary, dt, None if q is None else _rows(q, q_out, q_norm, "q"),
+                              _rows(k, None, k_norm, "k"), _rows(v, None, None, "v"), cache.c,
+                              _positions(rotary, positions, tokens), _ints(starts, (cache.batch + 1,), "starts"), tokens,
+                              cache.batch, eps, _ptr(ws), 0 if ws is None else ws.numel(), _on(stream, k, made)),
+           "ecokv_append")
+    return q_out
+
+
+def alloc_attend_workspace(tokens, batch, h_q, h_kv, dtype, device="cuda"):
+    """Workspace of attend() for up to `tokens` tokens of `batch` sequences (dtype: torch's)."""
+    import torch
+    n = ecokv_attend_workspace_size(tokens, batch, h_q, h_kv, ECOKV_F32 if dtype == torch.float32 else ECOKV_BF16)
+    if n == 0:
+        raise EcokvError(ECOKV_ERR_INVALID_ARG, "ecokv_attend_workspace_size")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None, flags=0, timeout_us=0, stream=None):
+    """Run ecokv_attend: q [tokens, h_q, 128] over prefix (a Prefix or None) and
+    cache (a PagedCache or None); returns out [tokens, h_q, 128].  starts int32
+    [batch + 1]: None = one token a sequence.  lse: float32 [tokens, h_q] to fill."""
+    import torch
+    made = []
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        made.append(out)
+    if prefix is None and cache is None:
+        raise ValueError("a prefix or a cache is wanted")
+    dt = _dtype(q, out, None if prefix is None else prefix.k, None if cache is None else cache.k_pages)
+    sq, so = _heads(q, "q"), _heads(out, "out")
+    tokens, h_q = q.shape[0], q.shape[1]
+    h_kv = prefix.h_kv if cache is None else cache.h_kv
+    if out.shape != q.shape or (prefix is not None and prefix.h_kv != h_kv):
+        raise ValueError("out or the prefix does not fit")
+    batch = 1 if cache is None else cache.batch
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (tokens, h_q) or
+                            not lse.is_contiguous() or not lse.is_cuda):
+        raise ValueError("lse: a contiguous float32 [tokens, h_q] CUDA tensor is wanted")
+    if ws is None:
+        ws = alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device)
+        made.append(ws)
+    p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, sq[0], sq[1], so[0], so[1], flags, timeout_us)
+    _check(lib().ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
+                              None if cache is None else cache.c,
+                              None if cache is None else _ints(starts, (batch + 1,), "starts"), out.data_ptr(),
+                              _ptr(lse), ws.data_ptr(), ws.numel(), _on(stream, q, *made)), "ecokv_attend")
+    return out
