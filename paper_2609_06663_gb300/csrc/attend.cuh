@@ -37,6 +37,7 @@ struct AttendArgs {
   int span;   // tokens an item holds (one or two row tiles)
   int parts;  // partial sums a CTA may have of a row: 2 where two row groups share the tiles
   int P;      // CTAs
+  int stall;  // fault injection: the first CTA's copies never come
   float scale_log2;
   unsigned long long timeout_ns;
   // workspace
@@ -292,6 +293,7 @@ __device__ __forceinline__ size_t next_row(const AttendArgs& a, int cta, int j, 
 
 ecokv_status check_pages(const ecokv_pages* c, int32_t batch, ecokv_dtype dt);
 cudaError_t launch_attend_simt(const AttendArgs& a, ecokv_dtype dt, cudaStream_t st);
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st);
 cudaError_t launch_attend_join(const AttendArgs& a, ecokv_dtype dt, cudaStream_t st);
 
 }  // namespace ecokv

@@ -222,7 +222,10 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   if (p == nullptr || !sizes_ok(p->tokens, p->batch, p->h_q, p->h_kv) || p->d < 1) return ECOKV_ERR_INVALID_ARG;
   if (dtype != ECOKV_F32 && dtype != ECOKV_BF16) return ECOKV_ERR_INVALID_ARG;
   const size_t e = dtype == ECOKV_F32 ? 4 : 2;
-  if ((p->flags & ~ECOKV_FLAG_FORCE_SIMT) != 0u || !isfinite(p->scale)) return ECOKV_ERR_INVALID_ARG;
+  if ((p->flags & ~(ECOKV_FLAG_FORCE_SIMT | ECOKV_FLAG_TEST_STALL)) != 0u || !isfinite(p->scale))
+    return ECOKV_ERR_INVALID_ARG;
+  const bool tc = dtype == ECOKV_BF16 && (p->flags & ECOKV_FLAG_FORCE_SIMT) == 0u;
+  if ((p->flags & ECOKV_FLAG_TEST_STALL) != 0u && !tc) return ECOKV_ERR_UNSUPPORTED;  // the waits are on that path
   if (p->d != kD || p->h_q / p->h_kv > kMaxGroup) return ECOKV_ERR_UNSUPPORTED;
   if (!q || !out || !aligned16(q) || !aligned16(out) || ((uintptr_t)lse & 3u)) return ECOKV_ERR_INVALID_ARG;
   if (p->q_token < 0 || p->q_head < 0 || p->out_token < 0 || p->out_head < 0 || !stride_ok(p->q_token, e) ||
@@ -262,9 +265,10 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   a.h_q = p->h_q;
   a.h_kv = p->h_kv;
   a.g = p->h_q / p->h_kv;
-  a.tpt = 64 / a.g;
-  a.span = a.tpt;
-  a.parts = 1;
+  a.tpt = (tc ? kTileRows : 64) / a.g;
+  a.span = tc ? 2 * a.tpt : a.tpt;
+  a.parts = tc ? 2 : 1;
+  a.stall = (p->flags & ECOKV_FLAG_TEST_STALL) ? 1 : 0;
   a.P = attend_sms();
   const double scale = p->scale > 0.f ? (double)p->scale : 1.0 / sqrt((double)kD);
   a.scale_log2 = (float)(1.4426950408889634 * scale);
@@ -282,7 +286,7 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   a.first_o = reinterpret_cast<float*>(w + L.first_o);
   a.next_o = reinterpret_cast<float*>(w + L.next_o);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_attend_simt(a, dtype, s) != cudaSuccess) return ECOKV_ERR_CUDA;
+  if ((tc ? launch_attend_tc(a, s) : launch_attend_simt(a, dtype, s)) != cudaSuccess) return ECOKV_ERR_CUDA;
   return launch_attend_join(a, dtype, s) == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
 }
 

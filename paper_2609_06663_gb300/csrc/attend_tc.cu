@@ -1,0 +1,494 @@
+// Attention of the decode step on the tensor cores (bf16): items and tiles as in
+// attend.cuh, one persistent CTA an SM.
+//
+// A row tile is 128 rows = tpt tokens x g query heads of one KV head, the M of both
+// products.  S = Q K^T goes to tensor memory, a thread a row takes it through the
+// softmax and leaves the weights there as bf16, from where the second product O +=
+// P V reads them; O stays in tensor memory through the item.  Two warpgroups ("streams") do
+// the softmax of alternating jobs, so that one's exponentials run beside the
+// other's products: the jobs of an item are its two row tiles on each key tile, or, with
+// one row tile, the key tiles in turn, whose sums then are two parts of the row.
+// The maximum that weights refer to is raised, and O rescaled, only when a tile
+// exceeds it by 2^8: the weights are fp32 before they are rounded, so that any
+// reference within their range is as exact.
+//
+// Warps: 0 copies (TMA; a lane a page), 1 MMAs, 2 the walk over the items, 3 tensor
+// memory, 4-7 and 8-11 the streams.
+
+#include <atomic>
+
+#include "attend.cuh"
+#include "ptx.cuh"
+#include "tc_pass.cuh"
+#include "tc_tile.cuh"
+
+namespace ecokv {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 384;
+constexpr int kStages = 5;          // tiles of K or V in the ring
+constexpr int kItems = 4;           // items ahead of their consumers
+constexpr uint32_t kHalf = kTileBytes / 2;  // 128 rows x 64 columns
+constexpr float kRaise = 8.f;       // log2 units
+
+struct Smem {
+  uint8_t q[2][kTileBytes];
+  uint8_t ring[kStages][kTileBytes];
+  uint64_t full[kStages], empty[kStages];
+  uint64_t qfull[2], qempty[2];
+  uint64_t sfull[2], pready[2], ofull[2];
+  uint64_t ifull[kItems], iempty[kItems];
+  uint64_t drained;
+  Item items[kItems];
+  uint32_t tmem;
+  volatile int abort;
+};
+
+static_assert(sizeof(Smem) + 1024 <= 232448, "one CTA's shared memory");
+
+struct Maps {
+  CUtensorMap q, pk, pv, ck, cv;
+};
+
+// Bounded wait: false once this CTA has given up.
+__device__ __forceinline__ bool wait_bar(Smem& s, const AttendArgs& a, uint64_t* bar, uint32_t parity, unsigned where) {
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  const unsigned long long t0 = now_ns();
+  while (!mbar_try_wait(bar, parity)) {
+    if (s.abort) return false;
+    if (now_ns() - t0 > a.timeout_ns) {
+      s.abort = 1;
+      note(a, ECOKV_ERR_TIMEOUT, where);
+      return false;
+    }
+  }
+  return true;
+}
+// A whole warp's wait.
+__device__ __forceinline__ bool wait_warp(Smem& s, const AttendArgs& a, uint64_t* bar, uint32_t parity,
+                                          unsigned where) {
+  return __all_sync(0xffffffffu, wait_bar(s, a, bar, parity, where)) != 0;
+}
+
+// The next item of the queue, for a warp; false: none left, or given up.
+struct ItemReader {
+  uint32_t n = 0;
+  __device__ __forceinline__ bool next(Smem& s, const AttendArgs& a, Item& it, int lane) {
+    const uint32_t e = n % kItems;
+    if (!wait_warp(s, a, &s.ifull[e], (n / kItems) & 1, 1u)) return false;
+    it = s.items[e];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&s.iempty[e]);
+    ++n;
+    return it.ntiles > 0;
+  }
+};
+
+__device__ __forceinline__ void store8(float* p, const uint32_t* r) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
+// Copies of one tile of K (or V) into a stage: its pages' rows, a lane a page, or the prefix's.
+__device__ __forceinline__ void copy_tile(const AttendArgs& a, const CUtensorMap* prefix, const CUtensorMap* pages,
+                                          const Item& it, int tile, int page, int n_pages, uint8_t* dst,
+                                          uint64_t* bar, int lane) {
+  if (it.source == 0) {
+    if (lane < 2)
+      tma_load_3d(dst + lane * kHalf, prefix, bar, lane * 64, it.row0 + tile * kKeys,
+                  a.prefix.head_off != nullptr ? 0 : it.head);
+  } else if (lane < n_pages) {
+    const int slot = a.page_shift >= 7 ? (tile * kKeys) & (a.cache.page_size - 1) : 0;
+    uint8_t* at = dst + ((lane << a.page_shift) & (kKeys - 1)) * 128;
+    tma_load_4d(at, pages, bar, 0, slot, it.head, page);
+    tma_load_4d(at + kHalf, pages, bar, 64, slot, it.head, page);
+  }
+}
+
+// load, ql: tiles of K and V, and of Q, whose copies have been issued.
+__device__ __forceinline__ void produce(Smem& s, const AttendArgs& a, const Maps& m, int lane, uint32_t& load,
+                                        uint32_t& ql) {
+  ItemReader items;
+  Item it;
+  const int q_bytes = a.tpt * a.g * 256;
+  while (items.next(s, a, it, lane)) {
+    const int nq = it.ntok > a.tpt ? 2 : 1;
+    for (int r = 0; r < nq; ++r) {
+      const int slot = ql & 1;
+      if (!wait_warp(s, a, &s.qempty[slot], ((ql >> 1) & 1) ^ 1, 2u)) return;
+      if (lane == 0) mbar_expect_tx(&s.qfull[slot], (uint32_t)q_bytes);
+      __syncwarp();
+      if (lane < 2)
+        tma_load_3d(s.q[slot] + lane * kHalf, &m.q, &s.qfull[slot], lane * 64, it.head * a.g, it.tok0 + r * a.tpt);
+      ++ql;
+    }
+    for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
+      int n_pages = 0, page = 0;
+      uint32_t bytes = kTileBytes;
+      if (it.source != 0) {
+        const int from = t * kKeys, to = min(from + kKeys, it.vis);
+        const int c0 = from >> a.page_shift;
+        n_pages = ((to - 1) >> a.page_shift) - c0 + 1;
+        bytes = (uint32_t)(min(a.cache.page_size, kKeys) * n_pages) * 256u;
+        if (lane < n_pages) {
+          page = a.cache.table[(int64_t)it.seq * a.cache.table_stride + c0 + lane];
+          if (page < 0 || page >= a.cache.n_pages) {
+            note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)it.seq);
+            page = a.cache.n_pages;  // out of the map's bounds: zeros
+          }
+        }
+      }
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const uint32_t st = load % kStages;
+        if (!wait_warp(s, a, &s.empty[st], ((load / kStages) & 1) ^ 1, 3u)) return;
+        if (lane == 0) mbar_expect_tx(&s.full[st], bytes);
+        __syncwarp();
+        copy_tile(a, kv == 0 ? &m.pk : &m.pv, kv == 0 ? &m.ck : &m.cv, it, t, page, n_pages, s.ring[st], &s.full[st],
+                  lane);
+        ++load;
+      }
+    }
+  }
+}
+
+// A job whose weights are awaited for the second product.
+struct Job {
+  bool any, first, last_v, last;  // first, last: of its stream in the item; last_v: last to read its tile of V
+  uint32_t stream, k, load;       // k: jobs of the stream before it
+};
+
+__device__ __forceinline__ bool second_product(Smem& s, const AttendArgs& a, const Job& j, uint32_t tmem) {
+  constexpr uint32_t idesc = idesc_bf16(128, 128, false, true);
+  const uint32_t st = j.load % kStages;
+  if (!wait_warp(s, a, &s.full[st], (j.load / kStages) & 1, 4u)) return false;
+  if (!wait_warp(s, a, &s.pready[j.stream], j.k & 1, 5u)) return false;
+  tc_fence_after();
+  if (elect_one()) {
+    const uint32_t p = tmem + j.stream * 256u, o = p + 128u;
+    const uint64_t vd = smem_desc(smem_u32(s.ring[st]), kHalf, 1024, 2);
+#pragma unroll
+    for (int k8 = 0; k8 < 8; ++k8)  // 16 keys a step
+      mma_bf16_ta(o, p + k8 * 8u, vd + (uint64_t)(k8 * 128), idesc, k8 > 0 || !j.first ? 1u : 0u);
+    if (j.last_v) mma_commit(&s.empty[st]);
+    if (j.last) mma_commit(&s.ofull[j.stream]);
+  }
+  __syncwarp();
+  return true;
+}
+
+__device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t tmem, int lane) {
+  constexpr uint32_t idesc = idesc_bf16(128, 128, false, false);
+  ItemReader items;
+  Item it;
+  Job prev{};
+  uint32_t n = 0, load = 0, ql = 0;  // jobs, tiles of K and V, tiles of Q so far
+  while (items.next(s, a, it, lane)) {
+    const int nq = it.ntok > a.tpt ? 2 : 1;
+    for (int t = 0; t < it.ntiles; ++t, load += 2) {
+      const uint32_t st = load % kStages;
+      for (int r = 0; r < nq; ++r, ++n) {
+        const uint32_t q = ql + r, i = n & 1;
+        if (t == 0 && !wait_warp(s, a, &s.qfull[q & 1], (q >> 1) & 1, 6u)) return;
+        if (r == 0 && !wait_warp(s, a, &s.full[st], (load / kStages) & 1, 7u)) return;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t qd = smem_desc(smem_u32(s.q[q & 1]), 16, 1024, 2);
+          const uint64_t kd = smem_desc(smem_u32(s.ring[st]), 16, 1024, 2);
+#pragma unroll
+          for (int k8 = 0; k8 < 8; ++k8) {
+            const uint64_t d = (uint64_t)((k8 >> 2) * (kHalf >> 4) + (k8 & 3) * 2);
+            mma_bf16(tmem + i * 256u, qd + d, kd + d, idesc, k8 > 0 ? 1u : 0u);
+          }
+          mma_commit(&s.sfull[i]);
+          if (r == nq - 1) mma_commit(&s.empty[st]);
+          if (t == it.ntiles - 1) mma_commit(&s.qempty[q & 1]);
+        }
+        __syncwarp();
+        if (prev.any && !second_product(s, a, prev, tmem)) return;
+        prev.any = true;
+        prev.first = nq == 2 ? t == 0 : t < 2;
+        prev.last = nq == 2 ? t == it.ntiles - 1 : t >= it.ntiles - 2;
+        prev.last_v = r == nq - 1;
+        prev.stream = i;
+        prev.k = n >> 1;
+        prev.load = load + 1;
+      }
+    }
+    ql += nq;
+  }
+  if (prev.any) second_product(s, a, prev, tmem);
+}
+
+__device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tmem, int stream) {
+  const int lane = threadIdx.x & 31, row = threadIdx.x & 127, warp = row >> 5;
+  const uint32_t ts = tmem + (uint32_t)stream * 256u + ((uint32_t)(warp * 32) << 16), to = ts + 128u;
+  const int row_k = row / a.g;
+  const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
+  ItemReader items;
+  Item it;
+  uint32_t n0 = 0, tile_n = 0, k = 0, ends = 0;  // jobs and tiles before the item; this stream's jobs; its items
+  while (items.next(s, a, it, lane)) {
+    const bool two = it.ntok > a.tpt;
+    const int p = (stream ^ (int)n0) & 1;  // which of the item's row tiles, or of its key tiles in turn
+    const int tok = two ? p * a.tpt : 0;
+    const int rows = min(it.ntok - tok, a.tpt) * a.g;
+    const bool active = warp * 32 < rows;
+    const int lim = it.lim0 + (tok + row_k) * it.slope;
+    float m = -INFINITY, l = 0.f;
+    const int step = two ? 1 : 2, t0 = two ? 0 : p;
+    for (int t = t0; t < it.ntiles; t += step, ++k) {
+      const int from = (it.tile0 + t) * kKeys;
+      const int nv = it.vis - from;  // keys of the tile that are there (128 or more: all)
+      if (!wait_warp(s, a, &s.sfull[stream], k & 1, 8u)) return;
+      tc_fence_after();
+      if (active) {
+        uint32_t x[kKeys];
+        tmem_ld<kKeys>(ts, x);
+        tmem_wait_ld();
+        tmem_landed(x);
+        const int seen = lim - from;
+        if (!__all_sync(0xffffffffu, seen >= kKeys)) {
+#pragma unroll
+          for (int c = 0; c < kKeys; ++c)
+            if (c >= seen) x[c] = 0xff800000u;  // -inf
+        }
+        float mx[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mx[c] = __uint_as_float(x[c]);
+#pragma unroll
+        for (int c = 4; c < kKeys; c += 4) {
+          mx[0] = fmaxf(mx[0], __uint_as_float(x[c]));
+          mx[1] = fmaxf(mx[1], __uint_as_float(x[c + 1]));
+          mx[2] = fmaxf(mx[2], __uint_as_float(x[c + 2]));
+          mx[3] = fmaxf(mx[3], __uint_as_float(x[c + 3]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+        if (t == t0) {
+          m = top;
+        } else if (__any_sync(0xffffffffu, top > m + kRaise)) {
+          // (this stream's product before is complete: it precedes this job's first in the tensor pipe)
+          const float up = top > m + kRaise ? top : m;
+          const float f = up == -INFINITY ? 1.f : ex2(m - up);
+          l *= f;
+          m = up;
+#pragma unroll
+          for (int c = 0; c < kD; c += 32) {
+            uint32_t o[32];
+            tmem_ld_x32(to + c, o);
+            tmem_wait_ld();
+            tmem_landed(o);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_st_x32(to + c, o);
+          }
+        }
+        const float nref = m == -INFINITY ? 0.f : -m;
+        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        uint32_t w[kKeys / 2];
+#pragma unroll
+        for (int c = 0; c < kKeys; c += 2) {
+          fma_pair(x[c], x[c + 1], scale2, nref, nref);
+          const float e0 = ex2(__uint_as_float(x[c])), e1 = ex2(__uint_as_float(x[c + 1]));
+          add_pair(sum[c & 7], sum[(c & 7) + 1], e0, e1);
+          w[c / 2] = pack_bf16x2(e0, e1);
+        }
+        l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+        tmem_st_x32(ts, w);
+        tmem_st_x32(ts + 32, w + 32);
+        tmem_wait_st();
+      }
+      if (nv < kKeys) {
+        // rows of V past the keys that are there may hold anything, and 0 * NaN is NaN
+        const uint32_t vl = 2 * (tile_n + t) + 1, st = vl % kStages;
+        if (!wait_warp(s, a, &s.full[st], (vl / kStages) & 1, 9u)) return;
+        if (row >= nv) {
+          uint4* v = reinterpret_cast<uint4*>(s.ring[st] + row * 128);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            v[c] = make_uint4(0u, 0u, 0u, 0u);
+            v[c + kHalf / 16] = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        fence_proxy_async_smem();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s.pready[stream]);
+    }
+    // the row's part
+    const bool any = t0 < it.ntiles;
+    if (any && !wait_warp(s, a, &s.ofull[stream], ends & 1, 10u)) return;
+    if (active) {
+      tc_fence_after();
+      const bool first = it.tile0 == 0;
+      const int token = it.tok0 + tok + row_k, hq = it.head * a.g + row - row_k * a.g;
+      const size_t at = first ? first_row(a, it.source, p, token, hq) : next_row(a, blockIdx.x, p, row);
+      float* dst = (first ? a.first_o : a.next_o) + at * kD;
+      const bool mine = row < rows;
+      if (mine) (first ? a.first_ml : a.next_ml)[at] = make_float2(m, l);
+      if (any) {
+#pragma unroll
+        for (int c = 0; c < kD; c += 32) {
+          uint32_t o[32];
+          tmem_ld_x32(to + c, o);
+          tmem_wait_ld();
+          tmem_landed(o);
+          if (mine) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) store8(dst + c + j, o + j);
+          }
+        }
+      }
+      tc_fence_before();
+    }
+    if (any) ++ends;
+    tile_n += it.ntiles;
+    n0 += it.ntiles * (two ? 2 : 1);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_tc_kernel(const __grid_constant__ Maps m, const __grid_constant__ AttendArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  Smem& s = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&s.full[i], 1);
+      mbar_init(&s.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s.qfull[i], 1);
+      mbar_init(&s.qempty[i], 1);
+      mbar_init(&s.sfull[i], 1);
+      mbar_init(&s.pready[i], 4);
+      mbar_init(&s.ofull[i], 1);
+    }
+    for (int i = 0; i < kItems; ++i) {
+      mbar_init(&s.ifull[i], 1);
+      mbar_init(&s.iempty[i], 10);  // the warps of the copies, the MMAs and the streams
+    }
+    mbar_init(&s.drained, 1);
+    s.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 3) {
+    tmem_alloc(&s.tmem, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s.tmem;
+  uint32_t load = 0, ql = 0;
+  // registers of the launch (3 x 168 a lane): 80 for the first warpgroup, 208 for a stream's
+  if (warp < 4) reg_dealloc<80>();
+  else reg_alloc<208>();
+  if (warp == 0) {
+    // (the injected stall: the first CTA's tiles never come)
+    if (!(a.stall != 0 && blockIdx.x == 0)) produce(s, a, m, lane, load, ql);
+  } else if (warp == 1) {
+    multiply(s, a, tmem, lane);
+  } else if (warp == 2) {
+    Walk w;
+    w.begin(a, blockIdx.x, lane);
+    for (uint32_t n = 0;; ++n) {
+      Item it;
+      it.ntiles = 0;
+      const bool more = w.next(a, it);
+      if (!more) it.ntiles = 0;
+      if (!wait_warp(s, a, &s.iempty[n % kItems], ((n / kItems) & 1) ^ 1, 11u)) break;
+      if (lane == 0) {
+        s.items[n % kItems] = it;
+        mbar_arrive(&s.ifull[n % kItems]);
+      }
+      __syncwarp();
+      if (!more) break;
+    }
+  } else if (warp >= 4) {
+    soften(s, a, tmem, (warp >> 2) - 1);
+  }
+  __syncwarp();
+  // every MMA has completed (a CTA that gave up: those that it had issued)
+  if (warp == 1) {
+    if (elect_one()) mma_commit(&s.drained);
+    __syncwarp();
+    drain_bar(&s.drained, 0u);
+  }
+  if (warp == 0) {
+    // ... and every copy has landed: the last of each buffer's, should no one have waited for it
+    for (uint32_t i = 0; i < kStages; ++i)
+      if (load > i) drain_bar(&s.full[i], ((load - 1 - i) / kStages) & 1);
+    for (uint32_t i = 0; i < 2; ++i)
+      if (ql > i) drain_bar(&s.qfull[i], ((ql - 1 - i) / 2) & 1);
+  }
+  __syncthreads();
+  if (warp == 3) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+std::atomic<bool> g_attr_set[64];
+
+// Rows [.., rows, outer ..] of 128 bf16, in boxes of 64 columns with the 128-byte swizzle.
+bool map_of(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const int64_t* strides,
+            const uint32_t* box) {
+  cuuint64_t d[5], st[4];
+  cuuint32_t b[5];
+  for (int i = 0; i < rank; ++i) {
+    d[i] = dims[i];
+    b[i] = box[i];
+    if (i > 0) st[i - 1] = (cuuint64_t)strides[i - 1] * 2;
+  }
+  return tensor_map_bf16(m, base, rank, d, st, b);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  Maps m;
+  {
+    const uint64_t dims[3] = {kD, (uint64_t)a.h_q, (uint64_t)a.tokens};
+    const int64_t strides[2] = {a.q_head, a.q_token};
+    const uint32_t box[3] = {64, (uint32_t)a.g, (uint32_t)a.tpt};
+    if (!map_of(&m.q, a.q, 3, dims, strides, box)) return cudaErrorInvalidValue;
+  }
+  m.pk = m.pv = m.ck = m.cv = m.q;  // those of a source that is not there are not used
+  if (a.prefix.rows > 0) {
+    const bool off = a.prefix.head_off != nullptr;
+    const uint64_t dims[3] = {kD, (uint64_t)a.prefix.rows, off ? 1 : (uint64_t)a.h_kv};
+    const int64_t strides[2] = {a.prefix.row_stride, off || a.h_kv == 1 ? a.prefix.row_stride : a.prefix.head_stride};
+    const uint32_t box[3] = {64, kKeys, 1};
+    if (!map_of(&m.pk, a.prefix.k, 3, dims, strides, box) || !map_of(&m.pv, a.prefix.v, 3, dims, strides, box))
+      return cudaErrorInvalidValue;
+  }
+  if (a.has_cache) {
+    const ecokv_pages& c = a.cache;
+    const uint64_t dims[4] = {kD, (uint64_t)c.page_size, (uint64_t)a.h_kv, (uint64_t)c.n_pages};
+    const int64_t strides[3] = {c.slot_stride, c.head_stride, c.page_stride};
+    const uint32_t box[4] = {64, (uint32_t)(c.page_size < kKeys ? c.page_size : kKeys), 1, 1};
+    if (!map_of(&m.ck, c.k, 4, dims, strides, box) || !map_of(&m.cv, c.v, 4, dims, strides, box))
+      return cudaErrorInvalidValue;
+  }
+  const int smem = (int)sizeof(Smem) + 1024;
+  if (!g_attr_set[dev].load()) {  // a racing thread repeats the idempotent setting
+    e = cudaFuncSetAttribute(attend_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    g_attr_set[dev].store(true);
+  }
+  attend_tc_kernel<<<a.P, kThreads, smem, st>>>(m, a);
+  return cudaGetLastError();
+}
+
+}  // namespace ecokv

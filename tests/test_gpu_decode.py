@@ -413,3 +413,18 @@ def test_a_decode_step_in_a_graph_on_another_stream():
                  for j, (ok, ov) in enumerate(b.own)]
         b.lens = [n + 1 for n in b.lens]
         assert torch.equal(check_attend(b, heads, pre, h_q, "bf16", q=q_out.cpu()), out)
+
+
+def test_attend_waits_that_run_out():
+    """The injected stall: a status, an untouched context, and the next call as ever."""
+    b = Batch(6, 4, [1] * 3, [40, 200, 300], 16, "bf16")
+    heads, pre = make_prefix(gen(2), [500] * 4, "bf16", False)
+    q = torch.randn(3, 28, D, generator=gen(1)).bfloat16().cuda()
+    ws = E.alloc_attend_workspace(3, 3, 28, 4, q.dtype)
+    good = E.attend(q, pre, b.cache, ws=ws)
+    E.attend(q, pre, b.cache, ws=ws, flags=E.ECOKV_FLAG_TEST_STALL, timeout_us=20000)
+    assert E.ecokv_device_status(ws) == E.ECOKV_ERR_TIMEOUT
+    assert torch.equal(E.attend(q, pre, b.cache, ws=ws), good) and E.ecokv_device_status(ws) == 0
+    with pytest.raises(E.EcokvError) as e:
+        E.attend(q, pre, b.cache, flags=E.ECOKV_FLAG_TEST_STALL | E.ECOKV_FLAG_FORCE_SIMT)
+    assert e.value.code == E.ECOKV_ERR_UNSUPPORTED
