@@ -387,32 +387,33 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = s.tmem;
   uint32_t load = 0, ql = 0;
-  // registers of the launch (3 x 168 a lane): 80 for the first warpgroup, 208 for a stream's
-  if (warp < 4) reg_dealloc<80>();
-  else reg_alloc<208>();
-  if (warp == 0) {
-    // (the injected stall: the first CTA's tiles never come)
-    if (!(a.stall != 0 && blockIdx.x == 0)) produce(s, a, m, lane, load, ql);
-  } else if (warp == 1) {
-    multiply(s, a, tmem, lane);
-  } else if (warp == 2) {
-    Walk w;
-    w.begin(a, blockIdx.x, lane);
-    for (uint32_t n = 0;; ++n) {
-      Item it;
-      it.ntiles = 0;
-      const bool more = w.next(a, it);
-      if (!more) it.ntiles = 0;
-      if (!wait_warp(s, a, &s.iempty[n % kItems], ((n / kItems) & 1) ^ 1, 11u)) break;
-      if (lane == 0) {
-        s.items[n % kItems] = it;
-        mbar_arrive(&s.ifull[n % kItems]);
-      }
-      __syncwarp();
-      if (!more) break;
-    }
-  } else if (warp >= 4) {
+  // registers of the launch (3 x 168 a lane): 64 for the first warpgroup, 216 for a stream's
+  if (warp >= 4) {
+    reg_alloc<216>();
     soften(s, a, tmem, (warp >> 2) - 1);
+  } else {
+    reg_dealloc<64>();
+    if (warp == 0) {
+      // (the injected stall: the first CTA's tiles never come)
+      if (!(a.stall != 0 && blockIdx.x == 0)) produce(s, a, m, lane, load, ql);
+    } else if (warp == 1) {
+      multiply(s, a, tmem, lane);
+    } else if (warp == 2) {
+      Walk w;
+      w.begin(a, blockIdx.x, lane);
+      for (uint32_t n = 0;; ++n) {
+        Item it;
+        const bool more = w.next(a, it);
+        if (!more) it.ntiles = 0;
+        if (!wait_warp(s, a, &s.iempty[n % kItems], ((n / kItems) & 1) ^ 1, 11u)) break;
+        if (lane == 0) {
+          s.items[n % kItems] = it;
+          mbar_arrive(&s.ifull[n % kItems]);
+        }
+        __syncwarp();
+        if (!more) break;
+      }
+    }
   }
   __syncwarp();
   // every MMA has completed (a CTA that gave up: those that it had issued)
