@@ -8,8 +8,9 @@
 // sequence's own slots.  Its keys are cut into tiles of 128.  All items' tiles in a
 // row (the prefix's by head and token group, then the own ones by head, sequence
 // and token group) are dealt to the CTAs in equal runs, wherever items begin and
-// end, so that no CTA has more tiles than another by more than one whatever the
-// lengths.  A CTA writes each of its items' unnormalised sum, maximum and sum of
+// end.  An item counts kItemUnits units more than its tiles, for its queries, the start
+// of its pipeline and its sums, so that a CTA with many short items has fewer
+// tiles: whatever the lengths, all CTAs take about as long.  A CTA writes each of its items' unnormalised sum, maximum and sum of
 // exponentials; a second kernel joins them row by row.  Partial sums are fp32.
 #pragma once
 
@@ -22,6 +23,10 @@ constexpr int kKeys = 128;        // keys a tile
 constexpr int kTileRows = 128;    // most rows a partial sum of a continued item has
 constexpr int kMaxGroup = 64;     // query heads a KV head
 constexpr int kMaxAttendSms = 256;
+#ifndef ITEM_UNITS
+#define ITEM_UNITS 2
+#endif
+constexpr int kItemUnits = ITEM_UNITS;
 
 struct AttendArgs {
   const void* q;
@@ -51,10 +56,10 @@ struct AttendArgs {
 
 // What the attention kernel leaves for the joining one.
 enum : int {
-  PLAN_RUN = 0,       // tiles a CTA
-  PLAN_PREFIX = 1,    // tiles of the prefix
-  PLAN_OWN = 2,       // tiles of one head's own slots over all sequences
-  PLAN_HEADS = 4      // [h_kv] first tile of each head's prefix, then [batch] first own tile of each sequence
+  PLAN_RUN = 0,       // units a CTA
+  PLAN_PREFIX = 1,    // units of the prefix
+  PLAN_OWN = 2,       // units of one head's own slots over all sequences
+  PLAN_HEADS = 4      // [h_kv] first unit of each head's prefix, then [batch] first own unit of each sequence
 };
 
 struct Item {
@@ -91,13 +96,15 @@ __device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b, bool report)
   if (report && (s.L != len || s.start != s0 || s.start + s.T != s1)) note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)b);
   return s;
 }
-// Keys that the tokens of group `rg` of a sequence see at most, and the tiles of them.
+// Units of an item of so many tiles: none without a tile, else kItemUnits before its first tile's.
+__host__ __device__ inline int item_units(int tiles) { return tiles > 0 ? tiles + kItemUnits : 0; }
+// Keys that the tokens of group `rg` of a sequence see at most, and the units of the groups before.
 __device__ __forceinline__ int seq_vis(const AttendArgs& a, const Seq& s, int rg) {
   return max(s.L - s.T + min(s.T, (rg + 1) * a.span), 0);
 }
-__device__ __forceinline__ int seq_tiles(const AttendArgs& a, const Seq& s, int groups) {
+__device__ __forceinline__ int seq_units(const AttendArgs& a, const Seq& s, int groups) {
   int n = 0;
-  for (int rg = 0; rg < groups; ++rg) n += div_up(seq_vis(a, s, rg), kKeys);
+  for (int rg = 0; rg < groups; ++rg) n += item_units(div_up(seq_vis(a, s, rg), kKeys));
   return n;
 }
 // Rows of head h's prefix.
@@ -111,17 +118,17 @@ __device__ __forceinline__ int prefix_rows(const AttendArgs& a, int h, int& row0
   return n;
 }
 
-// A warp's walk over its CTA's run of tiles, item by item.  Every lane holds the
+// A warp's walk over its CTA's run of units, item by item.  Every lane holds the
 // same state but for the 32 sequences (or heads) at hand, one a lane.
 struct Walk {
-  int x, end;               // tiles of all items: next, one past the CTA's last
-  int prefix_total, own;    // tiles of the prefix; of one head's own slots
+  int x, end;               // units of all items: next, one past the CTA's last
+  int prefix_total, own;    // units of the prefix; of one head's own slots
   int groups;               // token groups of the prefix
   int lane;
-  // the 32 sequences from b0 on: first tile of the first of them within a head
+  // the 32 sequences from b0 on: first unit of the first of them within a head
   int b0, base, head;
   Seq s;
-  int w, upto;              // this lane's tiles, and those of lanes up to it
+  int w, upto;              // this lane's units, and those of lanes up to it
 
   static __device__ __forceinline__ int scan(int v, int lane) {
 #pragma unroll
@@ -139,7 +146,7 @@ struct Walk {
     w = 0;
     if (b < a.batch) {
       s = load_seq(a, b, report);
-      w = seq_tiles(a, s, div_up(s.T, a.span));
+      w = seq_units(a, s, div_up(s.T, a.span));
     }
     upto = scan(w, lane);
   }
@@ -152,14 +159,14 @@ struct Walk {
     prefix_total = 0;
     if (a.prefix.rows > 0) {
       if (a.prefix.head_off == nullptr) {
-        const int per = groups * div_up(a.prefix.rows, kKeys);
+        const int per = groups * item_units(div_up(a.prefix.rows, kKeys));
         prefix_total = a.h_kv * per;
         if (lead)
           for (int h = lane; h < a.h_kv; h += 32) a.plan[PLAN_HEADS + h] = h * per;
       } else {
         for (int h0 = 0; h0 < a.h_kv; h0 += 32) {
           int row0, n = 0;
-          if (h0 + lane < a.h_kv) n = groups * div_up(prefix_rows(a, h0 + lane, row0, lead), kKeys);
+          if (h0 + lane < a.h_kv) n = groups * item_units(div_up(prefix_rows(a, h0 + lane, row0, lead), kKeys));
           const int up = scan(n, lane);
           if (lead && h0 + lane < a.h_kv) a.plan[PLAN_HEADS + h0 + lane] = prefix_total + up - n;
           prefix_total += __shfl_sync(0xffffffffu, up, 31);
@@ -185,7 +192,7 @@ struct Walk {
     base = 0;
     head = 0;
     const int total = prefix_total + a.h_kv * own;
-    const int run = max(div_up(total, a.P), 1);
+    const int run = max(div_up(total, a.P), kItemUnits + 1);  // (no CTA without a tile before the last)
     if (lead && lane == 0) {
       a.plan[PLAN_RUN] = run;
       a.plan[PLAN_PREFIX] = prefix_total;
@@ -197,11 +204,19 @@ struct Walk {
 
   // The next item (the same in every lane); false: none left.
   __device__ __forceinline__ bool next(const AttendArgs& a, Item& it) {
-    if (x >= end) return false;
+    while (x < end) {
+      if (!at(a, it)) return false;
+      if (it.ntiles > 0) return true;
+    }
+    return false;
+  }
+  // The part of an item from unit x on, which may be less than its first tile (ntiles <= 0).
+  __device__ __forceinline__ bool at(const AttendArgs& a, Item& it) {
+    int skip;  // units before the first tile
     if (x < prefix_total) {
       int h, y, nt, row0;
       if (a.prefix.head_off == nullptr) {
-        nt = div_up(a.prefix.rows, kKeys);
+        nt = item_units(div_up(a.prefix.rows, kKeys));
         h = x / (groups * nt);
         y = x - h * groups * nt;
         row0 = 0;
@@ -214,7 +229,7 @@ struct Walk {
           int n = 0, r0 = 0, rows = 0;
           if (h0 + lane < a.h_kv) {
             rows = prefix_rows(a, h0 + lane, r0, false);
-            n = groups * div_up(rows, kKeys);
+            n = groups * item_units(div_up(rows, kKeys));
           }
           const int up = scan(n, lane), all = __shfl_sync(0xffffffffu, up, 31);
           if (x < at + all) {
@@ -227,7 +242,7 @@ struct Walk {
           }
           at += all;
         }
-        nt = div_up(it.vis, kKeys);
+        nt = item_units(div_up(it.vis, kKeys));
       }
       const int rg = y / nt;
       it.source = 0;
@@ -237,8 +252,10 @@ struct Walk {
       it.ntok = min(a.span, a.tokens - it.tok0);
       it.lim0 = it.vis;
       it.slope = 0;
-      it.tile0 = y - rg * nt;
-      it.ntiles = min(nt - it.tile0, end - x);
+      y -= rg * nt;
+      skip = max(kItemUnits - y, 0);
+      it.tile0 = max(y - kItemUnits, 0);
+      it.ntiles = min(nt - y, end - x) - skip;
       it.row0 = row0;
     } else {
       int y = x - prefix_total;
@@ -262,7 +279,7 @@ struct Walk {
       q.T = __shfl_sync(0xffffffffu, s.T, l);
       q.L = __shfl_sync(0xffffffffu, s.L, l);
       int rg = 0, nt;
-      while (y >= (nt = div_up(seq_vis(a, q, rg), kKeys))) {
+      while (y >= (nt = item_units(div_up(seq_vis(a, q, rg), kKeys)))) {
         y -= nt;
         if (++rg * a.span >= q.T) return false;
       }
@@ -274,11 +291,12 @@ struct Walk {
       it.lim0 = q.L - q.T + rg * a.span + 1;
       it.slope = 1;
       it.vis = seq_vis(a, q, rg);
-      it.tile0 = y;
-      it.ntiles = min(nt - y, end - x);
+      skip = max(kItemUnits - y, 0);
+      it.tile0 = max(y - kItemUnits, 0);
+      it.ntiles = min(nt - y, end - x) - skip;
       it.row0 = 0;
     }
-    x += it.ntiles;
+    x += skip + it.ntiles;
     return true;
   }
 };

@@ -34,12 +34,13 @@ struct Parts {
   int row;        // row within a continued item
 };
 
-__device__ __forceinline__ Parts find_parts(const AttendArgs& a, int source, int tile, int nt, int run, int k, int ntok,
+// (unit: the item's first; nt: its tiles)
+__device__ __forceinline__ Parts find_parts(const AttendArgs& a, int source, int unit, int nt, int run, int k, int ntok,
                                             int token, int hq) {
   Parts p{0, 0, 1, 0, 0, 0};
   if (nt <= 0) return p;
-  p.c0 = tile / run;
-  const int ctas = (tile + nt - 1) / run - p.c0 + 1;
+  p.c0 = (unit + kItemUnits) / run;
+  const int ctas = (unit + kItemUnits + nt - 1) / run - p.c0 + 1;
   if (ntok > a.tpt) p.j0 = k / a.tpt;  // two row tiles: the row is in one of them
   else p.nj = a.parts;
   p.n = ctas * p.nj;
@@ -62,6 +63,8 @@ __device__ __forceinline__ const float* part(const AttendArgs& a, const Parts& p
 
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __grid_constant__ AttendArgs a) {
+  // (scheduled behind the attention kernel, whose end it waits for)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31;
   const long long id = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
   if (id >= (long long)a.tokens * a.h_q) return;
@@ -71,7 +74,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __gr
   if (a.prefix.rows > 0) {
     int row0;
     const int nt = div_up(prefix_rows(a, h, row0, false), kKeys), rg = token / a.span;
-    src[0] = find_parts(a, 0, a.plan[PLAN_HEADS + h] + rg * nt, nt, run, token - rg * a.span,
+    src[0] = find_parts(a, 0, a.plan[PLAN_HEADS + h] + rg * item_units(nt), nt, run, token - rg * a.span,
                         min(a.span, a.tokens - rg * a.span), token, hq);
   }
   if (a.has_cache && own > 0) {
@@ -86,7 +89,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __gr
     if (i >= 0 && i < s.T) {
       const int rg = i / a.span;
       src[1] = find_parts(a, 1,
-                          prefix_total + h * own + a.plan[PLAN_HEADS + a.h_kv + b] + seq_tiles(a, s, rg),
+                          prefix_total + h * own + a.plan[PLAN_HEADS + a.h_kv + b] + seq_units(a, s, rg),
                           div_up(seq_vis(a, s, rg), kKeys), run, i - rg * a.span, min(a.span, s.T - rg * a.span),
                           token, hq);
     }
@@ -179,8 +182,16 @@ int attend_sms() {
 template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
-  attend_join_kernel<T><<<(unsigned)((rows + kJoinWarps - 1) / kJoinWarps), 32 * kJoinWarps, 0, st>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((rows + kJoinWarps - 1) / kJoinWarps));
+  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attend_join_kernel<T>, a);
 }
 
 }  // namespace
@@ -273,9 +284,9 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   const double scale = p->scale > 0.f ? (double)p->scale : 1.0 / sqrt((double)kD);
   a.scale_log2 = (float)(1.4426950408889634 * scale);
   a.timeout_ns = (p->timeout_us ? (unsigned long long)p->timeout_us : 2000000ull) * 1000ull;
-  // tiles of every item, counted in 32 bits by the kernels
-  const long long groups = (a.tokens + a.span - 1) / a.span, cap_tiles = (a.cap + kKeys - 1) / kKeys;
-  const long long tiles = a.h_kv * (groups * ((a.prefix.rows + kKeys - 1) / kKeys) + (groups + a.batch) * cap_tiles);
+  // units of every item, counted in 32 bits by the kernels
+  const long long groups = (a.tokens + a.span - 1) / a.span, cap_tiles = item_units((a.cap + kKeys - 1) / kKeys);
+  const long long tiles = a.h_kv * (groups * item_units((a.prefix.rows + kKeys - 1) / kKeys) + (groups + a.batch) * cap_tiles);
   if (tiles > 0x7fffffff || groups * cap_tiles > (1 << 25)) return ECOKV_ERR_UNSUPPORTED;
   char* w = static_cast<char*>(ws);
   const AttendLayout L = attend_layout(a.tokens, a.batch, a.h_q, a.h_kv, a.parts);

@@ -12,8 +12,8 @@
 // exceeds it by 2^8: the weights are fp32 before they are rounded, so that any
 // reference within their range is as exact.
 //
-// Warps: 0 copies (TMA; a lane a page), 1 MMAs, 2 the walk over the items, 3 tensor
-// memory, 4-7 and 8-11 the streams.
+// Warps: 0 copies (TMA; a lane a page), 1 and 3 the streams' products, 2 the walk over
+// the items, 4-7 and 8-11 the streams' softmax.
 
 #include <atomic>
 
@@ -52,15 +52,17 @@ struct Maps {
   CUtensorMap q, pk, pv, ck, cv;
 };
 
-// Bounded wait: false once this CTA has given up.
+// Bounded wait: false once this CTA has given up.  (The clock is read every 16th
+// try: reading it takes longer than a try.)
 __device__ __forceinline__ bool wait_bar(Smem& s, const AttendArgs& a, uint64_t* bar, uint32_t parity, unsigned where) {
+  unsigned long long t0 = 0;
 #pragma unroll 1
-  for (int i = 0; i < 4; ++i)
-    if (mbar_try_wait(bar, parity)) return true;
-  const unsigned long long t0 = now_ns();
-  while (!mbar_try_wait(bar, parity)) {
+  for (uint32_t i = 1; !mbar_try_wait(bar, parity); ++i) {
+    if ((i & 15u) != 0) continue;
     if (s.abort) return false;
-    if (now_ns() - t0 > a.timeout_ns) {
+    const unsigned long long t = now_ns();
+    if (t0 == 0) t0 = t;
+    if (t - t0 > a.timeout_ns) {
       s.abort = 1;
       note(a, ECOKV_ERR_TIMEOUT, where);
       return false;
@@ -157,72 +159,65 @@ __device__ __forceinline__ void produce(Smem& s, const AttendArgs& a, const Maps
   }
 }
 
-// A job whose weights are awaited for the second product.
-struct Job {
-  bool any, first, last_v, last;  // first, last: of its stream in the item; last_v: last to read its tile of V
-  uint32_t stream, k, load;       // k: jobs of the stream before it
-};
-
-__device__ __forceinline__ bool second_product(Smem& s, const AttendArgs& a, const Job& j, uint32_t tmem) {
-  constexpr uint32_t idesc = idesc_bf16(128, 128, false, true);
-  const uint32_t st = j.load % kStages;
-  if (!wait_warp(s, a, &s.full[st], (j.load / kStages) & 1, 4u)) return false;
-  if (!wait_warp(s, a, &s.pready[j.stream], j.k & 1, 5u)) return false;
-  tc_fence_after();
-  if (elect_one()) {
-    const uint32_t p = tmem + j.stream * 256u, o = p + 128u;
-    const uint64_t vd = smem_desc(smem_u32(s.ring[st]), kHalf, 1024, 2);
-#pragma unroll
-    for (int k8 = 0; k8 < 8; ++k8)  // 16 keys a step
-      mma_bf16_ta(o, p + k8 * 8u, vd + (uint64_t)(k8 * 128), idesc, k8 > 0 || !j.first ? 1u : 0u);
-    if (j.last_v) mma_commit(&s.empty[st]);
-    if (j.last) mma_commit(&s.ofull[j.stream]);
-  }
-  __syncwarp();
-  return true;
-}
-
-__device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t tmem, int lane) {
-  constexpr uint32_t idesc = idesc_bf16(128, 128, false, false);
-  ItemReader items;
-  Item it;
-  Job prev{};
-  uint32_t n = 0, load = 0, ql = 0;  // jobs, tiles of K and V, tiles of Q so far
-  while (items.next(s, a, it, lane)) {
-    const int nq = it.ntok > a.tpt ? 2 : 1;
-    for (int t = 0; t < it.ntiles; ++t, load += 2) {
-      const uint32_t st = load % kStages;
-      for (int r = 0; r < nq; ++r, ++n) {
-        const uint32_t q = ql + r, i = n & 1;
-        if (t == 0 && !wait_warp(s, a, &s.qfull[q & 1], (q >> 1) & 1, 6u)) return;
-        if (r == 0 && !wait_warp(s, a, &s.full[st], (load / kStages) & 1, 7u)) return;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t qd = smem_desc(smem_u32(s.q[q & 1]), 16, 1024, 2);
-          const uint64_t kd = smem_desc(smem_u32(s.ring[st]), 16, 1024, 2);
-#pragma unroll
-          for (int k8 = 0; k8 < 8; ++k8) {
-            const uint64_t d = (uint64_t)((k8 >> 2) * (kHalf >> 4) + (k8 & 3) * 2);
-            mma_bf16(tmem + i * 256u, qd + d, kd + d, idesc, k8 > 0 ? 1u : 0u);
-          }
-          mma_commit(&s.sfull[i]);
-          if (r == nq - 1) mma_commit(&s.empty[st]);
-          if (t == it.ntiles - 1) mma_commit(&s.qempty[q & 1]);
-        }
-        __syncwarp();
-        if (prev.any && !second_product(s, a, prev, tmem)) return;
-        prev.any = true;
-        prev.first = nq == 2 ? t == 0 : t < 2;
-        prev.last = nq == 2 ? t == it.ntiles - 1 : t >= it.ntiles - 2;
-        prev.last_v = r == nq - 1;
-        prev.stream = i;
-        prev.k = n >> 1;
-        prev.load = load + 1;
+// The products of one stream, by one thread: the first of a job, then, when its
+// weights are there, the second, while the other stream's thread keeps the tensor pipe
+// busy.  (One thread for both streams took 2500 cycles a job: every wait stood
+// between products that had nothing to do with it.)
+__device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t tmem, uint32_t stream) {
+  constexpr uint32_t idesc1 = idesc_bf16(128, 128, false, false), idesc2 = idesc_bf16(128, 128, false, true);
+  const uint32_t ts = tmem + stream * 256u, to = ts + 128u;  // scores, later the weights; the sum
+  uint32_t n0 = 0, load = 0, ql = 0, k = 0;  // jobs before the item, tiles of K and V, of Q; this stream's jobs
+  for (uint32_t e = 0;; ++e) {
+    if (!wait_bar(s, a, &s.ifull[e % kItems], (e / kItems) & 1, 1u)) return;
+    const int ntiles = s.items[e % kItems].ntiles;
+    const bool two = s.items[e % kItems].ntok > a.tpt;
+    mbar_arrive(&s.iempty[e % kItems]);
+    if (ntiles <= 0) return;
+    const uint32_t p = (stream ^ n0) & 1, q = ql + (two ? p : 0);  // its row tile, or its key tiles in turn
+    if (!wait_bar(s, a, &s.qfull[q & 1], (q >> 1) & 1, 6u)) return;
+    const uint64_t qd = smem_desc(smem_u32(s.q[q & 1]), 16, 1024, 2);
+    bool first = true;
+    for (int t = 0; t < ntiles; ++t, load += 2) {
+      const uint32_t sk = load % kStages, sv = (load + 1) % kStages;
+      if (!wait_bar(s, a, &s.full[sk], (load / kStages) & 1, 7u)) return;
+      if (!two && ((uint32_t)t & 1) != p) {  // the other stream's
+        mbar_arrive(&s.empty[sk]);
+        if (!wait_bar(s, a, &s.full[sv], ((load + 1) / kStages) & 1, 4u)) return;
+        mbar_arrive(&s.empty[sv]);
+        continue;
       }
+      tc_fence_after();
+      const uint64_t kd = smem_desc(smem_u32(s.ring[sk]), 16, 1024, 2);
+#pragma unroll
+      for (int k8 = 0; k8 < 8; ++k8) {
+        const uint64_t d = (uint64_t)((k8 >> 2) * (kHalf >> 4) + (k8 & 3) * 2);
+        mma_bf16(ts, qd + d, kd + d, idesc1, k8 > 0 ? 1u : 0u);
+      }
+      mma_commit(&s.sfull[stream]);
+      mma_commit(&s.empty[sk]);
+      if (!wait_bar(s, a, &s.full[sv], ((load + 1) / kStages) & 1, 4u)) return;
+      if (!wait_bar(s, a, &s.pready[stream], k & 1, 5u)) return;
+      tc_fence_after();
+      const uint64_t vd = smem_desc(smem_u32(s.ring[sv]), kHalf, 1024, 2);
+#pragma unroll
+      for (int k8 = 0; k8 < 8; ++k8)  // 16 keys a step
+        mma_bf16_ta(to, ts + k8 * 8u, vd + (uint64_t)(k8 * 128), idesc2, k8 > 0 || !first ? 1u : 0u);
+      mma_commit(&s.empty[sv]);
+      first = false;
+      ++k;
     }
-    ql += nq;
+    if (!first) mma_commit(&s.ofull[stream]);
+    // both streams release every tile of Q, whether they use it or not
+    if (first) mbar_arrive(&s.qempty[q & 1]);
+    else mma_commit(&s.qempty[q & 1]);
+    if (two) {
+      const uint32_t o = ql + (p ^ 1);
+      if (!wait_bar(s, a, &s.qfull[o & 1], (o >> 1) & 1, 6u)) return;
+      mbar_arrive(&s.qempty[o & 1]);
+    }
+    n0 += (uint32_t)ntiles * (two ? 2u : 1u);
+    ql += two ? 2u : 1u;
   }
-  if (prev.any) second_product(s, a, prev, tmem);
 }
 
 __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tmem, int stream) {
@@ -361,20 +356,20 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&s.full[i], 1);
-      mbar_init(&s.empty[i], 1);
+      mbar_init(&s.empty[i], 2);  // both streams, whether they use the tile or not
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.qfull[i], 1);
-      mbar_init(&s.qempty[i], 1);
+      mbar_init(&s.qempty[i], 2);
       mbar_init(&s.sfull[i], 1);
       mbar_init(&s.pready[i], 4);
       mbar_init(&s.ofull[i], 1);
     }
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&s.ifull[i], 1);
-      mbar_init(&s.iempty[i], 10);  // the warps of the copies, the MMAs and the streams
+      mbar_init(&s.iempty[i], 11);  // the warps of the copies, the MMAs and the streams
     }
-    mbar_init(&s.drained, 1);
+    mbar_init(&s.drained, 2);
     s.abort = 0;
     fence_mbar_init();
   }
@@ -385,6 +380,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // (the joining kernel is scheduled behind this grid and waits for its end)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = s.tmem;
   uint32_t load = 0, ql = 0;
   // registers of the launch (3 x 168 a lane): 64 for the first warpgroup, 216 for a stream's
@@ -396,8 +393,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0) {
       // (the injected stall: the first CTA's tiles never come)
       if (!(a.stall != 0 && blockIdx.x == 0)) produce(s, a, m, lane, load, ql);
-    } else if (warp == 1) {
-      multiply(s, a, tmem, lane);
+    } else if (warp == 1 || warp == 3) {
+      if (lane == 0) {
+        multiply(s, a, tmem, (uint32_t)warp >> 1);
+        mma_commit(&s.drained);
+      }
+      __syncwarp();
     } else if (warp == 2) {
       Walk w;
       w.begin(a, blockIdx.x, lane);
@@ -417,11 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   __syncwarp();
   // every MMA has completed (a CTA that gave up: those that it had issued)
-  if (warp == 1) {
-    if (elect_one()) mma_commit(&s.drained);
-    __syncwarp();
-    drain_bar(&s.drained, 0u);
-  }
+  if (warp == 1 || warp == 3) drain_bar(&s.drained, 0u);
   if (warp == 0) {
     // ... and every copy has landed: the last of each buffer's, should no one have waited for it
     for (uint32_t i = 0; i < kStages; ++i)

@@ -469,16 +469,14 @@ def rotary(rot_dim=HEAD_DIM, base=10000.0, layout="half", scaling="none", factor
     return r
 
 
-def _dtype(*tensors) -> int:
+def _dtype(t, *others) -> int:
     """Their common dtype's code; all of them on one CUDA device."""
-    t = tensors[0]
-    code = dtype_code(t)
-    for x in tensors:
-        if x is not None:
-            if not x.is_cuda:
-                raise ValueError("CUDA tensors are wanted")
-            if x.dtype != t.dtype or x.device != t.device:
-                raise TypeError(f"{x.dtype} on {x.device} next to {t.dtype} on {t.device}")
+    code, dt, dev = dtype_code(t), t.dtype, t.get_device()
+    if dev < 0:
+        raise ValueError("CUDA tensors are wanted")
+    for x in others:
+        if x is not None and (x.dtype is not dt or x.get_device() != dev):
+            raise TypeError(f"{x.dtype} on {x.device} next to {dt} on {t.device}")
     return code
 
 
@@ -486,7 +484,7 @@ def _ints(x, shape, what):
     import torch
     if x is None:
         return None
-    if x.dtype != torch.int32 or not x.is_cuda or not x.is_contiguous() or (shape and tuple(x.shape) != shape):
+    if x.dtype is not torch.int32 or not x.is_cuda or not x.is_contiguous() or (shape and x.shape != shape):
         raise ValueError(f"{what}: a contiguous int32 CUDA tensor{f' of shape {shape}' if shape else ''} is wanted")
     return x.data_ptr()
 
@@ -497,33 +495,35 @@ def _strides(x):
 
 
 def _heads(x, what):
-    """Rows [tokens, heads, d]: their strides."""
-    s = _strides(x)
-    if x.dim() != 3 or x.shape[2] != HEAD_DIM or s[2] != 1:
+    """Rows [tokens, heads, d]: (tokens, heads, their two strides)."""
+    n, s = x.shape, x.stride()
+    if len(n) != 3 or n[2] != HEAD_DIM or s[2] != 1:
         raise ValueError(f"{what}: rows [tokens, heads, {HEAD_DIM}] with the last axis contiguous are wanted")
-    return s
+    # (a stride that is never taken counts as a row)
+    return n[0], n[1], s[0] if n[0] > 1 else HEAD_DIM, s[1] if n[1] > 1 else HEAD_DIM
 
 
 def _rows(x, y, norm, what):
-    sx = _heads(x, what)
-    r = ecokv_rows(x.data_ptr(), None, sx[0], sx[1], 0, 0, None, x.shape[1])
+    tokens, heads, st, sh = _heads(x, what)
+    at = yt = yh = w = None
     if y is not None:
-        sy = _heads(y, what)
-        if y.shape != x.shape:
+        ty, hy, yt, yh = _heads(y, what)
+        if ty != tokens or hy != heads:
             raise ValueError(f"{what}: the output has another shape")
-        r.y, r.y_token, r.y_head = y.data_ptr(), sy[0], sy[1]
+        at = y.data_ptr()
     if norm is not None:
         if norm.shape != (HEAD_DIM,) or norm.stride(0) != 1:
             raise ValueError(f"{what}: norm weights [{HEAD_DIM}] are wanted")
-        r.norm = norm.data_ptr()
-    return r
+        w = norm.data_ptr()
+    return ecokv_rows(x.data_ptr(), at, st, sh, yt or 0, yh or 0, w, heads)
 
 
 def _on(stream, t, *made):
     """The raw stream to launch on; tensors made here are kept from reuse until it is done with them."""
-    import torch
     if stream is None:
-        return torch.cuda.current_stream(t.device).cuda_stream
+        import torch
+        # (torch.cuda.current_stream builds an object: 2 us of a call of 8)
+        return torch._C._cuda_getCurrentRawStream(t.get_device())
     if isinstance(stream, int):
         return stream
     for x in made:
@@ -562,7 +562,8 @@ def _positions(rot, positions, tokens):
         return None
     if positions is None:
         raise ValueError("positions are wanted")
-    if positions.numel() != rot.axes * tokens or positions.shape[-1] != tokens:
+    n = positions.shape
+    if n != (rot.axes, tokens) and not (n == (tokens,) and rot.axes == 1):
         raise ValueError(f"positions: [{rot.axes}, {tokens}] is wanted")
     return _ints(positions, None, "positions")
 
@@ -649,10 +650,10 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
     if prefix is None and cache is None:
         raise ValueError("a prefix or a cache is wanted")
     dt = _dtype(q, out, None if prefix is None else prefix.k, None if cache is None else cache.k_pages)
-    sq, so = _heads(q, "q"), _heads(out, "out")
-    tokens, h_q = q.shape[0], q.shape[1]
+    tokens, h_q, qt, qh = _heads(q, "q")
+    to, ho, ot, oh = _heads(out, "out")
     h_kv = prefix.h_kv if cache is None else cache.h_kv
-    if out.shape != q.shape or (prefix is not None and prefix.h_kv != h_kv):
+    if to != tokens or ho != h_q or (prefix is not None and prefix.h_kv != h_kv):
         raise ValueError("out or the prefix does not fit")
     batch = 1 if cache is None else cache.batch
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (tokens, h_q) or
@@ -661,7 +662,7 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
     if ws is None:
         ws = alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device)
         made.append(ws)
-    p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, sq[0], sq[1], so[0], so[1], flags, timeout_us)
+    p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, qt, qh, ot, oh, flags, timeout_us)
     _check(lib().ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
                               None if cache is None else cache.c,
                               None if cache is None else _ints(starts, (batch + 1,), "starts"), out.data_ptr(),
