@@ -9,9 +9,11 @@
 namespace ecokv {
 namespace {
 
-// One warp a row (token, query head): the row's partial sums, wherever the CTAs
-// left them, weighted by 2^(their maximum - the largest).  Lanes find the weights of
-// 32 of them at a time, then each lane sums four columns.
+// kWarps warps a row (token, query head), kJoinWarps / kWarps rows a CTA: the row's
+// partial sums, wherever the CTAs left them, weighted by 2^(their maximum - the
+// largest).  Every warp finds the weights, 32 at a time, and sums those of its
+// share; each lane has four columns.  What bounds it is the latency of its chain of
+// loads, so a row with many parts has them read by four warps at once.
 constexpr int kJoinWarps = 4;
 
 template <typename T>
@@ -61,13 +63,12 @@ __device__ __forceinline__ const float* part(const AttendArgs& a, const Parts& p
   return a.next_o + at * kD;
 }
 
-template <typename T>
+template <typename T, int kWarps>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __grid_constant__ AttendArgs a) {
-  // (scheduled behind the attention kernel, whose end it waits for)
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int lane = threadIdx.x & 31;
-  const long long id = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
-  if (id >= (long long)a.tokens * a.h_q) return;
+  __shared__ float4 part_acc[kJoinWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp % kWarps;
+  const long long id = (long long)blockIdx.x * (kJoinWarps / kWarps) + warp / kWarps;
+  if (id >= (long long)a.tokens * a.h_q) return;  // (with kWarps = kJoinWarps the whole CTA)
   const int token = (int)(id / a.h_q), hq = (int)(id - (long long)token * a.h_q), h = hq / a.g;
   Parts src[2] = {{0, 0, 1, 0, 0, 0}, {0, 0, 1, 0, 0, 0}};
   const int run = a.plan[PLAN_RUN], prefix_total = a.plan[PLAN_PREFIX], own = a.plan[PLAN_OWN];
@@ -77,60 +78,77 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __gr
     src[0] = find_parts(a, 0, a.plan[PLAN_HEADS + h] + rg * item_units(nt), nt, run, token - rg * a.span,
                         min(a.span, a.tokens - rg * a.span), token, hq);
   }
-  if (a.has_cache && own > 0) {
+  if (a.has_cache) {
     int b = token;
     if (a.starts != nullptr) {
       b = 0;
       for (int j = lane; j < a.batch; j += 32) b += a.starts[1 + j] <= token ? 1 : 0;
       b = min((int)__reduce_add_sync(0xffffffffu, (unsigned)b), a.batch - 1);
     }
+    const int first = a.plan[PLAN_HEADS + a.h_kv + b];
     const Seq s = load_seq(a, b, false);
     const int i = token - s.start;
-    if (i >= 0 && i < s.T) {
+    if (i >= 0 && i < s.T && own > 0) {
       const int rg = i / a.span;
-      src[1] = find_parts(a, 1,
-                          prefix_total + h * own + a.plan[PLAN_HEADS + a.h_kv + b] + seq_units(a, s, rg),
+      src[1] = find_parts(a, 1, prefix_total + h * own + first + seq_units(a, s, rg),
                           div_up(seq_vis(a, s, rg), kKeys), run, i - rg * a.span, min(a.span, s.T - rg * a.span),
                           token, hq);
     }
   }
-  float M = -INFINITY;
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-    for (int e = lane; e < src[x].n; e += 32) {
-      float2 ml;
-      part(a, src[x], e, ml);
-      M = fmaxf(M, ml.x);
+  // the parts of both sources in one row: entry e < src[0].n is the prefix's
+  const int n = src[0].n + src[1].n;
+  float M = -INFINITY, M0 = -INFINITY, l0 = 0.f;
+  const float* o0 = nullptr;
+  for (int e = lane; e < n; e += 32) {
+    float2 ml;
+    const float* o = e < src[0].n ? part(a, src[0], e, ml) : part(a, src[1], e - src[0].n, ml);
+    if (e == lane) {
+      o0 = o;
+      M0 = ml.x;
+      l0 = ml.y;
     }
+    M = fmaxf(M, ml.x);
+  }
   M = ptx::redux_max(M);
   const float ref = M == -INFINITY ? 0.f : M;
   float L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-    for (int e0 = 0; e0 < src[x].n; e0 += 32) {
-      float w = 0.f;
-      const float* o = nullptr;
-      if (e0 + lane < src[x].n) {
-        float2 ml;
-        o = part(a, src[x], e0 + lane, ml);
-        w = ptx::ex2(ml.x - ref);
-        L = fmaf(w, ml.y, L);
-      }
-      const int n = min(32, src[x].n - e0);
-#pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const float wk = __shfl_sync(0xffffffffu, w, k);
-        const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, k));
-        if (wk > 0.f) {  // (a part that saw no key is not written)
-          const float4 v = *reinterpret_cast<const float4*>(ok + 4 * lane);
-          acc.x = fmaf(wk, v.x, acc.x);
-          acc.y = fmaf(wk, v.y, acc.y);
-          acc.z = fmaf(wk, v.z, acc.z);
-          acc.w = fmaf(wk, v.w, acc.w);
-        }
-      }
+  for (int e0 = 0; e0 < n; e0 += 32) {
+    if (e0 > 0 && e0 + lane < n) {
+      float2 ml;
+      const int e = e0 + lane;
+      o0 = e < src[0].n ? part(a, src[0], e, ml) : part(a, src[1], e - src[0].n, ml);
+      M0 = ml.x;
+      l0 = ml.y;
     }
+    const float w = e0 + lane < n ? ptx::ex2(M0 - ref) : 0.f;
+    L = fmaf(w, w > 0.f ? l0 : 0.f, L);
+    const int k1 = min(32, n - e0);
+#pragma unroll 8
+    for (int k = mine; k < k1; k += kWarps) {
+      const float wk = __shfl_sync(0xffffffffu, w, k);
+      const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o0, k));
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (wk > 0.f) v = *reinterpret_cast<const float4*>(ok + 4 * lane);  // (a part that saw no key is not written)
+      acc.x = fmaf(wk, v.x, acc.x);
+      acc.y = fmaf(wk, v.y, acc.y);
+      acc.z = fmaf(wk, v.z, acc.z);
+      acc.w = fmaf(wk, v.w, acc.w);
+    }
+  }
+  if constexpr (kWarps > 1) {
+    part_acc[warp][lane] = acc;
+    __syncthreads();
+    if (mine != 0) return;
+#pragma unroll
+    for (int k = 1; k < kWarps; ++k) {
+      const float4 v = part_acc[warp + k][lane];
+      acc.x += v.x;
+      acc.y += v.y;
+      acc.z += v.z;
+      acc.w += v.w;
+    }
+  }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
   const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -182,16 +200,12 @@ int attend_sms() {
 template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)((rows + kJoinWarps - 1) / kJoinWarps));
-  cfg.blockDim = dim3(32 * kJoinWarps);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attend_join_kernel<T>, a);
+  // four warps a row while the rows are few (and so have many parts each)
+  const bool wide = rows <= 2048;
+  const unsigned grid = (unsigned)(wide ? rows : (rows + kJoinWarps - 1) / kJoinWarps);
+  if (wide) attend_join_kernel<T, kJoinWarps><<<grid, 32 * kJoinWarps, 0, st>>>(a);
+  else attend_join_kernel<T, 1><<<grid, 32 * kJoinWarps, 0, st>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace

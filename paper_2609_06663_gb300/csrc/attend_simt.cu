@@ -186,8 +186,6 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Smem& s = *reinterpret_cast<Smem*>(smem_raw);
-  // (the joining kernel is scheduled behind this grid and waits for its end)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
   Walk w;
   if (threadIdx.x < 32) w.begin(a, blockIdx.x, lane);

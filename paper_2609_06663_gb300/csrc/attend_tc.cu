@@ -169,6 +169,7 @@ __device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t 
   uint32_t n0 = 0, load = 0, ql = 0, k = 0;  // jobs before the item, tiles of K and V, of Q; this stream's jobs
   for (uint32_t e = 0;; ++e) {
     if (!wait_bar(s, a, &s.ifull[e % kItems], (e / kItems) & 1, 1u)) return;
+    const int left = s.items[e % kItems].vis - s.items[e % kItems].tile0 * kKeys;  // keys from its first tile on
     const int ntiles = s.items[e % kItems].ntiles;
     const bool two = s.items[e % kItems].ntok > a.tpt;
     mbar_arrive(&s.iempty[e % kItems]);
@@ -199,9 +200,11 @@ __device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t 
       if (!wait_bar(s, a, &s.pready[stream], k & 1, 5u)) return;
       tc_fence_after();
       const uint64_t vd = smem_desc(smem_u32(s.ring[sv]), kHalf, 1024, 2);
+      const int steps = min(left - t * kKeys + 31, kKeys) >> 5;  // blocks of 32 keys that are there
 #pragma unroll
       for (int k8 = 0; k8 < 8; ++k8)  // 16 keys a step
-        mma_bf16_ta(to, ts + k8 * 8u, vd + (uint64_t)(k8 * 128), idesc2, k8 > 0 || !first ? 1u : 0u);
+        if (k8 < 2 * steps)
+          mma_bf16_ta(to, ts + k8 * 8u, vd + (uint64_t)(k8 * 128), idesc2, k8 > 0 || !first ? 1u : 0u);
       mma_commit(&s.empty[sv]);
       first = false;
       ++k;
@@ -242,26 +245,24 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
       const int nv = it.vis - from;  // keys of the tile that are there (128 or more: all)
       if (!wait_warp(s, a, &s.sfull[stream], k & 1, 8u)) return;
       tc_fence_after();
+      const int nc = min(nv + 31, kKeys) >> 5;  // blocks of 32 keys that are there
       if (active) {
         uint32_t x[kKeys];
         tmem_ld<kKeys>(ts, x);
         tmem_wait_ld();
         tmem_landed(x);
         const int seen = lim - from;
-        if (!__all_sync(0xffffffffu, seen >= kKeys)) {
+        const int full = (int)__reduce_min_sync(0xffffffffu, (unsigned)max(seen, 0)) >> 5;  // blocks all rows see
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < kKeys; ++c)
-            if (c >= seen) x[c] = 0xff800000u;  // -inf
-        }
-        float mx[4];
+        for (int b = 0; b < 4; ++b) {
+          if (b >= full) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mx[c] = __uint_as_float(x[c]);
+            for (int c = 32 * b; c < 32 * b + 32; ++c)
+              if (c >= seen) x[c] = 0xff800000u;  // -inf
+          }
 #pragma unroll
-        for (int c = 4; c < kKeys; c += 4) {
-          mx[0] = fmaxf(mx[0], __uint_as_float(x[c]));
-          mx[1] = fmaxf(mx[1], __uint_as_float(x[c + 1]));
-          mx[2] = fmaxf(mx[2], __uint_as_float(x[c + 2]));
-          mx[3] = fmaxf(mx[3], __uint_as_float(x[c + 3]));
+          for (int c = 32 * b; c < 32 * b + 32; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(x[c]));
         }
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
         if (t == t0) {
@@ -272,7 +273,7 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
           const float f = up == -INFINITY ? 1.f : ex2(m - up);
           l *= f;
           m = up;
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < kD; c += 32) {
             uint32_t o[32];
             tmem_ld_x32(to + c, o);
@@ -285,31 +286,31 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
         }
         const float nref = m == -INFINITY ? 0.f : -m;
         float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        uint32_t w[kKeys / 2];
 #pragma unroll
-        for (int c = 0; c < kKeys; c += 2) {
-          fma_pair(x[c], x[c + 1], scale2, nref, nref);
-          const float e0 = ex2(__uint_as_float(x[c])), e1 = ex2(__uint_as_float(x[c + 1]));
-          add_pair(sum[c & 7], sum[(c & 7) + 1], e0, e1);
-          w[c / 2] = pack_bf16x2(e0, e1);
+        for (int b = 0; b < 4; ++b) {
+          if (b >= nc) continue;
+          uint32_t w[16];
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const int c = 32 * b + j;
+            fma_pair(x[c], x[c + 1], scale2, nref, nref);
+            const float e0 = ex2(__uint_as_float(x[c])), e1 = ex2(__uint_as_float(x[c + 1]));
+            add_pair(sum[c & 7], sum[(c & 7) + 1], e0, e1);
+            w[j / 2] = pack_bf16x2(e0, e1);
+          }
+          tmem_st_x16(ts + 16 * b, w);
         }
         l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
-        tmem_st_x32(ts, w);
-        tmem_st_x32(ts + 32, w + 32);
         tmem_wait_st();
       }
-      if (nv < kKeys) {
+      if (nv < 32 * nc) {
         // rows of V past the keys that are there may hold anything, and 0 * NaN is NaN
         const uint32_t vl = 2 * (tile_n + t) + 1, st = vl % kStages;
         if (!wait_warp(s, a, &s.full[st], (vl / kStages) & 1, 9u)) return;
-        if (row >= nv) {
-          uint4* v = reinterpret_cast<uint4*>(s.ring[st] + row * 128);
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            v[c] = make_uint4(0u, 0u, 0u, 0u);
-            v[c + kHalf / 16] = make_uint4(0u, 0u, 0u, 0u);
-          }
-        }
+        // (sixteen threads a row's two halves)
+        for (int r = nv + (row >> 4); r < 32 * nc; r += 8)
+          *reinterpret_cast<uint4*>(s.ring[st] + (row & 8 ? kHalf : 0u) + r * 128 + (row & 7) * 16) =
+              make_uint4(0u, 0u, 0u, 0u);
         fence_proxy_async_smem();
       }
       tc_fence_before();
@@ -373,6 +374,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     s.abort = 0;
     fence_mbar_init();
   }
+  if (warp == 0 && lane < 5) tma_prefetch_desc(&m.q + lane);
+  Walk w;
+  if (warp == 2) w.begin(a, blockIdx.x, lane);
   if (warp == 3) {
     tmem_alloc(&s.tmem, 512);
     tmem_relinquish();
@@ -380,8 +384,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  // (the joining kernel is scheduled behind this grid and waits for its end)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = s.tmem;
   uint32_t load = 0, ql = 0;
   // registers of the launch (3 x 168 a lane): 64 for the first warpgroup, 216 for a stream's
@@ -400,8 +402,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncwarp();
     } else if (warp == 2) {
-      Walk w;
-      w.begin(a, blockIdx.x, lane);
       for (uint32_t n = 0;; ++n) {
         Item it;
         const bool more = w.next(a, it);
