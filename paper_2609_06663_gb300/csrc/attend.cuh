@@ -8,7 +8,7 @@
 // sequence's own slots.  Its keys are cut into tiles of 128.  All items' tiles in a
 // row (the prefix's by head and token group, then the own ones by head, sequence
 // and token group) are dealt to the CTAs in equal runs, wherever items begin and
-// end.  An item counts kItemUnits units more than its tiles, for its queries, the start
+// end.  An item counts `lead` units more than its tiles, for its queries, the start
 // of its pipeline and its sums, so that a CTA with many short items has fewer
 // tiles: whatever the lengths, all CTAs take about as long.  A CTA writes each of its items' unnormalised sum, maximum and sum of
 // exponentials; a second kernel joins them row by row.  Partial sums are fp32.
@@ -23,10 +23,6 @@ constexpr int kKeys = 128;        // keys a tile
 constexpr int kTileRows = 128;    // most rows a partial sum of a continued item has
 constexpr int kMaxGroup = 64;     // query heads a KV head
 constexpr int kMaxAttendSms = 256;
-#ifndef ITEM_UNITS
-#define ITEM_UNITS 2
-#endif
-constexpr int kItemUnits = ITEM_UNITS;
 
 struct AttendArgs {
   const void* q;
@@ -42,6 +38,7 @@ struct AttendArgs {
   int span;   // tokens an item holds (one or two row tiles)
   int parts;  // partial sums a CTA may have of a row: 2 where two row groups share the tiles
   int P;      // CTAs
+  int lead;   // units an item counts beside its tiles
   int stall;  // fault injection: the first CTA's copies never come
   float scale_log2;
   unsigned long long timeout_ns;
@@ -96,15 +93,15 @@ __device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b, bool report)
   if (report && (s.L != len || s.start != s0 || s.start + s.T != s1)) note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)b);
   return s;
 }
-// Units of an item of so many tiles: none without a tile, else kItemUnits before its first tile's.
-__host__ __device__ inline int item_units(int tiles) { return tiles > 0 ? tiles + kItemUnits : 0; }
+// Units of an item of so many tiles: none without a tile, else a.lead before its first tile's.
+__host__ __device__ inline int item_units(const AttendArgs& a, int tiles) { return tiles > 0 ? tiles + a.lead : 0; }
 // Keys that the tokens of group `rg` of a sequence see at most, and the units of the groups before.
 __device__ __forceinline__ int seq_vis(const AttendArgs& a, const Seq& s, int rg) {
   return max(s.L - s.T + min(s.T, (rg + 1) * a.span), 0);
 }
 __device__ __forceinline__ int seq_units(const AttendArgs& a, const Seq& s, int groups) {
   int n = 0;
-  for (int rg = 0; rg < groups; ++rg) n += item_units(div_up(seq_vis(a, s, rg), kKeys));
+  for (int rg = 0; rg < groups; ++rg) n += item_units(a, div_up(seq_vis(a, s, rg), kKeys));
   return n;
 }
 // Rows of head h's prefix.
@@ -159,14 +156,14 @@ struct Walk {
     prefix_total = 0;
     if (a.prefix.rows > 0) {
       if (a.prefix.head_off == nullptr) {
-        const int per = groups * item_units(div_up(a.prefix.rows, kKeys));
+        const int per = groups * item_units(a, div_up(a.prefix.rows, kKeys));
         prefix_total = a.h_kv * per;
         if (lead)
           for (int h = lane; h < a.h_kv; h += 32) a.plan[PLAN_HEADS + h] = h * per;
       } else {
         for (int h0 = 0; h0 < a.h_kv; h0 += 32) {
           int row0, n = 0;
-          if (h0 + lane < a.h_kv) n = groups * item_units(div_up(prefix_rows(a, h0 + lane, row0, lead), kKeys));
+          if (h0 + lane < a.h_kv) n = groups * item_units(a, div_up(prefix_rows(a, h0 + lane, row0, lead), kKeys));
           const int up = scan(n, lane);
           if (lead && h0 + lane < a.h_kv) a.plan[PLAN_HEADS + h0 + lane] = prefix_total + up - n;
           prefix_total += __shfl_sync(0xffffffffu, up, 31);
@@ -192,7 +189,7 @@ struct Walk {
     base = 0;
     head = 0;
     const int total = prefix_total + a.h_kv * own;
-    const int run = max(div_up(total, a.P), kItemUnits + 1);  // (no CTA without a tile before the last)
+    const int run = max(div_up(total, a.P), a.lead + 1);  // (no CTA without a tile before the last)
     if (lead && lane == 0) {
       a.plan[PLAN_RUN] = run;
       a.plan[PLAN_PREFIX] = prefix_total;
@@ -216,7 +213,7 @@ struct Walk {
     if (x < prefix_total) {
       int h, y, nt, row0;
       if (a.prefix.head_off == nullptr) {
-        nt = item_units(div_up(a.prefix.rows, kKeys));
+        nt = item_units(a, div_up(a.prefix.rows, kKeys));
         h = x / (groups * nt);
         y = x - h * groups * nt;
         row0 = 0;
@@ -229,7 +226,7 @@ struct Walk {
           int n = 0, r0 = 0, rows = 0;
           if (h0 + lane < a.h_kv) {
             rows = prefix_rows(a, h0 + lane, r0, false);
-            n = groups * item_units(div_up(rows, kKeys));
+            n = groups * item_units(a, div_up(rows, kKeys));
           }
           const int up = scan(n, lane), all = __shfl_sync(0xffffffffu, up, 31);
           if (x < at + all) {
@@ -242,7 +239,7 @@ struct Walk {
           }
           at += all;
         }
-        nt = item_units(div_up(it.vis, kKeys));
+        nt = item_units(a, div_up(it.vis, kKeys));
       }
       const int rg = y / nt;
       it.source = 0;
@@ -253,8 +250,8 @@ struct Walk {
       it.lim0 = it.vis;
       it.slope = 0;
       y -= rg * nt;
-      skip = max(kItemUnits - y, 0);
-      it.tile0 = max(y - kItemUnits, 0);
+      skip = max(a.lead - y, 0);
+      it.tile0 = max(y - a.lead, 0);
       it.ntiles = min(nt - y, end - x) - skip;
       it.row0 = row0;
     } else {
@@ -279,7 +276,7 @@ struct Walk {
       q.T = __shfl_sync(0xffffffffu, s.T, l);
       q.L = __shfl_sync(0xffffffffu, s.L, l);
       int rg = 0, nt;
-      while (y >= (nt = item_units(div_up(seq_vis(a, q, rg), kKeys)))) {
+      while (y >= (nt = item_units(a, div_up(seq_vis(a, q, rg), kKeys)))) {
         y -= nt;
         if (++rg * a.span >= q.T) return false;
       }
@@ -291,8 +288,8 @@ struct Walk {
       it.lim0 = q.L - q.T + rg * a.span + 1;
       it.slope = 1;
       it.vis = seq_vis(a, q, rg);
-      skip = max(kItemUnits - y, 0);
-      it.tile0 = max(y - kItemUnits, 0);
+      skip = max(a.lead - y, 0);
+      it.tile0 = max(y - a.lead, 0);
       it.ntiles = min(nt - y, end - x) - skip;
       it.row0 = 0;
     }

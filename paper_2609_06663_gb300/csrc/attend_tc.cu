@@ -36,9 +36,13 @@ constexpr float kRaise = 8.f;       // log2 units
 struct Smem {
   uint8_t q[2][kTileBytes];
   uint8_t ring[kStages][kTileBytes];
-  uint64_t full[kStages], empty[kStages];
+  // A tile's arrival is signalled to those who use it, on a barrier that no other
+  // tile of the stage is signalled on: to stream 0, to stream 1 or (2) to both.
+  // (A wait tells a phase from its neighbours by its parity only, so whoever waits on a
+  // barrier has to see each of its phases.)
+  uint64_t full[3][kStages], empty[kStages];
   uint64_t qfull[2], qempty[2];
-  uint64_t sfull[2], pready[2], ofull[2];
+  uint64_t sfull[2], vready[2], pready[2], ofull[2];
   uint64_t ifull[kItems], iempty[kItems];
   uint64_t drained;
   Item items[kItems];
@@ -96,66 +100,75 @@ __device__ __forceinline__ void store8(float* p, const uint32_t* r) {
                : "memory");
 }
 
-// Copies of one tile of K (or V) into a stage: its pages' rows, a lane a page, or the prefix's.
-__device__ __forceinline__ void copy_tile(const AttendArgs& a, const CUtensorMap* prefix, const CUtensorMap* pages,
-                                          const Item& it, int tile, int page, int n_pages, uint8_t* dst,
-                                          uint64_t* bar, int lane) {
-  if (it.source == 0) {
-    if (lane < 2)
-      tma_load_3d(dst + lane * kHalf, prefix, bar, lane * 64, it.row0 + tile * kKeys,
-                  a.prefix.head_off != nullptr ? 0 : it.head);
-  } else if (lane < n_pages) {
-    const int slot = a.page_shift >= 7 ? (tile * kKeys) & (a.cache.page_size - 1) : 0;
-    uint8_t* at = dst + ((lane << a.page_shift) & (kKeys - 1)) * 128;
-    tma_load_4d(at, pages, bar, 0, slot, it.head, page);
-    tma_load_4d(at + kHalf, pages, bar, 64, slot, it.head, page);
-  }
-}
+// What has been issued, for those who wait for it to land.
+struct Issued {
+  uint32_t load = 0, ql = 0;  // tiles of K and V, and of Q
+  uint32_t phase[3] = {0, 0, 0};  // bit st: the parity of full[.][st]'s next phase
+  uint32_t kind[kStages] = {};    // the stage's last: index of its barrier
+};
 
-// load, ql: tiles of K and V, and of Q, whose copies have been issued.
-__device__ __forceinline__ void produce(Smem& s, const AttendArgs& a, const Maps& m, int lane, uint32_t& load,
-                                        uint32_t& ql) {
+__device__ __forceinline__ void produce(Smem& s, const AttendArgs& a, const Maps& m, int lane, Issued& d) {
   ItemReader items;
   Item it;
+  uint32_t n0 = 0;  // jobs before the item
   const int q_bytes = a.tpt * a.g * 256;
   while (items.next(s, a, it, lane)) {
     const int nq = it.ntok > a.tpt ? 2 : 1;
     for (int r = 0; r < nq; ++r) {
-      const int slot = ql & 1;
-      if (!wait_warp(s, a, &s.qempty[slot], ((ql >> 1) & 1) ^ 1, 2u)) return;
+      const int slot = d.ql & 1;
+      if (!wait_warp(s, a, &s.qempty[slot], ((d.ql >> 1) & 1) ^ 1, 2u)) return;
       if (lane == 0) mbar_expect_tx(&s.qfull[slot], (uint32_t)q_bytes);
       __syncwarp();
       if (lane < 2)
         tma_load_3d(s.q[slot] + lane * kHalf, &m.q, &s.qfull[slot], lane * 64, it.head * a.g, it.tok0 + r * a.tpt);
-      ++ql;
+      ++d.ql;
     }
+    // what this lane copies of a tile: half the columns of the prefix's rows, or a page of it
+    const bool own = it.source != 0;
+    const int head = own || a.prefix.head_off == nullptr ? it.head : 0;
+    const uint32_t box = own ? (uint32_t)min(a.cache.page_size, kKeys) : kKeys;
+    const uint32_t at = own ? (((uint32_t)lane << a.page_shift) & (kKeys - 1)) * 128u : lane * kHalf;
+    const int* table = a.cache.table + (int64_t)it.seq * a.cache.table_stride;
+    int c0 = 0, n = 2, page = 0;
+    auto look_up = [&](int t) {  // this lane's page of tile t, ahead of its turn
+      const int from = t * kKeys, to = min(from + kKeys, it.vis);
+      c0 = from >> a.page_shift;
+      n = ((to - 1) >> a.page_shift) - c0 + 1;
+      if (lane < n) page = table[c0 + lane];
+    };
+    if (own) look_up(it.tile0);
     for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
-      int n_pages = 0, page = 0;
-      uint32_t bytes = kTileBytes;
-      if (it.source != 0) {
-        const int from = t * kKeys, to = min(from + kKeys, it.vis);
-        const int c0 = from >> a.page_shift;
-        n_pages = ((to - 1) >> a.page_shift) - c0 + 1;
-        bytes = (uint32_t)(min(a.cache.page_size, kKeys) * n_pages) * 256u;
-        if (lane < n_pages) {
-          page = a.cache.table[(int64_t)it.seq * a.cache.table_stride + c0 + lane];
-          if (page < 0 || page >= a.cache.n_pages) {
-            note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)it.seq);
-            page = a.cache.n_pages;  // out of the map's bounds: zeros
-          }
-        }
-      }
+      const int row = own ? (t * kKeys) & (a.cache.page_size - 1) : it.row0 + t * kKeys;
+      const int copies = n, z = page;
+      const uint32_t kind = nq == 2 ? 2u : (n0 + (uint32_t)(t - it.tile0)) & 1;
+      const bool bad = own && lane < copies && (z < 0 || z >= a.cache.n_pages);
+      if (bad) note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)it.seq);
+      const int w = bad ? a.cache.n_pages : z;  // out of the map's bounds: zeros
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
-        const uint32_t st = load % kStages;
-        if (!wait_warp(s, a, &s.empty[st], ((load / kStages) & 1) ^ 1, 3u)) return;
-        if (lane == 0) mbar_expect_tx(&s.full[st], bytes);
+        const uint32_t st = d.load % kStages;
+        if (!wait_warp(s, a, &s.empty[st], ((d.load / kStages) & 1) ^ 1, 3u)) return;
+        uint8_t* dst = s.ring[st] + at;
+        uint64_t* bar = &s.full[kind][st];
+#pragma unroll
+        for (uint32_t i = 0; i < 3; ++i) d.phase[i] ^= i == kind ? 1u << st : 0u;
+#pragma unroll
+        for (uint32_t i = 0; i < kStages; ++i) d.kind[i] = i == st ? kind : d.kind[i];
+        if (lane == 0) mbar_expect_tx(bar, own ? box * copies * 256u : kTileBytes);
         __syncwarp();
-        copy_tile(a, kv == 0 ? &m.pk : &m.pv, kv == 0 ? &m.ck : &m.cv, it, t, page, n_pages, s.ring[st], &s.full[st],
-                  lane);
-        ++load;
+        if (lane < copies) {
+          if (own) {
+            tma_load_4d(dst, kv == 0 ? &m.ck : &m.cv, bar, 0, row, head, w);
+            tma_load_4d(dst + kHalf, kv == 0 ? &m.ck : &m.cv, bar, 64, row, head, w);
+          } else {
+            tma_load_3d(dst, kv == 0 ? &m.pk : &m.pv, bar, lane * 64, row, head);
+          }
+        }
+        ++d.load;
+        if (kv == 0 && own && t + 1 < it.tile0 + it.ntiles) look_up(t + 1);
       }
     }
+    n0 += (uint32_t)(it.ntiles * nq);
   }
 }
 
@@ -167,6 +180,7 @@ __device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t 
   constexpr uint32_t idesc1 = idesc_bf16(128, 128, false, false), idesc2 = idesc_bf16(128, 128, false, true);
   const uint32_t ts = tmem + stream * 256u, to = ts + 128u;  // scores, later the weights; the sum
   uint32_t n0 = 0, load = 0, ql = 0, k = 0;  // jobs before the item, tiles of K and V, of Q; this stream's jobs
+  uint32_t phase[2] = {0, 0};  // bit st: parity of the next phase of this stream's full[.][st], of both streams'
   for (uint32_t e = 0;; ++e) {
     if (!wait_bar(s, a, &s.ifull[e % kItems], (e / kItems) & 1, 1u)) return;
     const int left = s.items[e % kItems].vis - s.items[e % kItems].tile0 * kKeys;  // keys from its first tile on
@@ -175,18 +189,20 @@ __device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t 
     mbar_arrive(&s.iempty[e % kItems]);
     if (ntiles <= 0) return;
     const uint32_t p = (stream ^ n0) & 1, q = ql + (two ? p : 0);  // its row tile, or its key tiles in turn
-    if (!wait_bar(s, a, &s.qfull[q & 1], (q >> 1) & 1, 6u)) return;
+    // Every buffer is released by two arrivals: one of each stream for Q and, with two
+    // row tiles, for K and V; with one row tile both of the key tile's stream.
+    for (uint32_t x = ql; x < ql + (two ? 2u : 1u); ++x) {
+      if (!wait_bar(s, a, &s.qfull[x & 1], (x >> 1) & 1, 6u)) return;
+      if (x != q) mbar_arrive(&s.qempty[x & 1]);
+    }
     const uint64_t qd = smem_desc(smem_u32(s.q[q & 1]), 16, 1024, 2);
-    bool first = true;
-    for (int t = 0; t < ntiles; ++t, load += 2) {
-      const uint32_t sk = load % kStages, sv = (load + 1) % kStages;
-      if (!wait_bar(s, a, &s.full[sk], (load / kStages) & 1, 7u)) return;
-      if (!two && ((uint32_t)t & 1) != p) {  // the other stream's
-        mbar_arrive(&s.empty[sk]);
-        if (!wait_bar(s, a, &s.full[sv], ((load + 1) / kStages) & 1, 4u)) return;
-        mbar_arrive(&s.empty[sv]);
-        continue;
-      }
+    const int step = two ? 1 : 2, t0 = two ? 0 : (int)p;
+    uint64_t* full = s.full[two ? 2u : stream];
+    uint32_t ph = two ? phase[1] : phase[0];
+    for (int t = t0; t < ntiles; t += step, ++k) {
+      const uint32_t sk = (load + 2 * t) % kStages, sv = (load + 2 * t + 1) % kStages;
+      if (!wait_bar(s, a, &full[sk], (ph >> sk) & 1, 7u)) return;
+      ph ^= 1u << sk;
       tc_fence_after();
       const uint64_t kd = smem_desc(smem_u32(s.ring[sk]), 16, 1024, 2);
 #pragma unroll
@@ -196,28 +212,31 @@ __device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t 
       }
       mma_commit(&s.sfull[stream]);
       mma_commit(&s.empty[sk]);
-      if (!wait_bar(s, a, &s.full[sv], ((load + 1) / kStages) & 1, 4u)) return;
+      if (!two) mma_commit(&s.empty[sk]);
+      const int there = left - t * kKeys;  // keys of the tile
+      if (!wait_bar(s, a, &full[sv], (ph >> sv) & 1, 4u)) return;
+      ph ^= 1u << sv;
+      if (there < kKeys) mbar_arrive(&s.vready[stream]);
       if (!wait_bar(s, a, &s.pready[stream], k & 1, 5u)) return;
       tc_fence_after();
       const uint64_t vd = smem_desc(smem_u32(s.ring[sv]), kHalf, 1024, 2);
-      const int steps = min(left - t * kKeys + 31, kKeys) >> 5;  // blocks of 32 keys that are there
+      const int steps = min(there + 31, kKeys) >> 5;  // blocks of 32 keys that are there
 #pragma unroll
       for (int k8 = 0; k8 < 8; ++k8)  // 16 keys a step
         if (k8 < 2 * steps)
-          mma_bf16_ta(to, ts + k8 * 8u, vd + (uint64_t)(k8 * 128), idesc2, k8 > 0 || !first ? 1u : 0u);
+          mma_bf16_ta(to, ts + k8 * 8u, vd + (uint64_t)(k8 * 128), idesc2, k8 > 0 || t > t0 ? 1u : 0u);
       mma_commit(&s.empty[sv]);
-      first = false;
-      ++k;
+      if (!two) mma_commit(&s.empty[sv]);
     }
-    if (!first) mma_commit(&s.ofull[stream]);
-    // both streams release every tile of Q, whether they use it or not
-    if (first) mbar_arrive(&s.qempty[q & 1]);
-    else mma_commit(&s.qempty[q & 1]);
-    if (two) {
-      const uint32_t o = ql + (p ^ 1);
-      if (!wait_bar(s, a, &s.qfull[o & 1], (o >> 1) & 1, 6u)) return;
-      mbar_arrive(&s.qempty[o & 1]);
+    if (two) phase[1] = ph;
+    else phase[0] = ph;
+    if (t0 < ntiles) {
+      mma_commit(&s.ofull[stream]);
+      mma_commit(&s.qempty[q & 1]);
+    } else {
+      mbar_arrive(&s.qempty[q & 1]);
     }
+    load += 2 * (uint32_t)ntiles;
     n0 += (uint32_t)ntiles * (two ? 2u : 1u);
     ql += two ? 2u : 1u;
   }
@@ -230,7 +249,8 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
   const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
   ItemReader items;
   Item it;
-  uint32_t n0 = 0, tile_n = 0, k = 0, ends = 0;  // jobs and tiles before the item; this stream's jobs; its items
+  // jobs and tiles before the item; this stream's jobs, items and ragged tiles
+  uint32_t n0 = 0, tile_n = 0, k = 0, ends = 0, tails = 0;
   while (items.next(s, a, it, lane)) {
     const bool two = it.ntok > a.tpt;
     const int p = (stream ^ (int)n0) & 1;  // which of the item's row tiles, or of its key tiles in turn
@@ -303,15 +323,16 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
         l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
         tmem_wait_st();
       }
-      if (nv < 32 * nc) {
+      if (nv < kKeys) {
         // rows of V past the keys that are there may hold anything, and 0 * NaN is NaN
-        const uint32_t vl = 2 * (tile_n + t) + 1, st = vl % kStages;
-        if (!wait_warp(s, a, &s.full[st], (vl / kStages) & 1, 9u)) return;
+        const uint32_t st = (2 * (tile_n + t) + 1) % kStages;
+        if (!wait_warp(s, a, &s.vready[stream], tails & 1, 9u)) return;
         // (sixteen threads a row's two halves)
         for (int r = nv + (row >> 4); r < 32 * nc; r += 8)
           *reinterpret_cast<uint4*>(s.ring[st] + (row & 8 ? kHalf : 0u) + r * 128 + (row & 7) * 16) =
               make_uint4(0u, 0u, 0u, 0u);
         fence_proxy_async_smem();
+        ++tails;
       }
       tc_fence_before();
       __syncwarp();
@@ -356,13 +377,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(&s.full[i], 1);
-      mbar_init(&s.empty[i], 2);  // both streams, whether they use the tile or not
+      for (int k = 0; k < 3; ++k) mbar_init(&s.full[k][i], 1);
+      mbar_init(&s.empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.qfull[i], 1);
       mbar_init(&s.qempty[i], 2);
       mbar_init(&s.sfull[i], 1);
+      mbar_init(&s.vready[i], 1);
       mbar_init(&s.pready[i], 4);
       mbar_init(&s.ofull[i], 1);
     }
@@ -385,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s.tmem;
-  uint32_t load = 0, ql = 0;
+  Issued d;
   // registers of the launch (3 x 168 a lane): 64 for the first warpgroup, 216 for a stream's
   if (warp >= 4) {
     reg_alloc<216>();
@@ -394,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     reg_dealloc<64>();
     if (warp == 0) {
       // (the injected stall: the first CTA's tiles never come)
-      if (!(a.stall != 0 && blockIdx.x == 0)) produce(s, a, m, lane, load, ql);
+      if (!(a.stall != 0 && blockIdx.x == 0)) produce(s, a, m, lane, d);
     } else if (warp == 1 || warp == 3) {
       if (lane == 0) {
         multiply(s, a, tmem, (uint32_t)warp >> 1);
@@ -421,10 +443,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 1 || warp == 3) drain_bar(&s.drained, 0u);
   if (warp == 0) {
     // ... and every copy has landed: the last of each buffer's, should no one have waited for it
+#pragma unroll
     for (uint32_t i = 0; i < kStages; ++i)
-      if (load > i) drain_bar(&s.full[i], ((load - 1 - i) / kStages) & 1);
+      if (d.load > i) {
+        const uint32_t k = d.kind[i], next = k == 0 ? d.phase[0] : k == 1 ? d.phase[1] : d.phase[2];
+        drain_bar(&s.full[k][i], ((next >> i) & 1) ^ 1);
+      }
     for (uint32_t i = 0; i < 2; ++i)
-      if (ql > i) drain_bar(&s.qfull[i], ((ql - 1 - i) / 2) & 1);
+      if (d.ql > i) drain_bar(&s.qfull[i], ((d.ql - 1 - i) / 2) & 1);
   }
   __syncthreads();
   if (warp == 3) {
