@@ -142,8 +142,8 @@ typedef struct {
   float scale;         /* of q . k; <= 0 selects 1 / sqrt(d)                                 */
   int64_t q_token, q_head, out_token, out_head; /* strides of q and out                      */
   uint32_t flags;      /* ECOKV_FLAG_FORCE_SIMT (bf16 on CUDA cores) or ECOKV_FLAG_TEST_STALL
-                          (bf16 on tensor cores, else ECOKV_ERR_UNSUPPORTED: a CTA's tiles never
-                          come, its waits run out, ECOKV_ERR_TIMEOUT is recorded)            */
+                          (bf16 on tensor cores, else ECOKV_ERR_UNSUPPORTED: no tile of the cache
+                          ever comes, the waits run out, ECOKV_ERR_TIMEOUT is recorded)            */
   uint32_t timeout_us; /* as in ecokv_params                                                 */
 } ecokv_attend_params;
 

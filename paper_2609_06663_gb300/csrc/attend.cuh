@@ -8,9 +8,10 @@
 // sequence's own slots.  Its keys are cut into tiles of 128.  All items' tiles in a
 // row (the prefix's by head and token group, then the own ones by head, sequence
 // and token group) are dealt to the CTAs in equal runs, wherever items begin and
-// end.  An item counts `lead` units more than its tiles, for its queries, the start
-// of its pipeline and its sums, so that a CTA with many short items has fewer
-// tiles: whatever the lengths, all CTAs take about as long.  A CTA writes each of its items' unnormalised sum, maximum and sum of
+// end.  A tile counts a unit for each row tile that it meets (two take twice as
+// long), and an item lead_units() more, for its queries, the start of its pipeline
+// and its sums, so that a CTA with many short items has fewer tiles: whatever the
+// lengths, all CTAs take about as long.  A CTA writes each of its items' unnormalised sum, maximum and sum of
 // exponentials; a second kernel joins them row by row.  Partial sums are fp32.
 #pragma once
 
@@ -38,8 +39,8 @@ struct AttendArgs {
   int span;   // tokens an item holds (one or two row tiles)
   int parts;  // partial sums a CTA may have of a row: 2 where two row groups share the tiles
   int P;      // CTAs
-  int lead;   // units an item counts beside its tiles
-  int stall;  // fault injection: the first CTA's copies never come
+  int lead;   // see lead_units()
+  int stall;  // fault injection: no tile ever comes
   float scale_log2;
   unsigned long long timeout_ns;
   // workspace
@@ -93,15 +94,27 @@ __device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b, bool report)
   if (report && (s.L != len || s.start != s0 || s.start + s.T != s1)) note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)b);
   return s;
 }
-// Units of an item of so many tiles: none without a tile, else a.lead before its first tile's.
-__host__ __device__ inline int item_units(const AttendArgs& a, int tiles) { return tiles > 0 ? tiles + a.lead : 0; }
+// Units of a tile of an item of so many tokens; those an item has before its first
+// tile's (one row tile: 1, two: 4, their sums being up to 128 KB; at 1 for both 16
+// sequences of 31 to 61 tokens over 6554 rows took 176 us, at 4 122; at 4 for both 61
+// single tokens of 32 heads over 1095 rows 79, at 1 54); all of an item's.
+__host__ __device__ inline int tile_units(const AttendArgs& a, int ntok) { return ntok > a.tpt ? 2 : 1; }
+__host__ __device__ inline int lead_units(const AttendArgs& a, int ntok) { return ntok > a.tpt ? 4 * a.lead : a.lead; }
+__host__ __device__ inline int item_units(const AttendArgs& a, int tiles, int ntok) {
+  return tiles > 0 ? tiles * tile_units(a, ntok) + lead_units(a, ntok) : 0;
+}
+// ... of all token groups of the prefix of one head (the last may be a shorter one).
+__host__ __device__ inline int prefix_units(const AttendArgs& a, int tiles) {
+  const int groups = div_up(a.tokens, a.span), last = a.tokens - (groups - 1) * a.span;
+  return (groups - 1) * item_units(a, tiles, a.span) + item_units(a, tiles, last);
+}
 // Keys that the tokens of group `rg` of a sequence see at most, and the units of the groups before.
 __device__ __forceinline__ int seq_vis(const AttendArgs& a, const Seq& s, int rg) {
   return max(s.L - s.T + min(s.T, (rg + 1) * a.span), 0);
 }
 __device__ __forceinline__ int seq_units(const AttendArgs& a, const Seq& s, int groups) {
   int n = 0;
-  for (int rg = 0; rg < groups; ++rg) n += item_units(a, div_up(seq_vis(a, s, rg), kKeys));
+  for (int rg = 0; rg < groups; ++rg) n += item_units(a, div_up(seq_vis(a, s, rg), kKeys), min(s.T - rg * a.span, a.span));
   return n;
 }
 // Rows of head h's prefix.
@@ -120,7 +133,6 @@ __device__ __forceinline__ int prefix_rows(const AttendArgs& a, int h, int& row0
 struct Walk {
   int x, end;               // units of all items: next, one past the CTA's last
   int prefix_total, own;    // units of the prefix; of one head's own slots
-  int groups;               // token groups of the prefix
   int lane;
   // the 32 sequences from b0 on: first unit of the first of them within a head
   int b0, base, head;
@@ -152,18 +164,17 @@ struct Walk {
   __device__ __forceinline__ void begin(const AttendArgs& a, int cta, int lane_) {
     lane = lane_;
     const bool lead = cta == 0;
-    groups = div_up(a.tokens, a.span);
     prefix_total = 0;
     if (a.prefix.rows > 0) {
       if (a.prefix.head_off == nullptr) {
-        const int per = groups * item_units(a, div_up(a.prefix.rows, kKeys));
+        const int per = prefix_units(a, div_up(a.prefix.rows, kKeys));
         prefix_total = a.h_kv * per;
         if (lead)
           for (int h = lane; h < a.h_kv; h += 32) a.plan[PLAN_HEADS + h] = h * per;
       } else {
         for (int h0 = 0; h0 < a.h_kv; h0 += 32) {
           int row0, n = 0;
-          if (h0 + lane < a.h_kv) n = groups * item_units(a, div_up(prefix_rows(a, h0 + lane, row0, lead), kKeys));
+          if (h0 + lane < a.h_kv) n = prefix_units(a, div_up(prefix_rows(a, h0 + lane, row0, lead), kKeys));
           const int up = scan(n, lane);
           if (lead && h0 + lane < a.h_kv) a.plan[PLAN_HEADS + h0 + lane] = prefix_total + up - n;
           prefix_total += __shfl_sync(0xffffffffu, up, 31);
@@ -189,7 +200,8 @@ struct Walk {
     base = 0;
     head = 0;
     const int total = prefix_total + a.h_kv * own;
-    const int run = max(div_up(total, a.P), a.lead + 1);  // (no CTA without a tile before the last)
+    // (at least a tile's units: no CTA between the first and the last of an item is without a tile of it)
+    const int run = max(div_up(total, a.P), tile_units(a, a.span));
     if (lead && lane == 0) {
       a.plan[PLAN_RUN] = run;
       a.plan[PLAN_PREFIX] = prefix_total;
@@ -209,13 +221,13 @@ struct Walk {
   }
   // The part of an item from unit x on, which may be less than its first tile (ntiles <= 0).
   __device__ __forceinline__ bool at(const AttendArgs& a, Item& it) {
-    int skip;  // units before the first tile
+    int y, nt;  // place within the item; its tiles
     if (x < prefix_total) {
-      int h, y, nt, row0;
+      int h, row0;
       if (a.prefix.head_off == nullptr) {
-        nt = item_units(a, div_up(a.prefix.rows, kKeys));
-        h = x / (groups * nt);
-        y = x - h * groups * nt;
+        const int per = prefix_units(a, div_up(a.prefix.rows, kKeys));
+        h = x / per;
+        y = x - h * per;
         row0 = 0;
         it.vis = a.prefix.rows;
       } else {
@@ -226,7 +238,7 @@ struct Walk {
           int n = 0, r0 = 0, rows = 0;
           if (h0 + lane < a.h_kv) {
             rows = prefix_rows(a, h0 + lane, r0, false);
-            n = groups * item_units(a, div_up(rows, kKeys));
+            n = prefix_units(a, div_up(rows, kKeys));
           }
           const int up = scan(n, lane), all = __shfl_sync(0xffffffffu, up, 31);
           if (x < at + all) {
@@ -239,9 +251,9 @@ struct Walk {
           }
           at += all;
         }
-        nt = item_units(a, div_up(it.vis, kKeys));
       }
-      const int rg = y / nt;
+      nt = div_up(it.vis, kKeys);
+      const int rg = y / item_units(a, nt, a.span);
       it.source = 0;
       it.head = h;
       it.seq = 0;
@@ -249,13 +261,10 @@ struct Walk {
       it.ntok = min(a.span, a.tokens - it.tok0);
       it.lim0 = it.vis;
       it.slope = 0;
-      y -= rg * nt;
-      skip = max(a.lead - y, 0);
-      it.tile0 = max(y - a.lead, 0);
-      it.ntiles = min(nt - y, end - x) - skip;
+      y -= rg * item_units(a, nt, a.span);
       it.row0 = row0;
     } else {
-      int y = x - prefix_total;
+      y = x - prefix_total;
       const int h = y / own;
       y -= h * own;
       if (h != head && b0 != 0) {
@@ -275,9 +284,9 @@ struct Walk {
       q.start = __shfl_sync(0xffffffffu, s.start, l);
       q.T = __shfl_sync(0xffffffffu, s.T, l);
       q.L = __shfl_sync(0xffffffffu, s.L, l);
-      int rg = 0, nt;
-      while (y >= (nt = item_units(a, div_up(seq_vis(a, q, rg), kKeys)))) {
-        y -= nt;
+      int rg = 0, n;
+      while (y >= (n = item_units(a, div_up(seq_vis(a, q, rg), kKeys), min(q.T - rg * a.span, a.span)))) {
+        y -= n;
         if (++rg * a.span >= q.T) return false;
       }
       it.source = 1;
@@ -288,13 +297,16 @@ struct Walk {
       it.lim0 = q.L - q.T + rg * a.span + 1;
       it.slope = 1;
       it.vis = seq_vis(a, q, rg);
-      skip = max(a.lead - y, 0);
-      it.tile0 = max(y - a.lead, 0);
-      it.ntiles = min(nt - y, end - x) - skip;
       it.row0 = 0;
+      nt = div_up(it.vis, kKeys);
     }
-    x += skip + it.ntiles;
-    return true;
+    // the tiles whose first unit lies within this CTA's part of the item, y .. z - 1
+    const int u = tile_units(a, it.ntok), z = min(item_units(a, nt, it.ntok), y + end - x);
+    const int lead = lead_units(a, it.ntok);
+    it.tile0 = div_up(max(y - lead, 0), u);
+    it.ntiles = div_up(max(z - lead, 0), u) - it.tile0;
+    x += z - y;
+    return z > y;  // (else nothing would move on)
   }
 };
 

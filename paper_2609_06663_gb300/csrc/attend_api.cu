@@ -6,9 +6,6 @@
 #include "attend.cuh"
 #include "ptx.cuh"
 
-#ifndef LEAD
-#define LEAD 2
-#endif
 namespace ecokv {
 namespace {
 
@@ -44,8 +41,9 @@ __device__ __forceinline__ Parts find_parts(const AttendArgs& a, int source, int
                                             int token, int hq) {
   Parts p{0, 0, 1, 0, 0, 0};
   if (nt <= 0) return p;
-  p.c0 = (unit + a.lead) / run;
-  const int ctas = (unit + a.lead + nt - 1) / run - p.c0 + 1;
+  unit += lead_units(a, ntok);
+  p.c0 = unit / run;
+  const int ctas = (unit + (nt - 1) * tile_units(a, ntok)) / run - p.c0 + 1;
   if (ntok > a.tpt) p.j0 = k / a.tpt;  // two row tiles: the row is in one of them
   else p.nj = a.parts;
   p.n = ctas * p.nj;
@@ -78,7 +76,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __gr
   if (a.prefix.rows > 0) {
     int row0;
     const int nt = div_up(prefix_rows(a, h, row0, false), kKeys), rg = token / a.span;
-    src[0] = find_parts(a, 0, a.plan[PLAN_HEADS + h] + rg * item_units(a, nt), nt, run, token - rg * a.span,
+    src[0] = find_parts(a, 0, a.plan[PLAN_HEADS + h] + rg * item_units(a, nt, a.span), nt, run, token - rg * a.span,
                         min(a.span, a.tokens - rg * a.span), token, hq);
   }
   if (a.has_cache) {
@@ -296,16 +294,18 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   a.tpt = (tc ? kTileRows : 64) / a.g;
   a.span = tc ? 2 * a.tpt : a.tpt;
   a.parts = tc ? 2 : 1;
-  a.lead = tc ? LEAD : 0;
+  a.lead = tc ? 1 : 0;
   a.stall = (p->flags & ECOKV_FLAG_TEST_STALL) ? 1 : 0;
   a.P = attend_sms();
   const double scale = p->scale > 0.f ? (double)p->scale : 1.0 / sqrt((double)kD);
   a.scale_log2 = (float)(1.4426950408889634 * scale);
   a.timeout_ns = (p->timeout_us ? (unsigned long long)p->timeout_us : 2000000ull) * 1000ull;
   // units of every item, counted in 32 bits by the kernels
-  const long long groups = (a.tokens + a.span - 1) / a.span, cap_tiles = item_units(a, (a.cap + kKeys - 1) / kKeys);
-  const long long tiles = a.h_kv * (groups * item_units(a, (a.prefix.rows + kKeys - 1) / kKeys) + (groups + a.batch) * cap_tiles);
-  if (tiles > 0x7fffffff || groups * cap_tiles > (1 << 25)) return ECOKV_ERR_UNSUPPORTED;
+  const long long groups = (a.tokens + a.span - 1) / a.span;
+  const long long of_cap = item_units(a, (a.cap + kKeys - 1) / kKeys, a.span),
+                  of_prefix = item_units(a, (a.prefix.rows + kKeys - 1) / kKeys, a.span);
+  const long long units = a.h_kv * (groups * of_prefix + (groups + a.batch) * of_cap);
+  if (units > 0x7fffffff || groups * of_cap > (1 << 25)) return ECOKV_ERR_UNSUPPORTED;
   char* w = static_cast<char*>(ws);
   const AttendLayout L = attend_layout(a.tokens, a.batch, a.h_q, a.h_kv, a.parts);
   a.status = reinterpret_cast<unsigned*>(w);

@@ -415,8 +415,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     reg_dealloc<64>();
     if (warp == 0) {
-      // (the injected stall: the first CTA's tiles never come)
-      if (!(a.stall != 0 && blockIdx.x == 0)) produce(s, a, m, lane, d);
+      // (the injected stall: no tile ever comes)
+      if (a.stall == 0) produce(s, a, m, lane, d);
     } else if (warp == 1 || warp == 3) {
       if (lane == 0) {
         multiply(s, a, tmem, (uint32_t)warp >> 1);
