@@ -6,14 +6,18 @@
 #include "attend.cuh"
 #include "ptx.cuh"
 
+#ifndef JOIN_ROWS
+#define JOIN_ROWS 2048
+#endif
 namespace ecokv {
 namespace {
 
-// kWarps warps a row (token, query head), kJoinWarps / kWarps rows a CTA: the row's
-// partial sums, wherever the CTAs left them, weighted by 2^(their maximum - the
-// largest).  Every warp finds the weights, 32 at a time, and sums those of its
-// share; each lane has four columns.  What bounds it is the latency of its chain of
-// loads, so a row with many parts has them read by four warps at once.
+// A row's (token, query head) partial sums, wherever the CTAs left them, weighted by
+// 2^(their maximum - the largest).  What bounds this is the latency of its chain of
+// loads.  With few rows a CTA takes one, its warps a share of the parts each, and the
+// sums are loaded beside the weights that may turn out to be zero; with many rows
+// a warp takes the rows of one token and KV head, whose parts lie side by side.
+// Each lane has four columns.
 constexpr int kJoinWarps = 4;
 
 template <typename T>
@@ -64,92 +68,76 @@ __device__ __forceinline__ const float* part(const AttendArgs& a, const Parts& p
   return a.next_o + at * kD;
 }
 
-template <typename T, int kWarps>
-__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __grid_constant__ AttendArgs a) {
-  __shared__ float4 part_acc[kJoinWarps][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp % kWarps;
-  const long long id = (long long)blockIdx.x * (kJoinWarps / kWarps) + warp / kWarps;
-  if (id >= (long long)a.tokens * a.h_q) return;  // (with kWarps = kJoinWarps the whole CTA)
-  const int token = (int)(id / a.h_q), hq = (int)(id - (long long)token * a.h_q), h = hq / a.g;
-  Parts src[2] = {{0, 0, 1, 0, 0, 0}, {0, 0, 1, 0, 0, 0}};
-  const int run = a.plan[PLAN_RUN], prefix_total = a.plan[PLAN_PREFIX], own = a.plan[PLAN_OWN];
+// The parts of both sources of a row in one list: entry e < src[0].n is the prefix's.
+struct PartList {
+  Parts src[2];
+  int n;
+  // (row r of the token's rows of the KV head, of which row 0 was looked up)
+  __device__ __forceinline__ const float* at(const AttendArgs& a, int e, int r, float2& ml) const {
+    const bool second = e >= src[0].n;
+    Parts p = second ? src[1] : src[0];
+    p.first += r;
+    p.row += r;
+    return part(a, p, second ? e - src[0].n : e, ml);
+  }
+};
+
+__device__ __forceinline__ PartList list_parts(const AttendArgs& a, int token, int h, int lane) {
+  PartList l{};
+  l.src[0].nj = l.src[1].nj = 1;
+  int b = token;
+  if (a.has_cache && a.starts != nullptr) {
+    b = 0;
+    for (int j = lane; j < a.batch; j += 32) b += a.starts[1 + j] <= token ? 1 : 0;
+    b = min((int)__reduce_add_sync(0xffffffffu, (unsigned)b), a.batch - 1);
+  }
+  const int4 head = *reinterpret_cast<const int4*>(a.plan);
+  const int run = head.x, prefix_total = head.y, own = head.z;
   if (a.prefix.rows > 0) {
     int row0;
+    const int first = a.plan[PLAN_HEADS + h];
     const int nt = div_up(prefix_rows(a, h, row0, false), kKeys), rg = token / a.span;
-    src[0] = find_parts(a, 0, a.plan[PLAN_HEADS + h] + rg * item_units(a, nt, a.span), nt, run, token - rg * a.span,
-                        min(a.span, a.tokens - rg * a.span), token, hq);
+    l.src[0] = find_parts(a, 0, first + rg * item_units(a, nt, a.span), nt, run, token - rg * a.span,
+                          min(a.span, a.tokens - rg * a.span), token, h * a.g);
   }
   if (a.has_cache) {
-    int b = token;
-    if (a.starts != nullptr) {
-      b = 0;
-      for (int j = lane; j < a.batch; j += 32) b += a.starts[1 + j] <= token ? 1 : 0;
-      b = min((int)__reduce_add_sync(0xffffffffu, (unsigned)b), a.batch - 1);
-    }
     const int first = a.plan[PLAN_HEADS + a.h_kv + b];
     const Seq s = load_seq(a, b, false);
     const int i = token - s.start;
     if (i >= 0 && i < s.T && own > 0) {
       const int rg = i / a.span;
-      src[1] = find_parts(a, 1, prefix_total + h * own + first + seq_units(a, s, rg),
-                          div_up(seq_vis(a, s, rg), kKeys), run, i - rg * a.span, min(a.span, s.T - rg * a.span),
-                          token, hq);
+      l.src[1] = find_parts(a, 1, prefix_total + h * own + first + seq_units(a, s, rg),
+                            div_up(seq_vis(a, s, rg), kKeys), run, i - rg * a.span, min(a.span, s.T - rg * a.span),
+                            token, h * a.g);
     }
   }
-  // the parts of both sources in one row: entry e < src[0].n is the prefix's
-  const int n = src[0].n + src[1].n;
-  float M = -INFINITY, M0 = -INFINITY, l0 = 0.f;
-  const float* o0 = nullptr;
-  for (int e = lane; e < n; e += 32) {
-    float2 ml;
-    const float* o = e < src[0].n ? part(a, src[0], e, ml) : part(a, src[1], e - src[0].n, ml);
-    if (e == lane) {
-      o0 = o;
-      M0 = ml.x;
-      l0 = ml.y;
-    }
-    M = fmaxf(M, ml.x);
+  l.n = l.src[0].n + l.src[1].n;
+  return l;
+}
+
+// acc += w v, v = 0 where w is (a part that saw no key is not written).
+__device__ __forceinline__ void add_part(float4& acc, float w, float4 v) {
+  const bool any = w > 0.f;
+  acc.x = fmaf(w, any ? v.x : 0.f, acc.x);
+  acc.y = fmaf(w, any ? v.y : 0.f, acc.y);
+  acc.z = fmaf(w, any ? v.z : 0.f, acc.z);
+  acc.w = fmaf(w, any ? v.w : 0.f, acc.w);
+}
+
+// The largest maximum of a row's parts; o, ml: this lane's part of the first 32.
+__device__ __forceinline__ float row_max(const AttendArgs& a, const PartList& l, int r, int lane, float2 ml) {
+  float M = ml.x;
+  for (int e = lane + 32; e < l.n; e += 32) {
+    float2 x;
+    l.at(a, e, r, x);
+    M = fmaxf(M, x.x);
   }
-  M = ptx::redux_max(M);
-  const float ref = M == -INFINITY ? 0.f : M;
-  float L = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int e0 = 0; e0 < n; e0 += 32) {
-    if (e0 > 0 && e0 + lane < n) {
-      float2 ml;
-      const int e = e0 + lane;
-      o0 = e < src[0].n ? part(a, src[0], e, ml) : part(a, src[1], e - src[0].n, ml);
-      M0 = ml.x;
-      l0 = ml.y;
-    }
-    const float w = e0 + lane < n ? ptx::ex2(M0 - ref) : 0.f;
-    L = fmaf(w, w > 0.f ? l0 : 0.f, L);
-    const int k1 = min(32, n - e0);
-#pragma unroll 8
-    for (int k = mine; k < k1; k += kWarps) {
-      const float wk = __shfl_sync(0xffffffffu, w, k);
-      const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o0, k));
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (wk > 0.f) v = *reinterpret_cast<const float4*>(ok + 4 * lane);  // (a part that saw no key is not written)
-      acc.x = fmaf(wk, v.x, acc.x);
-      acc.y = fmaf(wk, v.y, acc.y);
-      acc.z = fmaf(wk, v.z, acc.z);
-      acc.w = fmaf(wk, v.w, acc.w);
-    }
-  }
-  if constexpr (kWarps > 1) {
-    part_acc[warp][lane] = acc;
-    __syncthreads();
-    if (mine != 0) return;
-#pragma unroll
-    for (int k = 1; k < kWarps; ++k) {
-      const float4 v = part_acc[warp + k][lane];
-      acc.x += v.x;
-      acc.y += v.y;
-      acc.z += v.z;
-      acc.w += v.w;
-    }
-  }
+  return ptx::redux_max(M);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(const AttendArgs& a, int token, int hq, int lane, float4 acc, float M,
+                                          float L) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
   const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -160,6 +148,107 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const __gr
   store4(static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)hq * a.out_head + 4 * lane, acc);
   if (a.lse != nullptr && lane == 0)
     a.lse[(int64_t)token * a.h_q + hq] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+constexpr int kAhead = 8;  // sums whose loads are in flight
+
+// One warp a (token, KV head).
+template <typename T>
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_heads_kernel(const __grid_constant__ AttendArgs a) {
+  const int lane = threadIdx.x & 31;
+  const long long id = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
+  if (id >= (long long)a.tokens * a.h_kv) return;
+  const int token = (int)(id / a.h_kv), h = (int)(id - (long long)token * a.h_kv);
+  const PartList l = list_parts(a, token, h, lane);
+  float2 ml = make_float2(-INFINITY, 0.f), ml_next = ml;
+  const float *o = nullptr, *o_next = nullptr;
+  if (lane < l.n) o_next = l.at(a, lane, 0, ml_next);
+  for (int r = 0; r < a.g; ++r) {
+    ml = ml_next;
+    o = o_next;
+    if (lane < l.n && r + 1 < a.g) o_next = l.at(a, lane, r + 1, ml_next);
+    const float M = row_max(a, l, r, lane, ml), ref = M == -INFINITY ? 0.f : M;
+    float L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int e0 = 0; e0 < l.n; e0 += 32) {
+      if (e0 > 0) {
+        ml = make_float2(-INFINITY, 0.f);
+        if (e0 + lane < l.n) o = l.at(a, e0 + lane, r, ml);
+      }
+      const float w = ptx::ex2(ml.x - ref);
+      L = fmaf(w, w > 0.f ? ml.y : 0.f, L);
+      const int n = min(32, l.n - e0);
+      for (int k0 = 0; k0 < n; k0 += kAhead) {
+        float4 v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float* ok =
+              reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, (k0 + k) & 31));
+          v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k0 + k < n) v[k] = *reinterpret_cast<const float4*>(ok + 4 * lane);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) add_part(acc, k0 + k < n ? __shfl_sync(0xffffffffu, w, (k0 + k) & 31) : 0.f, v[k]);
+      }
+    }
+    store_row<T>(a, token, h * a.g + r, lane, acc, M, L);
+  }
+}
+
+// One CTA a row.
+template <typename T>
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_row_kernel(const __grid_constant__ AttendArgs a) {
+  __shared__ float4 sums[kJoinWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int token = blockIdx.x / a.h_q, hq = blockIdx.x - token * a.h_q, h = hq / a.g, r = hq - h * a.g;
+  const PartList l = list_parts(a, token, h, lane);
+  float2 ml = make_float2(-INFINITY, 0.f);
+  const float* o = nullptr;
+  if (lane < l.n) o = l.at(a, lane, r, ml);
+  float4 v[kAhead];  // this warp's sums of the first 32
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int e = k * kJoinWarps + warp;
+    const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, e & 31));
+    v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (e < min(l.n, 32)) v[k] = *reinterpret_cast<const float4*>(ok + 4 * lane);
+  }
+  const float M = row_max(a, l, r, lane, ml), ref = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int e0 = 0; e0 < l.n; e0 += 32) {
+    if (e0 > 0) {
+      ml = make_float2(-INFINITY, 0.f);
+      if (e0 + lane < l.n) o = l.at(a, e0 + lane, r, ml);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int e = k * kJoinWarps + warp;
+        const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, e & 31));
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (e0 + e < l.n && e < 32) v[k] = *reinterpret_cast<const float4*>(ok + 4 * lane);
+      }
+    }
+    const float w = ptx::ex2(ml.x - ref);
+    L = fmaf(w, w > 0.f ? ml.y : 0.f, L);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int e = k * kJoinWarps + warp;
+      const float wk = __shfl_sync(0xffffffffu, w, e & 31);
+      add_part(acc, e < 32 ? wk : 0.f, v[k]);
+    }
+  }
+  sums[warp][lane] = acc;
+  __syncthreads();
+  if (warp != 0) return;
+#pragma unroll
+  for (int k = 1; k < kJoinWarps; ++k) {
+    const float4 x = sums[k][lane];
+    acc.x += x.x;
+    acc.y += x.y;
+    acc.z += x.z;
+    acc.w += x.w;
+  }
+  store_row<T>(a, token, hq, lane, acc, M, L);
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
@@ -201,11 +290,9 @@ int attend_sms() {
 template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
-  // four warps a row while the rows are few (and so have many parts each)
-  const bool wide = rows <= 2048;
-  const unsigned grid = (unsigned)(wide ? rows : (rows + kJoinWarps - 1) / kJoinWarps);
-  if (wide) attend_join_kernel<T, kJoinWarps><<<grid, 32 * kJoinWarps, 0, st>>>(a);
-  else attend_join_kernel<T, 1><<<grid, 32 * kJoinWarps, 0, st>>>(a);
+  const long long heads = (long long)a.tokens * a.h_kv;
+  if (rows <= JOIN_ROWS) attend_join_row_kernel<T><<<(unsigned)rows, 32 * kJoinWarps, 0, st>>>(a);
+  else attend_join_heads_kernel<T><<<(unsigned)((heads + kJoinWarps - 1) / kJoinWarps), 32 * kJoinWarps, 0, st>>>(a);
   return cudaGetLastError();
 }
 
