@@ -6,9 +6,6 @@
 #include "attend.cuh"
 #include "ptx.cuh"
 
-#ifndef JOIN_ROWS
-#define JOIN_ROWS 2048
-#endif
 namespace ecokv {
 namespace {
 
@@ -155,6 +152,9 @@ constexpr int kAhead = 8;  // sums whose loads are in flight
 // One warp a (token, KV head).
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_heads_kernel(const __grid_constant__ AttendArgs a) {
+  // (the next call's first kernel is scheduled behind this one)
+  ptx::grid_trigger();
+  ptx::grid_wait();
   const int lane = threadIdx.x & 31;
   const long long id = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
   if (id >= (long long)a.tokens * a.h_kv) return;
@@ -199,6 +199,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_heads_kernel(cons
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_row_kernel(const __grid_constant__ AttendArgs a) {
   __shared__ float4 sums[kJoinWarps][32];
+  ptx::grid_trigger();
+  ptx::grid_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int token = blockIdx.x / a.h_q, hq = blockIdx.x - token * a.h_q, h = hq / a.g, r = hq - h * a.g;
   const PartList l = list_parts(a, token, h, lane);
@@ -291,9 +293,9 @@ template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
   const long long heads = (long long)a.tokens * a.h_kv;
-  if (rows <= JOIN_ROWS) attend_join_row_kernel<T><<<(unsigned)rows, 32 * kJoinWarps, 0, st>>>(a);
-  else attend_join_heads_kernel<T><<<(unsigned)((heads + kJoinWarps - 1) / kJoinWarps), 32 * kJoinWarps, 0, st>>>(a);
-  return cudaGetLastError();
+  if (rows <= 2048) return launch_behind(attend_join_row_kernel<T>, (unsigned)rows, 32 * kJoinWarps, 0, st, a);
+  return launch_behind(attend_join_heads_kernel<T>, (unsigned)((heads + kJoinWarps - 1) / kJoinWarps),
+                       32 * kJoinWarps, 0, st, a);
 }
 
 }  // namespace

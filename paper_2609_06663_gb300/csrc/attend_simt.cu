@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_c
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Smem& s = *reinterpret_cast<Smem*>(smem_raw);
   const int lane = threadIdx.x & 31;
+  ptx::grid_wait();
   Walk w;
   if (threadIdx.x < 32) w.begin(a, blockIdx.x, lane);
   while (true) {
@@ -205,6 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_c
     if (it.ntok * a.g <= 16) item_rows<T, 1>(a, s, it);
     else item_rows<T, 4>(a, s, it);
   }
+  ptx::grid_trigger();
 }
 
 template <typename T>
@@ -212,8 +214,7 @@ cudaError_t launch(const AttendArgs& a, cudaStream_t st) {
   const cudaError_t e =
       cudaFuncSetAttribute(attend_simt_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
   if (e != cudaSuccess) return e;
-  attend_simt_kernel<T><<<a.P, kThreads, sizeof(Smem), st>>>(a);
-  return cudaGetLastError();
+  return launch_behind(attend_simt_kernel<T>, (unsigned)a.P, kThreads, sizeof(Smem), st, a);
 }
 
 }  // namespace

@@ -397,8 +397,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_mbar_init();
   }
   if (warp == 0 && lane < 5) tma_prefetch_desc(&m.q + lane);
-  Walk w;
-  if (warp == 2) w.begin(a, blockIdx.x, lane);
   if (warp == 3) {
     tmem_alloc(&s.tmem, 512);
     tmem_relinquish();
@@ -406,6 +404,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // (what is above runs beside the end of the grid before)
+  grid_wait();
+  Walk w;
+  if (warp == 2) w.begin(a, blockIdx.x, lane);
   const uint32_t tmem = s.tmem;
   Issued d;
   // registers of the launch (3 x 168 a lane): 64 for the first warpgroup, 216 for a stream's
@@ -453,6 +455,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (d.ql > i) drain_bar(&s.qfull[i], ((d.ql - 1 - i) / 2) & 1);
   }
   __syncthreads();
+  // (triggered at the start, the joining kernel's launch took 2 us longer)
+  grid_trigger();
   if (warp == 3) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
@@ -511,8 +515,7 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     g_attr_set[dev].store(true);
   }
-  attend_tc_kernel<<<a.P, kThreads, smem, st>>>(m, a);
-  return cudaGetLastError();
+  return launch_behind(attend_tc_kernel, (unsigned)a.P, kThreads, (size_t)smem, st, m, a);
 }
 
 }  // namespace ecokv

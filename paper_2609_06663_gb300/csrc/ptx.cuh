@@ -290,6 +290,12 @@ __device__ __forceinline__ void reg_dealloc() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
+// ---------------------------------------------------------------- programmatic launch
+// Wait for the grids before this one in the stream (launched with the attribute
+// of programmatic serialisation); let the grid behind it be scheduled.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---------------------------------------------------------------- global sync
 __device__ __forceinline__ unsigned ld_acquire(const unsigned* p) {
   unsigned v;

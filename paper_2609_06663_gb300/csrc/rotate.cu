@@ -20,6 +20,7 @@
 #include <string.h>
 
 #include "attend.cuh"
+#include "ptx.cuh"
 
 namespace ecokv {
 namespace {
@@ -188,6 +189,9 @@ __device__ __forceinline__ Slot find_slot(const RotateArgs& a, int t, int lane) 
 
 template <typename T, bool kInter, bool kAppend>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant__ RotateArgs a) {
+  // (the next kernel's launch may go ahead; this one's has, until here)
+  ptx::grid_trigger();
+  ptx::grid_wait();
   const int lane = threadIdx.x & 31, c = threadIdx.x & (kGroup - 1);
   const long long unit = (long long)blockIdx.x * kGroups + threadIdx.x / kGroup;
   // whole warps stay: a warp's groups share shuffles; one past the end repeats the last unit without storing
@@ -309,10 +313,8 @@ cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
   const long long units = (long long)a.tokens * a.chunks;
   const unsigned grid = (unsigned)((units + kGroups - 1) / kGroups);
   if (a.r.rot_dim > 0 && a.r.layout == ECOKV_ROTARY_INTERLEAVED)
-    rotate_kernel<T, true, kAppend><<<grid, kThreads, 0, st>>>(a);
-  else
-    rotate_kernel<T, false, kAppend><<<grid, kThreads, 0, st>>>(a);
-  return cudaGetLastError();
+    return launch_behind(rotate_kernel<T, true, kAppend>, grid, kThreads, 0, st, a);
+  return launch_behind(rotate_kernel<T, false, kAppend>, grid, kThreads, 0, st, a);
 }
 
 // Heads a group takes: one while that still leaves SMs without a warp, then as
