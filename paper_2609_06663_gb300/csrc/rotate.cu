@@ -4,9 +4,12 @@
 // A row is 128 elements, held by eight lanes of sixteen.  Lane c holds the pairs
 // of frequencies 8c .. 8c + 7 in either layout: elements 8c.. and rot/2 + 8c.. (half)
 // or 16c .. 16c + 15 (interleaved), so that a rotation stays within a lane, its loads
-// are 16 bytes wide, and the norm's sum is three shuffles away.  A group of eight
-// lanes takes one token and some of its heads: the sines and cosines of a token
-// are formed once per group.
+// are 16 bytes wide, and the norm's sum is three shuffles away.  A warp takes a run
+// of rows in the order of tokens and heads, four at a time: its reads are whole
+// kilobytes side by side where heads are.  (With a run for each eight lanes 32768
+// tokens of 28 + 4 heads took 97 us.)  All runs are equally long and resident at
+// once.  The warp forms the sines and cosines of each token that it meets once,
+// two a lane, and hands them round.
 //
 // The angle.  position * inv_freq / 2 pi mod 1 is position * turns mod 2^64 with
 // turns = inv_freq / 2 pi in units of 2^-64: the product wraps as the angle does, so
@@ -27,7 +30,13 @@ namespace {
 
 constexpr int kGroup = 8;                // lanes a row
 constexpr int kThreads = 256;
-constexpr int kGroups = kThreads / kGroup;
+constexpr int kWarps = kThreads / 32;
+#ifndef MB
+#define MB 4
+#define KB 2
+#endif
+constexpr int kResident = MB;            // CTAs an SM
+constexpr int kBatch = KB;               // rows of bf16 whose loads a lane has in flight
 
 struct RowSet {
   const void* x;
@@ -41,8 +50,8 @@ struct RotateArgs {
   ecokv_rotary r;          // rot_dim 0: no rotation
   RowSet q, k, v;          // v: append only, copied
   const int32_t* positions;
-  int tokens, per;         // per: heads (of q, k and v together) a group takes
-  int chunks;              // ceil(heads / per)
+  int tokens;
+  int run;                 // rows (of q, k and v together) a warp takes
   float eps;
   // append
   ecokv_pages cache;
@@ -115,7 +124,7 @@ __device__ __forceinline__ void turn_row(Vec<T>& v0, Vec<T>& v1, const float (&c
     ss += s1;
 #pragma unroll
     for (int o = 1; o < kGroup; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float inv = 1.f / sqrtf(ss * (1.f / kD) + eps);
+    const float inv = rsqrtf(ss * (1.f / kD) + eps);
     float wa[8], wb[8];
     w0.get(wa);
     w1.get(wb);
@@ -148,125 +157,132 @@ __device__ __forceinline__ void turn_row(Vec<T>& v0, Vec<T>& v1, const float (&c
   v1.set(b);
 }
 
-// The sequence of token t and its slot's page and row; row -1: none.
+// The sequence of a warp's token, and the token's slot.
 struct Slot {
+  int b, start, n, len;  // sequence; its first token, tokens and slots
   int64_t page;
-  int row;
+  int row;               // -1: none
 };
-__device__ __forceinline__ Slot find_slot(const RotateArgs& a, int t, int lane) {
-  int b = t, i = 0, n = 1;
+__device__ __forceinline__ void load_sequence(const RotateArgs& a, Slot& s, int b) {
+  s.b = b;
+  s.start = b;
+  s.n = 1;
   if (a.starts != nullptr) {
-    // b = how many of starts[1 .. batch] are <= t: a warp's lanes read 32 of them
-    // at a time for its four tokens
-    const int g = lane >> 3;
+    s.start = a.starts[b];
+    s.n = a.starts[b + 1] - s.start;
+  }
+  s.len = a.cache.lengths[b];
+}
+// ... of the warp's first token t: as many of starts[1 .. batch] as are <= t come before it.
+__device__ __forceinline__ void first_sequence(const RotateArgs& a, Slot& s, int t, int lane) {
+  int b = t;
+  if (a.starts != nullptr) {
     b = 0;
-    for (int j0 = 0; j0 < a.batch; j0 += 32) {
-      const int s = j0 + lane < a.batch ? a.starts[1 + j0 + lane] : 0x7fffffff;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int n_le = __popc(__ballot_sync(0xffffffffu, s <= __shfl_sync(0xffffffffu, t, k * 8)));
-        if (k == g) b += n_le;
-      }
-    }
-    b = min(b, a.batch - 1);
-    const int s0 = a.starts[b];
-    i = t - s0;
-    n = a.starts[b + 1] - s0;
+    for (int j = lane; j < a.batch; j += 32) b += a.starts[1 + j] <= t ? 1 : 0;
+    b = min((int)__reduce_add_sync(0xffffffffu, (unsigned)b), a.batch - 1);
   }
-  const long long slot = (long long)a.cache.lengths[b] - n + i;
-  const long long col = slot >> a.page_shift;
-  int row = -1;
-  int64_t page = 0;
-  if (slot >= 0 && col < a.cache.table_stride && i >= 0 && i < n) {
-    page = a.cache.table[(int64_t)b * a.cache.table_stride + col];
-    if (page >= 0 && page < a.cache.n_pages) row = (int)(slot & (a.cache.page_size - 1));
+  load_sequence(a, s, b);
+}
+__device__ __forceinline__ void find_slot(const RotateArgs& a, Slot& s, int t) {
+  const int i = t - s.start;
+  const long long slot = (long long)s.len - s.n + i, col = slot >> a.page_shift;
+  s.row = -1;
+  s.page = 0;
+  if (slot >= 0 && col < a.cache.table_stride && i >= 0 && i < s.n) {
+    s.page = a.cache.table[(int64_t)s.b * a.cache.table_stride + col];
+    if (s.page >= 0 && s.page < a.cache.n_pages) s.row = (int)(slot & (a.cache.page_size - 1));
   }
-  if (row < 0 && a.status != nullptr) {
-    if (atomicCAS(a.status, 0u, (unsigned)ECOKV_ERR_DEVICE_INDEX) == 0u) a.status[1] = (unsigned)b;
+  if (s.row < 0 && a.status != nullptr) {
+    if (atomicCAS(a.status, 0u, (unsigned)ECOKV_ERR_DEVICE_INDEX) == 0u) a.status[1] = (unsigned)s.b;
   }
-  return {page, row};
 }
 
 template <typename T, bool kInter, bool kAppend>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant__ RotateArgs a) {
+__global__ void __launch_bounds__(kThreads, kResident) rotate_kernel(const __grid_constant__ RotateArgs a) {
   // (the next kernel's launch may go ahead; this one's has, until here)
   ptx::grid_trigger();
   ptx::grid_wait();
-  const int lane = threadIdx.x & 31, c = threadIdx.x & (kGroup - 1);
-  const long long unit = (long long)blockIdx.x * kGroups + threadIdx.x / kGroup;
-  // whole warps stay: a warp's groups share shuffles; one past the end repeats the last unit without storing
-  const long long last = (long long)a.tokens * a.chunks - 1;
-  const bool live = unit <= last;
-  const long long u = live ? unit : last;
-  const int t = (int)(u / a.chunks), r0 = (int)(u - (long long)t * a.chunks) * a.per;
+  const int lane = threadIdx.x & 31, c = lane & (kGroup - 1), g = lane / kGroup;
+  const int n_turn = a.q.heads + a.k.heads, n_all = n_turn + (kAppend ? a.v.heads : 0);
+  const long long total = (long long)a.tokens * n_all;
+  const long long first = ((long long)blockIdx.x * kWarps + threadIdx.x / 32) * a.run;
+  if (first >= total) return;
+  int left = (int)min((long long)a.run, total - first);
+  int t = (int)(first / n_all), r0 = (int)(first - (long long)t * n_all);
   const int F8 = a.r.rot_dim >> 4;  // lanes whose elements turn
   const bool turned = c < F8;
   // this lane's two eights of elements
   const int e0 = !kInter && turned ? 8 * c : 16 * c;
   const int e1 = !kInter && turned ? 8 * c + 8 * F8 : 16 * c + 8;
-  Slot at{0, -1};
-  if constexpr (kAppend) at = find_slot(a, t, lane);
-  float cs[8], sn[8];
-  const int n_turn = a.q.heads + a.k.heads;
-  if (turned && r0 < n_turn) {
-    uint64_t pos[ECOKV_ROTARY_AXES];
-#pragma unroll
-    for (int x = 0; x < ECOKV_ROTARY_AXES; ++x)
-      pos[x] = x < a.r.axes ? (uint64_t)(int64_t)a.positions[(int64_t)x * a.tokens + t] : 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int f = 8 * c + i, ax = a.r.axis[f];
-      const uint64_t p = ax == 0 ? pos[0] : ax == 1 ? pos[1] : ax == 2 ? pos[2] : pos[3];
-      // the upper 32 bits as a signed fraction of a turn: -1/2 .. 1/2, in half turns
-      const int32_t ph = (int32_t)((p * a.r.turns[f] + 0x80000000ull) >> 32);
-      float s_, c_;
-      sincospif((float)ph * 4.656612873077393e-10f, &s_, &c_);
-      cs[i] = c_ * a.r.magnitude;
-      sn[i] = s_ * a.r.magnitude;
-    }
-  }
-  const int n_all = n_turn + (kAppend ? a.v.heads : 0);
-  const int r1 = min(r0 + a.per, n_all);
+  Slot at{};
+  at.row = -1;
+  if constexpr (kAppend) first_sequence(a, at, t, lane);
 #pragma unroll 1
-  for (int seg = 0; seg < (kAppend ? 3 : 2); ++seg) {
-    const RowSet& s = seg == 0 ? a.q : seg == 1 ? a.k : a.v;
-    const int base = seg == 0 ? 0 : seg == 1 ? a.q.heads : n_turn;
-    const int lo = max(r0, base) - base, hi = min(r1, base + s.heads) - base;
-    // (the groups of a warp differ in their rows: the loop runs as long as the longest of them)
-    const int steps = (int)__reduce_max_sync(0xffffffffu, (unsigned)max(hi - lo, 0));
-    if (steps == 0) continue;
-    const bool norm = s.norm != nullptr;
-    Vec<T> w0{}, w1{};
-    if (norm) {
-      w0.load(static_cast<const T*>(s.norm) + e0);
-      w1.load(static_cast<const T*>(s.norm) + e1);
+  for (; left > 0; ++t, r0 = 0) {
+    if constexpr (kAppend) {
+      while (t >= at.start + at.n && at.b + 1 < a.batch) load_sequence(a, at, at.b + 1);
+      find_slot(a, at, t);
     }
-    const T* x = static_cast<const T*>(s.x) + (int64_t)t * s.x_token;
-    T* y = static_cast<T*>(s.y) + (int64_t)t * s.y_token;
-    int64_t y_head = s.y_head;
-    bool store = live;
-    if (kAppend && seg > 0) {
-      y = static_cast<T*>(seg == 1 ? a.cache.k : a.cache.v) + at.page * a.cache.page_stride +
-          (int64_t)at.row * a.cache.slot_stride;
-      y_head = a.cache.head_stride;
-      store = live && at.row >= 0;
+    const int r1 = min(r0 + left, n_all);
+    left -= r1 - r0;
+    float cs[8], sn[8];
+    if (r0 < n_turn && F8 > 0) {
+      float s2[2], c2[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int f = turned ? 8 * c + 2 * g + i : 0;
+        const uint64_t p = (uint64_t)(int64_t)a.positions[(int64_t)a.r.axis[f] * a.tokens + t];
+        // the upper 32 bits as a signed fraction of a turn: -1/2 .. 1/2, in half turns
+        const int32_t ph = (int32_t)((p * a.r.turns[f] + 0x80000000ull) >> 32);
+        sincospif((float)ph * 4.656612873077393e-10f, &s2[i], &c2[i]);
+        s2[i] *= a.r.magnitude;
+        c2[i] *= a.r.magnitude;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        cs[i] = __shfl_sync(0xffffffffu, c2[i & 1], (i >> 1) * kGroup + c);
+        sn[i] = __shfl_sync(0xffffffffu, s2[i & 1], (i >> 1) * kGroup + c);
+      }
     }
-    constexpr int kB = sizeof(T) == 2 ? 4 : 2;  // rows whose loads are in flight together
 #pragma unroll 1
-    for (int j = 0; j < steps; j += kB) {
-      Vec<T> v0[kB], v1[kB];
+    for (int seg = 0; seg < (kAppend ? 3 : 2); ++seg) {
+      const RowSet& s = seg == 0 ? a.q : seg == 1 ? a.k : a.v;
+      const int base = seg == 0 ? 0 : seg == 1 ? a.q.heads : n_turn;
+      const int lo = max(r0, base) - base, hi = min(r1, base + s.heads) - base;
+      if (lo >= hi) continue;
+      const bool norm = s.norm != nullptr;
+      Vec<T> w0{}, w1{};
+      if (norm) {
+        w0.load(static_cast<const T*>(s.norm) + e0);
+        w1.load(static_cast<const T*>(s.norm) + e1);
+      }
+      const T* x = static_cast<const T*>(s.x) + (int64_t)t * s.x_token;
+      T* y = static_cast<T*>(s.y) + (int64_t)t * s.y_token;
+      int64_t y_head = s.y_head;
+      bool store = true;
+      if (kAppend && seg > 0) {
+        y = static_cast<T*>(seg == 1 ? a.cache.k : a.cache.v) + at.page * a.cache.page_stride +
+            (int64_t)at.row * a.cache.slot_stride;
+        y_head = a.cache.head_stride;
+        store = at.row >= 0;
+      }
+      constexpr int kB = sizeof(T) == 2 ? kBatch : (kBatch + 1) / 2;  // rows whose loads are in flight together
+#pragma unroll 1
+      for (int j = lo + g; j < hi + g; j += 4 * kB) {
+        Vec<T> v0[kB], v1[kB];
 #pragma unroll
-      for (int k = 0; k < kB; ++k)
-        if (lo + j + k < hi) {
-          v0[k].load(x + (int64_t)(lo + j + k) * s.x_head + e0);
-          v1[k].load(x + (int64_t)(lo + j + k) * s.x_head + e1);
-        }
+        for (int k = 0; k < kB; ++k)
+          if (j + 4 * k < hi) {
+            v0[k].load(x + (j + 4 * k) * s.x_head + e0);
+            v1[k].load(x + (j + 4 * k) * s.x_head + e1);
+          }
 #pragma unroll
-      for (int k = 0; k < kB; ++k) {
-        if (!kAppend || seg < 2) turn_row<T, kInter>(v0[k], v1[k], cs, sn, turned, norm, w0, w1, a.eps);
-        if (store && lo + j + k < hi) {
-          v0[k].store(y + (int64_t)(lo + j + k) * y_head + e0);
-          v1[k].store(y + (int64_t)(lo + j + k) * y_head + e1);
+        for (int k = 0; k < kB; ++k) {
+          if (!kAppend || seg < 2) turn_row<T, kInter>(v0[k], v1[k], cs, sn, turned, norm, w0, w1, a.eps);
+          if (store && j + 4 * k < hi) {
+            v0[k].store(y + (j + 4 * k) * y_head + e0);
+            v1[k].store(y + (j + 4 * k) * y_head + e1);
+          }
         }
       }
     }
@@ -310,21 +326,20 @@ RowSet row_set(const ecokv_rows* s) {
 
 template <typename T, bool kAppend>
 cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
-  const long long units = (long long)a.tokens * a.chunks;
-  const unsigned grid = (unsigned)((units + kGroups - 1) / kGroups);
+  const long long rows = (long long)a.tokens * (a.q.heads + a.k.heads + a.v.heads);
+  const long long warps = (rows + a.run - 1) / a.run;
+  const unsigned grid = (unsigned)((warps + kWarps - 1) / kWarps);
   if (a.r.rot_dim > 0 && a.r.layout == ECOKV_ROTARY_INTERLEAVED)
     return launch_behind(rotate_kernel<T, true, kAppend>, grid, kThreads, 0, st, a);
   return launch_behind(rotate_kernel<T, false, kAppend>, grid, kThreads, 0, st, a);
 }
 
-// Heads a group takes: one while that still leaves SMs without a warp, then as
-// many as keep every SM at its resident groups, so that a token's sines are
-// formed for as many rows as possible.
-void set_split(RotateArgs& a, int heads) {
-  const long long rows = (long long)a.tokens * heads;
-  const long long per = rows / (152ll * kGroups * 6);
-  a.per = (int)(per < 1 ? 1 : per > heads ? heads : per);
-  a.chunks = (heads + a.per - 1) / a.per;
+// Rows a warp takes: as many as leave every warp resident (152 SMs), so that the last
+// of them ends with the others, and four at least.
+void set_run(RotateArgs& a, int heads) {
+  const long long rows = (long long)a.tokens * heads, warps = 152ll * kResident * kWarps;
+  const long long run = (rows + warps - 1) / warps;
+  a.run = (int)(run > 4 ? run : 4);
 }
 
 ecokv_status common(RotateArgs& a, const ecokv_rotary* r, const int32_t* positions, int32_t tokens, float eps) {
@@ -339,7 +354,7 @@ ecokv_status common(RotateArgs& a, const ecokv_rotary* r, const int32_t* positio
   return ECOKV_OK;
 }
 
-bool too_many(int32_t tokens, long long heads) { return (long long)tokens * heads > (1ll << 31) * (kGroups / 2); }
+bool too_many(int32_t tokens, long long heads) { return (long long)tokens * heads > 1ll << 40; }
 
 }  // namespace
 }  // namespace ecokv
@@ -428,7 +443,7 @@ ecokv_status ecokv_rotate(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_
   const int heads = a.q.heads + a.k.heads;
   if (too_many(tokens, heads)) return ECOKV_ERR_UNSUPPORTED;
   if (tokens == 0 || heads == 0) return ECOKV_OK;
-  set_split(a, heads);
+  set_run(a, heads);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t err = dtype == ECOKV_F32 ? launch<float, false>(a, s) : launch<__nv_bfloat16, false>(a, s);
   return err == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
@@ -461,7 +476,7 @@ ecokv_status ecokv_append(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_
   a.batch = batch;
   a.page_shift = __builtin_ctz((unsigned)cache->page_size);
   a.status = static_cast<unsigned*>(ws);
-  set_split(a, heads);
+  set_run(a, heads);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t err = dtype == ECOKV_F32 ? launch<float, true>(a, s) : launch<__nv_bfloat16, true>(a, s);
   return err == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
