@@ -13,7 +13,8 @@ namespace {
 // 2^(their maximum - the largest).  What bounds this is the latency of its chain of
 // loads.  With few rows a CTA takes one, its warps a share of the parts each, and the
 // sums are loaded beside the weights that may turn out to be zero; with many rows
-// a warp takes the rows of one token and KV head, whose parts lie side by side.
+// a warp takes rows of one token and KV head, whose parts lie side by side and are
+// looked up once.
 // Each lane has four columns.
 constexpr int kJoinWarps = 4;
 
@@ -149,24 +150,27 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, int token, int hq
 
 constexpr int kAhead = 8;  // sums whose loads are in flight
 
-// One warp a (token, KV head).
+// One warp `per` rows of a (token, KV head).
 template <typename T>
-__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_heads_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps)
+    attend_join_heads_kernel(const __grid_constant__ AttendArgs a, int per, int split) {
   // (the next call's first kernel is scheduled behind this one)
   ptx::grid_trigger();
   ptx::grid_wait();
   const int lane = threadIdx.x & 31;
   const long long id = (long long)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
-  if (id >= (long long)a.tokens * a.h_kv) return;
-  const int token = (int)(id / a.h_kv), h = (int)(id - (long long)token * a.h_kv);
+  if (id >= (long long)a.tokens * a.h_kv * split) return;
+  const long long unit = id / split;
+  const int token = (int)(unit / a.h_kv), h = (int)(unit - (long long)token * a.h_kv);
+  const int r0 = (int)(id - unit * split) * per, r1 = min(r0 + per, a.g);
   const PartList l = list_parts(a, token, h, lane);
   float2 ml = make_float2(-INFINITY, 0.f), ml_next = ml;
   const float *o = nullptr, *o_next = nullptr;
-  if (lane < l.n) o_next = l.at(a, lane, 0, ml_next);
-  for (int r = 0; r < a.g; ++r) {
+  if (lane < l.n) o_next = l.at(a, lane, r0, ml_next);
+  for (int r = r0; r < r1; ++r) {
     ml = ml_next;
     o = o_next;
-    if (lane < l.n && r + 1 < a.g) o_next = l.at(a, lane, r + 1, ml_next);
+    if (lane < l.n && r + 1 < r1) o_next = l.at(a, lane, r + 1, ml_next);
     const float M = row_max(a, l, r, lane, ml), ref = M == -INFINITY ? 0.f : M;
     float L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -292,10 +296,15 @@ int attend_sms() {
 template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
-  const long long heads = (long long)a.tokens * a.h_kv;
-  if (rows <= 2048) return launch_behind(attend_join_row_kernel<T>, (unsigned)rows, 32 * kJoinWarps, 0, st, a);
-  return launch_behind(attend_join_heads_kernel<T>, (unsigned)((heads + kJoinWarps - 1) / kJoinWarps),
-                       32 * kJoinWarps, 0, st, a);
+  // one CTA a row while all of them are resident (152 SMs of 8; 1792 rows, the whole
+  // call: 63.9 us so, 61.1 by warps), past that as many rows a warp as leave 10 warps
+  // an SM (3700 rows: 20.5 us at 20 warps, 18.4 at 10; 20600: 121.7 and 121.8, 128 at 100)
+  if (rows <= 152 * 8) return launch_behind(attend_join_row_kernel<T>, (unsigned)rows, 32 * kJoinWarps, 0, st, a);
+  const long long want = rows / (152 * 10);
+  const int per = (int)(want < 1 ? 1 : want > a.g ? a.g : want), split = div_up(a.g, per);
+  const long long warps = (long long)a.tokens * a.h_kv * split;
+  return launch_behind(attend_join_heads_kernel<T>, (unsigned)((warps + kJoinWarps - 1) / kJoinWarps),
+                       32 * kJoinWarps, 0, st, a, per, split);
 }
 
 }  // namespace
