@@ -3,6 +3,8 @@
 
 #include <math.h>
 
+#include <atomic>
+
 #include "attend.cuh"
 #include "ptx.cuh"
 
@@ -285,11 +287,16 @@ bool sizes_ok(int32_t tokens, int32_t batch, int32_t h_q, int32_t h_kv) {
   return tokens >= 0 && batch >= 1 && h_q >= 1 && h_kv >= 1 && h_q % h_kv == 0 && h_q <= (1 << 16);
 }
 
+// CTAs of the attention kernels: the current device's SMs (cached per device; a
+// racing thread repeats the query).
 int attend_sms() {
+  static std::atomic<int> cached[64];
   int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
-    n = 152;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 152;
+  if ((n = cached[dev].load()) == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 152;
+    cached[dev].store(n);
+  }
   return n < kMaxAttendSms ? n : kMaxAttendSms;
 }
 

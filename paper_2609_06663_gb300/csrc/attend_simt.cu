@@ -20,6 +20,8 @@
 
 #include <math.h>
 
+#include <atomic>
+
 #include "attend.cuh"
 #include "ptx.cuh"
 
@@ -369,9 +371,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_c
 
 template <typename T>
 cudaError_t launch(const AttendArgs& a, cudaStream_t st) {
-  const cudaError_t e =
-      cudaFuncSetAttribute(attend_simt_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+  static std::atomic<bool> set[64];  // a racing thread repeats the idempotent setting
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (!set[dev].load()) {
+    e = cudaFuncSetAttribute(attend_simt_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+    if (e != cudaSuccess) return e;
+    set[dev].store(true);
+  }
   return launch_behind(attend_simt_kernel<T>, (unsigned)a.P, kThreads, sizeof(Smem), st, a);
 }
 

@@ -471,13 +471,19 @@ def rotary(rot_dim=HEAD_DIM, base=10000.0, layout="half", scaling="none", factor
 
 def _dtype(t, *others) -> int:
     """Their common dtype's code; all of them on one CUDA device."""
-    code, dt, dev = dtype_code(t), t.dtype, t.get_device()
+    dt, dev = t.dtype, t.get_device()
     if dev < 0:
         raise ValueError("CUDA tensors are wanted")
     for x in others:
         if x is not None and (x.dtype is not dt or x.get_device() != dev):
             raise TypeError(f"{x.dtype} on {x.device} next to {dt} on {t.device}")
+    code = _codes.get(dt)
+    if code is None:
+        code = _codes[dt] = dtype_code(t)
     return code
+
+
+_codes = {}  # torch dtype -> code
 
 
 def _ints(x, shape, what):
@@ -499,31 +505,39 @@ def _heads(x, what):
     n, s = x.shape, x.stride()
     if len(n) != 3 or n[2] != HEAD_DIM or s[2] != 1:
         raise ValueError(f"{what}: rows [tokens, heads, {HEAD_DIM}] with the last axis contiguous are wanted")
+    tokens, heads, _ = n
     # (a stride that is never taken counts as a row)
-    return n[0], n[1], s[0] if n[0] > 1 else HEAD_DIM, s[1] if n[1] > 1 else HEAD_DIM
+    return tokens, heads, s[0] if tokens > 1 else HEAD_DIM, s[1] if heads > 1 else HEAD_DIM
 
 
 def _rows(x, y, norm, what):
     tokens, heads, st, sh = _heads(x, what)
-    at = yt = yh = w = None
-    if y is not None:
-        ty, hy, yt, yh = _heads(y, what)
-        if ty != tokens or hy != heads:
-            raise ValueError(f"{what}: the output has another shape")
-        at = y.data_ptr()
     if norm is not None:
-        if norm.shape != (HEAD_DIM,) or norm.stride(0) != 1:
-            raise ValueError(f"{what}: norm weights [{HEAD_DIM}] are wanted")
-        w = norm.data_ptr()
-    return ecokv_rows(x.data_ptr(), at, st, sh, yt or 0, yh or 0, w, heads)
+        if norm.numel() != HEAD_DIM or not norm.is_contiguous():
+            raise ValueError(f"{what}: contiguous norm weights [{HEAD_DIM}] are wanted")
+        norm = norm.data_ptr()
+    if y is None:
+        return ecokv_rows(x.data_ptr(), None, st, sh, 0, 0, norm, heads)
+    if y is x:
+        return ecokv_rows(x.data_ptr(), x.data_ptr(), st, sh, st, sh, norm, heads)
+    ty, hy, yt, yh = _heads(y, what)
+    if ty != tokens or hy != heads:
+        raise ValueError(f"{what}: the output has another shape")
+    return ecokv_rows(x.data_ptr(), y.data_ptr(), st, sh, yt, yh, norm, heads)
+
+
+_raw_stream = None
 
 
 def _on(stream, t, *made):
     """The raw stream to launch on; tensors made here are kept from reuse until it is done with them."""
     if stream is None:
-        import torch
-        # (torch.cuda.current_stream builds an object: 2 us of a call of 8)
-        return torch._C._cuda_getCurrentRawStream(t.get_device())
+        global _raw_stream
+        if _raw_stream is None:
+            import torch
+            # (torch.cuda.current_stream builds an object: 2 us of a call of 8)
+            _raw_stream = torch._C._cuda_getCurrentRawStream
+        return _raw_stream(t.get_device())
     if isinstance(stream, int):
         return stream
     for x in made:
@@ -538,20 +552,19 @@ def rotate(rot, positions, q, k=None, q_norm=None, k_norm=None, eps=1e-6, q_out=
     positions int32 [axes, tokens] (or [tokens]).  Outputs may have any strides
     (k_out a view of the [heads, tokens, 128] that the eviction pass reads) or be
     the inputs.  Returns (q_out, k_out)."""
-    import torch
     made = []
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = q.new_empty(q.shape)
         made.append(q_out)
     if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = k.new_empty(k.shape)
         made.append(k_out)
     dt = _dtype(q, k, q_norm, k_norm, q_out, k_out)
     tokens = q.shape[0]
     if k is not None and k.shape[0] != tokens:
         raise ValueError("q and k have different numbers of tokens")
     pos = _positions(rot, positions, tokens)
-    _check(lib().ecokv_rotate(rot, dt, _rows(q, q_out, q_norm, "q"),
+    _check((_lib or lib()).ecokv_rotate(rot, dt, _rows(q, q_out, q_norm, "q"),
                               None if k is None else _rows(k, k_out, k_norm, "k"), pos, tokens, eps,
                               _on(stream, q, *made)), "ecokv_rotate")
     return q_out, k_out
@@ -613,15 +626,14 @@ def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm
     cache's slots, q (normed, rotated) to q_out, which is returned.  starts int32
     [batch + 1]: None = one token a sequence.  ws: a workspace whose status word
     takes device-side errors."""
-    import torch
     made = None
     if q is not None and q_out is None:
-        made = q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        made = q_out = q.new_empty(q.shape)
     dt = _dtype(k, v, cache.k_pages, q, q_norm, k_norm, q_out)
     tokens = k.shape[0]
     if v.shape != k.shape or k.shape[1] != cache.h_kv or (q is not None and q.shape[0] != tokens):
         raise ValueError("k, v and q do not fit together or the cache")
-    _check(lib().ecokv_append(rotary, dt, None if q is None else _rows(q, q_out, q_norm, "q"),
+    _check((_lib or lib()).ecokv_append(rotary, dt, None if q is None else _rows(q, q_out, q_norm, "q"),
                               _rows(k, None, k_norm, "k"), _rows(v, None, None, "v"), cache.c,
                               _positions(rotary, positions, tokens), _ints(starts, (cache.batch + 1,), "starts"), tokens,
                               cache.batch, eps, _ptr(ws), 0 if ws is None else ws.numel(), _on(stream, k, made)),
@@ -642,10 +654,9 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
     """Run ecokv_attend: q [tokens, h_q, 128] over prefix (a Prefix or None) and
     cache (a PagedCache or None); returns out [tokens, h_q, 128].  starts int32
     [batch + 1]: None = one token a sequence.  lse: float32 [tokens, h_q] to fill."""
-    import torch
     made = []
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
         made.append(out)
     if prefix is None and cache is None:
         raise ValueError("a prefix or a cache is wanted")
@@ -656,14 +667,14 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
     if to != tokens or ho != h_q or (prefix is not None and prefix.h_kv != h_kv):
         raise ValueError("out or the prefix does not fit")
     batch = 1 if cache is None else cache.batch
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (tokens, h_q) or
+    if lse is not None and (str(lse.dtype) != "torch.float32" or tuple(lse.shape) != (tokens, h_q) or
                             not lse.is_contiguous() or not lse.is_cuda):
         raise ValueError("lse: a contiguous float32 [tokens, h_q] CUDA tensor is wanted")
     if ws is None:
         ws = alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device)
         made.append(ws)
     p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, qt, qh, ot, oh, flags, timeout_us)
-    _check(lib().ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
+    _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
                               None if cache is None else cache.c,
                               None if cache is None else _ints(starts, (batch + 1,), "starts"), out.data_ptr(),
                               _ptr(lse), ws.data_ptr(), ws.numel(), _on(stream, q, *made)), "ecokv_attend")
