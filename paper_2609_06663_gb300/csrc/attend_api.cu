@@ -358,6 +358,7 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   const bool tc = dtype == ECOKV_BF16 && (p->flags & ECOKV_FLAG_FORCE_SIMT) == 0u;
   if ((p->flags & ECOKV_FLAG_TEST_STALL) != 0u && !tc) return ECOKV_ERR_UNSUPPORTED;  // the waits are on that path
   if (p->d != kD || p->h_q / p->h_kv > kMaxGroup) return ECOKV_ERR_UNSUPPORTED;
+  if (p->tokens == 0) return ECOKV_OK;  // (tensors of no rows may have no address)
   if (!q || !out || !aligned16(q) || !aligned16(out) || ((uintptr_t)lse & 3u)) return ECOKV_ERR_INVALID_ARG;
   if (p->q_token < 0 || p->q_head < 0 || p->out_token < 0 || p->out_head < 0 || !stride_ok(p->q_token, e) ||
       !stride_ok(p->q_head, e) || !stride_ok(p->out_token, e) || !stride_ok(p->out_head, e))
@@ -383,7 +384,6 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   }
   if (ws == nullptr || !aligned16(ws) || ws_bytes < attend_layout(p->tokens, p->batch, p->h_q, p->h_kv, 2).total)
     return ECOKV_ERR_WORKSPACE;
-  if (p->tokens == 0) return ECOKV_OK;
   a.q = q;
   a.out = out;
   a.lse = lse;

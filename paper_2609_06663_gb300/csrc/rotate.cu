@@ -504,6 +504,7 @@ ecokv_status ecokv_rotary_sections(ecokv_rotary* r, const int32_t* counts, int32
 ecokv_status ecokv_rotate(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_rows* q, const ecokv_rows* k,
                           const int32_t* positions, int32_t tokens, float eps, void* stream) {
   if (dtype != ECOKV_F32 && dtype != ECOKV_BF16) return ECOKV_ERR_INVALID_ARG;
+  if (tokens == 0) return ECOKV_OK;  // (tensors of no rows may have no address)
   const size_t e = dtype == ECOKV_F32 ? 4 : 2;
   if (!rows_ok(q, e, true) || !rows_ok(k, e, true)) return ECOKV_ERR_INVALID_ARG;
   RotateArgs a{};
@@ -513,7 +514,7 @@ ecokv_status ecokv_rotate(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_
   a.k = row_set(k);
   const int heads = a.q.heads + a.k.heads;
   if (too_many(tokens, heads)) return ECOKV_ERR_UNSUPPORTED;
-  if (tokens == 0 || heads == 0) return ECOKV_OK;
+  if (heads == 0) return ECOKV_OK;
   set_run(a, heads);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t err = dtype == ECOKV_F32 ? launch<float, false>(a, s) : launch<__nv_bfloat16, false>(a, s);
@@ -525,6 +526,7 @@ ecokv_status ecokv_append(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_
                           const int32_t* starts, int32_t tokens, int32_t batch, float eps, void* ws,
                           size_t ws_bytes, void* stream) {
   if (dtype != ECOKV_F32 && dtype != ECOKV_BF16) return ECOKV_ERR_INVALID_ARG;
+  if (tokens == 0) return ECOKV_OK;
   const size_t e = dtype == ECOKV_F32 ? 4 : 2;
   if (k == nullptr || v == nullptr || !rows_ok(q, e, true) || !rows_ok(k, e, false) || !rows_ok(v, e, false))
     return ECOKV_ERR_INVALID_ARG;
@@ -541,7 +543,6 @@ ecokv_status ecokv_append(const ecokv_rotary* r, ecokv_dtype dtype, const ecokv_
   a.v = row_set(v);
   const int heads = a.q.heads + a.k.heads + a.v.heads;
   if (too_many(tokens, heads)) return ECOKV_ERR_UNSUPPORTED;
-  if (tokens == 0) return ECOKV_OK;
   a.cache = *cache;
   a.starts = starts;
   a.batch = batch;

@@ -428,3 +428,72 @@ def test_attend_waits_that_run_out():
     with pytest.raises(E.EcokvError) as e:
         E.attend(q, pre, b.cache, flags=E.ECOKV_FLAG_TEST_STALL | E.ECOKV_FLAG_FORCE_SIMT)
     assert e.value.code == E.ECOKV_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("seed", range(6))
+def test_attend_random_batches(seed, dt):
+    """Batches of up to 70 sequences with and without tokens, slots and prefix rows, any group, page size and order."""
+    import random
+    r = random.Random(seed)
+    h_kv, group = r.choice([1, 2, 3]), r.choice([1, 2, 5, 7, 16, 33])
+    one = r.random() < 0.4
+    n = r.choice([1, 5, 31, 32, 33, 70])
+    new = [1 if one else r.choice([0, 1, 1, 2, r.randint(0, 40)]) for _ in range(n)]
+    if sum(new) == 0:
+        new[-1] = 3
+    lens = [max(0, x + r.choice([-1, 0, 0, 1, 17, r.randint(0, 300)])) for x in new]
+    uneven = r.random() < 0.5
+    rows = [r.randint(0, 400) for _ in range(h_kv)] if uneven else [r.choice([0, 1, 64, 300])] * h_kv
+    b = Batch(seed, h_kv, new, lens, r.choice([8, 16, 64, 256]), dt, r.choice(["head", "slot"]))
+    heads, pre = make_prefix(gen(seed), rows, dt, uneven)
+    check_attend(b, heads, pre if sum(rows) else None, h_kv * group, dt)
+
+
+def test_attend_layouts():
+    """Queries and outputs by head, K and V side by side in one tensor: the same bits as in their usual order."""
+    b = Batch(17, 4, [2, 1, 3], [70, 1, 200], 16, "bf16")
+    heads, pre = make_prefix(gen(3), [150] * 4, "bf16", False)
+    q = torch.randn(6, 8, D, generator=gen(2)).bfloat16()
+    want = check_attend(b, heads, pre, 8, "bf16", q=q)
+    both = torch.stack([b.dk, b.dv], 1)          # [pages, 2, heads, slots, d]
+    cache = E.PagedCache(both[:, 0], both[:, 1], b.cache.table, b.cache.lengths)
+    pkv = torch.stack([pre.k, pre.v], 2)         # [heads, rows, 2, d]
+    by_head = q.transpose(0, 1).contiguous().cuda().transpose(0, 1)
+    out = torch.zeros(8, 6, D, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    got = E.attend(by_head, E.Prefix(pkv[:, :, 0], pkv[:, :, 1]), cache, b.starts.cuda(), out=out)
+    assert got is out and torch.equal(out, want)
+    # appended through the other layout
+    k, v = torch.randn(2, 6, 4, D, generator=gen(5)).bfloat16().cuda()
+    E.append(cache, k, v, b.starts.cuda())
+    E.append(b.cache, k, v, b.starts.cuda())
+    assert torch.equal(both[:, 0].nan_to_num(), b.dk.nan_to_num()) and torch.equal(both[:, 1].nan_to_num(), b.dv.nan_to_num())
+
+
+def test_calls_on_two_streams_with_workspaces_of_their_own():
+    b = Batch(19, 4, [1] * 9, [50 * i + 1 for i in range(9)], 16, "bf16")
+    _, pre = make_prefix(gen(3), [900] * 4, "bf16", False)
+    q = [torch.randn(9, 28, D, generator=gen(i)).bfloat16().cuda() for i in range(2)]
+    want = [E.attend(x, pre, b.cache) for x in q]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    ws = [E.alloc_attend_workspace(9, 9, 28, 4, torch.bfloat16) for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i in range(2):
+            got[i].append(E.attend(q[i], pre, b.cache, ws=ws[i], stream=streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i]) and E.ecokv_device_status(ws[i]) == 0
+
+
+def test_nothing_to_do():
+    b = Batch(1, 2, [1, 1], [4, 5], 8, "bf16")
+    empty = torch.zeros(0, 4, D, dtype=torch.bfloat16, device="cuda")
+    starts = torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert E.attend(empty, None, b.cache, starts).shape == (0, 4, D)
+    before = b.dk.clone()
+    assert E.append(b.cache, empty[:, :2], empty[:, :2], starts) is None
+    assert E.rotate(E.rotary(), torch.zeros(1, 0, dtype=torch.int32, device="cuda"), empty)[0].shape == (0, 4, D)
+    assert torch.equal(before.nan_to_num(), b.dk.nan_to_num())
