@@ -184,17 +184,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
       const float w = ptx::ex2(ml.x - ref);
       L = fmaf(w, w > 0.f ? ml.y : 0.f, L);
       const int n = min(32, l.n - e0);
-      for (int k0 = 0; k0 < n; k0 += kAhead) {
-        float4 v[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const float* ok =
-              reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, (k0 + k) & 31));
-          v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (k0 + k < n) v[k] = *reinterpret_cast<const float4*>(ok + 4 * lane);
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) add_part(acc, k0 + k < n ? __shfl_sync(0xffffffffu, w, (k0 + k) & 31) : 0.f, v[k]);
+      for (int k = 0; k < n; ++k) {
+        const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, k));
+        add_part(acc, __shfl_sync(0xffffffffu, w, k), *reinterpret_cast<const float4*>(ok + 4 * lane));
       }
     }
     store_row<T>(a, token, h * a.g + r, lane, acc, M, L);
