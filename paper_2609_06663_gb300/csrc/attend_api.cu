@@ -6,7 +6,7 @@
 #include <atomic>
 
 #include "attend.cuh"
-#include "ptx.cuh"
+#include "decode_ptx.cuh"
 
 namespace ecokv {
 namespace {

@@ -18,8 +18,7 @@
 #include <atomic>
 
 #include "attend.cuh"
-#include "ptx.cuh"
-#include "tc_pass.cuh"
+#include "decode_ptx.cuh"
 #include "tc_tile.cuh"
 
 namespace ecokv {
@@ -473,17 +472,42 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 std::atomic<bool> g_attr_set[64];
 
-// Rows [.., rows, outer ..] of 128 bf16, in boxes of 64 columns with the 128-byte swizzle.
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+  static std::atomic<EncodeTiledFn> fn{nullptr};  // a racing thread repeats the lookup
+  EncodeTiledFn f = fn.load();
+  if (f == nullptr) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess) {
+      f = reinterpret_cast<EncodeTiledFn>(p);
+      fn.store(f);
+    }
+  }
+  return f;
+}
+
+// A tensor of bf16 rows of 128, the axes after the first `strides` elements apart, in
+// boxes of 64 columns with the 128-byte swizzle.
 bool map_of(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const int64_t* strides,
             const uint32_t* box) {
-  cuuint64_t d[5], st[4];
-  cuuint32_t b[5];
+  const EncodeTiledFn enc = encode_fn();
+  cuuint64_t d[4], st[3];
+  cuuint32_t b[4];
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
   for (int i = 0; i < rank; ++i) {
     d[i] = dims[i];
     b[i] = box[i];
     if (i > 0) st[i - 1] = (cuuint64_t)strides[i - 1] * 2;
   }
-  return tensor_map_bf16(m, base, rank, d, st, b);
+  return enc != nullptr &&
+         enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st, b, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace

@@ -178,22 +178,4 @@ ecokv_status evict_host_rows(const ecokv_params* p, ecokv_dtype dtype, const voi
                              int32_t* idx, int32_t* idx_out, void* K_out, void* V_out, float* lambda, void* ws,
                              size_t ws_bytes, void* stream);
 
-// Launch a kernel that may be scheduled while the grid before it in the stream still
-// runs; the kernel waits for that grid itself (ptx::grid_wait) before it touches memory.
-template <typename... A>
-cudaError_t launch_behind(void (*kernel)(A...), unsigned grid, unsigned block, size_t smem, cudaStream_t st,
-                          const A&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 }  // namespace ecokv

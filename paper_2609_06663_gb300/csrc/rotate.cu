@@ -24,7 +24,7 @@
 #include <string.h>
 
 #include "attend.cuh"
-#include "ptx.cuh"
+#include "decode_ptx.cuh"
 
 namespace ecokv {
 namespace {

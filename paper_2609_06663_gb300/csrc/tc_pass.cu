@@ -966,16 +966,6 @@ EncodeTiledFn encode_fn() {
 
 }  // namespace
 
-bool tensor_map_bf16(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
-                     const cuuint32_t* box) {
-  EncodeTiledFn enc = encode_fn();
-  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  return enc != nullptr &&
-         enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int tc_record_slots(int T, int L) {
   // slices of a wave of L tiles hold at least s = max(1, floor(L / kTcMaxSms))
   // tiles (P <= kTcMaxSms; a shorter last wave's slices are no shorter); a

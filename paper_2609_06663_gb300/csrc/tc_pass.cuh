@@ -45,10 +45,6 @@ int tc_rows(int R);
 int tc_record_slots(int T, int L);
 cudaError_t launch_tc(const void* K, const TcArgs& args, cudaStream_t st);
 
-// A tensor map of bf16 with the 128-byte swizzle (rank up to 5; strides in bytes, of all axes but the first).
-bool tensor_map_bf16(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
-                     const cuuint32_t* box);
-
 // Tensor maps of the keys [U][N][d] (boxes of 128 keys x 64 dimensions) and of
 // the window queries [q_rows][d] (boxes of RP rows x 64), 128-byte swizzle.
 cudaError_t tc_tensor_maps(const void* K, int N, int U, const void* Q, int q_rows, int RP, CUtensorMap* tm,
