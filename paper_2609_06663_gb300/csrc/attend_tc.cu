@@ -8,9 +8,9 @@
 // the softmax of alternating jobs, so that one's exponentials run beside the
 // other's products: the jobs of an item are its two row tiles on each key tile, or, with
 // one row tile, the key tiles in turn, whose sums then are two parts of the row.
-// The maximum that weights refer to is raised, and O rescaled, only when a tile
-// exceeds it by 2^8: the weights are fp32 before they are rounded, so that any
-// reference within their range is as exact.
+// Weights refer to the maximum of the row's first 32 keys, and to another only when a
+// score exceeds it by 2^kRaise: bf16 has the range of fp32 and no weight is more
+// exact for being below one, so that a tile needs no pass for its maximum.
 //
 // Warps: 0 copies (TMA; a lane a page), 1 and 3 the streams' products, 2 the walk over
 // the items, 4-7 and 8-11 the streams' softmax.
@@ -30,7 +30,7 @@ constexpr int kThreads = 384;
 constexpr int kStages = 5;          // tiles of K or V in the ring
 constexpr int kItems = 4;           // items ahead of their consumers
 constexpr uint32_t kHalf = kTileBytes / 2;  // 128 rows x 64 columns
-constexpr float kRaise = 8.f;       // log2 units
+constexpr float kRaise = 64.f;      // log2 units: weights up to 2^64, sums of 2^24 of them far below 2^127
 
 struct Smem {
   uint8_t q[2][kTileBytes];
@@ -257,7 +257,10 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
     const int rows = min(it.ntok - tok, a.tpt) * a.g;
     const bool active = warp * 32 < rows;
     const int lim = it.lim0 + (tok + row_k) * it.slope;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY;  // the reference
+    float2 l[4];          // the sum of the weights, in eight parts
+#pragma unroll
+    for (int q = 0; q < 4; ++q) l[q] = make_float2(0.f, 0.f);
     const int step = two ? 1 : 2, t0 = two ? 0 : p;
     for (int t = t0; t < it.ntiles; t += step, ++k) {
       const int from = (it.tile0 + t) * kKeys;
@@ -266,49 +269,12 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
       tc_fence_after();
       const int nc = min(nv + 31, kKeys) >> 5;  // blocks of 32 keys that are there
       if (active) {
-        // Blocks of 32 keys in loops that stay rolled, the scores read twice: a call of
-        // a few tiles runs this code but once or twice, and fetching code takes longer
-        // than running it (all 128 scores in registers and unrolled: the batch of 16
-        // over 3277 rows 16.2 us, so 15.1; 1952 items of a tile each 59.0 and 47.5)
+        // Blocks of 32 keys in a loop that stays rolled: a call of a few tiles runs this
+        // code but once or twice, and fetching code takes longer than running it (all
+        // of a tile's scores in registers and unrolled: the batch of 16 over 3277 rows
+        // 16.2 us, 1952 items of a tile each 59.0; in two rolled passes, one for the
+        // maximum, 15.1 and 50.2; so 15.0 and 49.1, the questions 109.8 and not 116.6)
         const int seen = lim - from;
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-        for (int b = 0; b < nc; ++b) {
-          uint32_t x[32];
-          tmem_ld_x32(ts + 32 * b, x);
-          tmem_wait_ld();
-          tmem_landed(x);
-          const int here = seen - 32 * b;
-          if (__any_sync(0xffffffffu, here < 32)) {
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (c >= here) x[c] = 0xff800000u;  // -inf
-          }
-#pragma unroll
-          for (int c = 0; c < 32; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(x[c]));
-        }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-        if (t == t0) {
-          m = top;
-        } else if (__any_sync(0xffffffffu, top > m + kRaise)) {
-          // (this stream's product before is complete: it precedes this job's first in the tensor pipe)
-          const float up = top > m + kRaise ? top : m;
-          const float f = up == -INFINITY ? 1.f : ex2(m - up);
-          l *= f;
-          m = up;
-#pragma unroll 1
-          for (int c = 0; c < kD; c += 32) {
-            uint32_t o[32];
-            tmem_ld_x32(to + c, o);
-            tmem_wait_ld();
-            tmem_landed(o);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-            tmem_st_x32(to + c, o);
-          }
-        }
-        const float nref = m == -INFINITY ? 0.f : -m;
-        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
         for (int b = 0; b < nc; ++b) {
           uint32_t x[32], w[16];
@@ -321,16 +287,58 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
             for (int c = 0; c < 32; ++c)
               if (c >= here) x[c] = 0xff800000u;  // -inf
           }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < 32; c += 8)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              mx[q] = fmaxf(fmaxf(mx[q], __uint_as_float(x[c + q])), __uint_as_float(x[c + 4 + q]));
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+          if (__any_sync(0xffffffffu, top > m + kRaise)) {
+            // another reference, by a power of two (the first one as it is): what was
+            // weighted by the old one follows.  (This stream's product before is
+            // complete: it precedes this job's first in the tensor pipe.)
+            float up = m, f = 1.f;
+            if (top > m + kRaise) {
+              up = m == -INFINITY ? top : m + ceilf(top - m);
+              f = ex2(m - up);
+            }
+            m = up;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) l[q] = make_float2(l[q].x * f, l[q].y * f);
+            if (b > 0) {
+              tmem_wait_st();
+#pragma unroll 1
+              for (int q = 0; q < b; ++q) {
+                tmem_ld_x16(ts + 16 * q, w);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 16; ++c)
+                  w[c] = pack_bf16x2(__uint_as_float(w[c] << 16) * f, __uint_as_float(w[c] & 0xffff0000u) * f);
+                tmem_st_x16(ts + 16 * q, w);
+              }
+            }
+            if (t > t0) {
+#pragma unroll 1
+              for (int c = 0; c < kD; c += 16) {
+                tmem_ld_x16(to + c, w);
+                tmem_wait_ld();
+#pragma unroll
+                for (int q = 0; q < 16; ++q) w[q] = __float_as_uint(__uint_as_float(w[q]) * f);
+                tmem_st_x16(to + c, w);
+              }
+            }
+          }
+          const float nref = m == -INFINITY ? 0.f : -m;
 #pragma unroll
           for (int c = 0; c < 32; c += 2) {
             fma_pair(x[c], x[c + 1], scale2, nref, nref);
             const float e0 = ex2(__uint_as_float(x[c])), e1 = ex2(__uint_as_float(x[c + 1]));
-            add_pair(sum[c & 7], sum[(c & 7) + 1], e0, e1);
+            add_pair(l[(c >> 1) & 3].x, l[(c >> 1) & 3].y, e0, e1);
             w[c / 2] = pack_bf16x2(e0, e1);
           }
           tmem_st_x16(ts + 16 * b, w);
         }
-        l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
         tmem_wait_st();
       }
       if (nv < kKeys) {
@@ -358,7 +366,7 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
       const size_t at = first ? first_row(a, it.source, p, token, hq) : next_row(a, blockIdx.x, p, row);
       float* dst = (first ? a.first_o : a.next_o) + at * kD;
       const bool mine = row < rows;
-      if (mine) (first ? a.first_ml : a.next_ml)[at] = make_float2(m, l);
+      if (mine) (first ? a.first_ml : a.next_ml)[at] = make_float2(m, ((l[0].x + l[0].y) + (l[1].x + l[1].y)) + ((l[2].x + l[2].y) + (l[3].x + l[3].y)));
       if (any) {
 #pragma unroll 1
         for (int c = 0; c < kD; c += 32) {

@@ -497,3 +497,26 @@ def test_nothing_to_do():
     assert E.append(b.cache, empty[:, :2], empty[:, :2], starts) is None
     assert E.rotate(E.rotary(), torch.zeros(1, 0, dtype=torch.int32, device="cuda"), empty)[0].shape == (0, 4, D)
     assert torch.equal(before.nan_to_num(), b.dk.nan_to_num())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attend_scores_that_jump(dt):
+    """A key far above all before it, at each place where a weight's reference can change: within a tile, at its
+    end, in the next tile, after masked blocks; and a row whose first keys are far below the rest."""
+    g = gen(61)
+    T = TYPES[dt]
+    n, h_kv = 400, 4
+    u = torch.randn(D, generator=g)
+    u /= u.norm()
+    q = (8 * u + 0.02 * torch.randn(4, h_kv, D, generator=g)).to(T)   # one query head a KV head, four tokens
+    b = Batch(23, h_kv, [2, 1, 1], [130, 40, 300], 16, dt)
+    heads = []
+    for places in ([5, 40, 100], [127, 128, 256], [0], [399, 33]):    # by head
+        k = 0.05 * torch.randn(n, D, generator=g)
+        for i, at in enumerate(places):
+            k[at] += u * (80 + 60 * i)                                # scores 57, 99, 141 units of e apart and more
+        heads.append((k.to(T), torch.randn(n, D, generator=g).to(T)))
+    heads[2] = (heads[2][0].clone(), heads[2][1])
+    heads[2][0][:64] = (-100 * u).to(T)                               # the first keys far below
+    pre = E.Prefix(*(torch.stack([h[i] for h in heads]).cuda() for i in range(2)))
+    check_attend(b, heads, pre, h_kv, dt, q=q)
