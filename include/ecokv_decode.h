@@ -18,9 +18,10 @@
  * `stream`, device-side errors in the workspace's status word
  * (ecokv_device_status), calls that share a workspace ordered on one stream.
  * Rows are d = 128 contiguous elements at 16-byte aligned addresses; strides
- * count elements, multiples of 16 bytes.  Data on the device (positions, lengths,
- * page numbers) is read on the device, so a call can be captured in a graph and
- * replayed as they change.  A call of no tokens does nothing, whatever its pointers.
+ * count elements and are positive multiples of 16 bytes.  Data on the device
+ * (positions, lengths, page numbers) is read on the device, so a call can be captured
+ * in a graph and replayed as they change.  A call of no tokens does nothing, whatever
+ * its pointers.
  */
 #ifndef ECOKV_DECODE_H
 #define ECOKV_DECODE_H

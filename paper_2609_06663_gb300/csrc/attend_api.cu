@@ -352,14 +352,14 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   if (p->d != kD || p->h_q / p->h_kv > kMaxGroup) return ECOKV_ERR_UNSUPPORTED;
   if (p->tokens == 0) return ECOKV_OK;  // (tensors of no rows may have no address)
   if (!q || !out || !aligned16(q) || !aligned16(out) || ((uintptr_t)lse & 3u)) return ECOKV_ERR_INVALID_ARG;
-  if (p->q_token < 0 || p->q_head < 0 || p->out_token < 0 || p->out_head < 0 || !stride_ok(p->q_token, e) ||
+  if (p->q_token <= 0 || p->q_head <= 0 || p->out_token <= 0 || p->out_head <= 0 || !stride_ok(p->q_token, e) ||
       !stride_ok(p->q_head, e) || !stride_ok(p->out_token, e) || !stride_ok(p->out_head, e))
     return ECOKV_ERR_INVALID_ARG;
   AttendArgs a{};
   if (prefix != nullptr && prefix->rows != 0) {
     if (prefix->rows < 0 || !prefix->k || !prefix->v || !aligned16(prefix->k) || !aligned16(prefix->v) ||
         ((uintptr_t)prefix->head_off & 3u) || prefix->row_stride <= 0 || !stride_ok(prefix->row_stride, e) ||
-        (!prefix->head_off && (prefix->head_stride < 0 || !stride_ok(prefix->head_stride, e))))
+        (!prefix->head_off && (prefix->head_stride <= 0 || !stride_ok(prefix->head_stride, e))))
       return ECOKV_ERR_INVALID_ARG;
     if (prefix->rows > kMaxN) return ECOKV_ERR_UNSUPPORTED;
     a.prefix = *prefix;

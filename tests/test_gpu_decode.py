@@ -245,6 +245,7 @@ ATTEND = [  # h_q, h_kv, new, lengths, page, prefix rows (a list: uneven), order
     (8, 1, [150], [300], 512, 40, "slot"),                                  # many token groups of one sequence
     (64, 1, [1, 2, 5], [9, 20, 500], 256, 64, "head"),                      # the largest group
     (6, 2, [2, 2, 2, 2], [1, 0, 2, 30], 16, 0, "head"),                     # tokens that see nothing
+    (6, 2, [1, 1, 1], [0, 0, 0], 8, 0, "head"),                             # none that sees anything
     (10, 5, [1] * 33, [2] * 33, 8, [0, 300, 1, 128, 77], "head"),           # uneven heads, one of them empty
     (12, 4, [4, 9], [40, 1000], 16, [1000, 0, 0, 513], "slot"),
     (40, 40, [1] * 3, [40, 50, 600], 16, [i % 7 * 40 for i in range(40)], "head"),  # more heads than lanes
