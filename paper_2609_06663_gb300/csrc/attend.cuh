@@ -37,6 +37,7 @@ struct AttendArgs {
   const int32_t* starts;
   int tpt;    // tokens a row tile holds
   int span;   // tokens an item holds (one or two row tiles)
+  int groups, last;  // items that all tokens make, the last one's tokens
   int parts;  // partial sums a CTA may have of a row: 2 where two row groups share the tiles
   int P;      // CTAs
   int lead;   // see lead_units()
@@ -75,6 +76,8 @@ __device__ __forceinline__ void note(const AttendArgs& a, unsigned code, unsigne
 }
 
 __host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
+__host__ __device__ inline int tiles_of(int keys) { return (keys + kKeys - 1) >> 7; }  // (keys >= 0)
+static_assert(kKeys == 128, "tiles_of");
 
 // Tokens and slots of sequence b, clamped to what the buffers hold.
 struct Seq {
@@ -105,16 +108,20 @@ __host__ __device__ inline int item_units(const AttendArgs& a, int tiles, int nt
 }
 // ... of all token groups of the prefix of one head (the last may be a shorter one).
 __host__ __device__ inline int prefix_units(const AttendArgs& a, int tiles) {
-  const int groups = div_up(a.tokens, a.span), last = a.tokens - (groups - 1) * a.span;
-  return (groups - 1) * item_units(a, tiles, a.span) + item_units(a, tiles, last);
+  return (a.groups - 1) * item_units(a, tiles, a.span) + item_units(a, tiles, a.last);
 }
-// Keys that the tokens of group `rg` of a sequence see at most, and the units of the groups before.
-__device__ __forceinline__ int seq_vis(const AttendArgs& a, const Seq& s, int rg) {
-  return max(s.L - s.T + min(s.T, (rg + 1) * a.span), 0);
+// Keys that a sequence's item from its token i on sees at most, the item's units, and
+// those of all its items from tokens below `until`.
+__device__ __forceinline__ int seq_vis(const AttendArgs& a, const Seq& s, int i) {
+  return max(s.L - s.T + min(s.T, i + a.span), 0);
 }
-__device__ __forceinline__ int seq_units(const AttendArgs& a, const Seq& s, int groups) {
+__device__ __forceinline__ int seq_item(const AttendArgs& a, const Seq& s, int i) {
+  return item_units(a, tiles_of(seq_vis(a, s, i)), min(s.T - i, a.span));
+}
+__device__ __forceinline__ int seq_units(const AttendArgs& a, const Seq& s, int until) {
   int n = 0;
-  for (int rg = 0; rg < groups; ++rg) n += item_units(a, div_up(seq_vis(a, s, rg), kKeys), min(s.T - rg * a.span, a.span));
+#pragma unroll 1
+  for (int i = 0; i < until; i += a.span) n += seq_item(a, s, i);
   return n;
 }
 // Rows of head h's prefix.
@@ -155,7 +162,7 @@ struct Walk {
     w = 0;
     if (b < a.batch) {
       s = load_seq(a, b, report);
-      w = seq_units(a, s, div_up(s.T, a.span));
+      w = seq_units(a, s, s.T);
     }
     upto = scan(w, lane);
   }
@@ -167,14 +174,16 @@ struct Walk {
     prefix_total = 0;
     if (a.prefix.rows > 0) {
       if (a.prefix.head_off == nullptr) {
-        const int per = prefix_units(a, div_up(a.prefix.rows, kKeys));
+        const int per = prefix_units(a, tiles_of(a.prefix.rows));
         prefix_total = a.h_kv * per;
         if (lead)
+#pragma unroll 1
           for (int h = lane; h < a.h_kv; h += 32) a.plan[PLAN_HEADS + h] = h * per;
       } else {
+#pragma unroll 1
         for (int h0 = 0; h0 < a.h_kv; h0 += 32) {
           int row0, n = 0;
-          if (h0 + lane < a.h_kv) n = prefix_units(a, div_up(prefix_rows(a, h0 + lane, row0, lead), kKeys));
+          if (h0 + lane < a.h_kv) n = prefix_units(a, tiles_of(prefix_rows(a, h0 + lane, row0, lead)));
           const int up = scan(n, lane);
           if (lead && h0 + lane < a.h_kv) a.plan[PLAN_HEADS + h0 + lane] = prefix_total + up - n;
           prefix_total += __shfl_sync(0xffffffffu, up, 31);
@@ -184,6 +193,7 @@ struct Walk {
     own = 0;
     if (a.has_cache) {
       long long sum = 0;
+#pragma unroll 1
       for (int c = 0; c < a.batch; c += 32) {
         chunk(a, c, lead);
         if (lead && c + lane < a.batch) a.plan[PLAN_HEADS + a.h_kv + c + lane] = (int)sum + upto - w;
@@ -213,6 +223,7 @@ struct Walk {
 
   // The next item (the same in every lane); false: none left.
   __device__ __forceinline__ bool next(const AttendArgs& a, Item& it) {
+#pragma unroll 1
     while (x < end) {
       if (!at(a, it)) return false;
       if (it.ntiles > 0) return true;
@@ -225,7 +236,7 @@ struct Walk {
     if (x < prefix_total) {
       int h, row0;
       if (a.prefix.head_off == nullptr) {
-        const int per = prefix_units(a, div_up(a.prefix.rows, kKeys));
+        const int per = prefix_units(a, tiles_of(a.prefix.rows));
         h = x / per;
         y = x - h * per;
         row0 = 0;
@@ -233,12 +244,13 @@ struct Walk {
       } else {
         int at = 0;
         h = 0;
+#pragma unroll 1
         for (int h0 = 0;; h0 += 32) {
           if (h0 >= a.h_kv) return false;  // (only when the offsets change under the kernel; so below)
           int n = 0, r0 = 0, rows = 0;
           if (h0 + lane < a.h_kv) {
             rows = prefix_rows(a, h0 + lane, r0, false);
-            n = prefix_units(a, div_up(rows, kKeys));
+            n = prefix_units(a, tiles_of(rows));
           }
           const int up = scan(n, lane), all = __shfl_sync(0xffffffffu, up, 31);
           if (x < at + all) {
@@ -252,7 +264,7 @@ struct Walk {
           at += all;
         }
       }
-      nt = div_up(it.vis, kKeys);
+      nt = tiles_of(it.vis);
       const int rg = y / item_units(a, nt, a.span);
       it.source = 0;
       it.head = h;
@@ -273,6 +285,7 @@ struct Walk {
       }
       head = h;
       int all;
+#pragma unroll 1
       while (y >= base + (all = __shfl_sync(0xffffffffu, upto, 31))) {
         base += all;
         if (b0 + 32 >= a.batch) return false;
@@ -284,27 +297,28 @@ struct Walk {
       q.start = __shfl_sync(0xffffffffu, s.start, l);
       q.T = __shfl_sync(0xffffffffu, s.T, l);
       q.L = __shfl_sync(0xffffffffu, s.L, l);
-      int rg = 0, n;
-      while (y >= (n = item_units(a, div_up(seq_vis(a, q, rg), kKeys), min(q.T - rg * a.span, a.span)))) {
+      int i = 0, n;
+#pragma unroll 1
+      while (y >= (n = seq_item(a, q, i))) {
         y -= n;
-        if (++rg * a.span >= q.T) return false;
+        if ((i += a.span) >= q.T) return false;
       }
       it.source = 1;
       it.head = h;
       it.seq = b0 + l;
-      it.tok0 = q.start + rg * a.span;
-      it.ntok = min(a.span, q.T - rg * a.span);
-      it.lim0 = q.L - q.T + rg * a.span + 1;
+      it.tok0 = q.start + i;
+      it.ntok = min(a.span, q.T - i);
+      it.lim0 = q.L - q.T + i + 1;
       it.slope = 1;
-      it.vis = seq_vis(a, q, rg);
+      it.vis = seq_vis(a, q, i);
       it.row0 = 0;
-      nt = div_up(it.vis, kKeys);
+      nt = tiles_of(it.vis);
     }
     // the tiles whose first unit lies within this CTA's part of the item, y .. z - 1
     const int u = tile_units(a, it.ntok), z = min(item_units(a, nt, it.ntok), y + end - x);
     const int lead = lead_units(a, it.ntok);
-    it.tile0 = div_up(max(y - lead, 0), u);
-    it.ntiles = div_up(max(z - lead, 0), u) - it.tile0;
+    it.tile0 = (max(y - lead, 0) + u - 1) >> (u - 1);  // (u: 1 or 2)
+    it.ntiles = ((max(z - lead, 0) + u - 1) >> (u - 1)) - it.tile0;
     x += z - y;
     return z > y;  // (else nothing would move on)
   }

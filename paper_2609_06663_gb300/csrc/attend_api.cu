@@ -57,7 +57,7 @@ __device__ __forceinline__ Parts find_parts(const AttendArgs& a, int source, int
 }
 
 __device__ __forceinline__ const float* part(const AttendArgs& a, const Parts& p, int e, float2& ml) {
-  const int c = e / p.nj, j = e - c * p.nj;
+  const int c = e >> (p.nj - 1), j = e - c * p.nj;  // (nj: 1 or 2)
   if (c == 0) {
     const size_t at = p.first + (size_t)j * a.tokens * a.h_q;
     ml = a.first_ml[at];
@@ -96,7 +96,7 @@ __device__ __forceinline__ PartList list_parts(const AttendArgs& a, int token, i
   if (a.prefix.rows > 0) {
     int row0;
     const int first = a.plan[PLAN_HEADS + h];
-    const int nt = div_up(prefix_rows(a, h, row0, false), kKeys), rg = token / a.span;
+    const int nt = tiles_of(prefix_rows(a, h, row0, false)), rg = token / a.span;
     l.src[0] = find_parts(a, 0, first + rg * item_units(a, nt, a.span), nt, run, token - rg * a.span,
                           min(a.span, a.tokens - rg * a.span), token, h * a.g);
   }
@@ -105,10 +105,9 @@ __device__ __forceinline__ PartList list_parts(const AttendArgs& a, int token, i
     const Seq s = load_seq(a, b, false);
     const int i = token - s.start;
     if (i >= 0 && i < s.T && own > 0) {
-      const int rg = i / a.span;
-      l.src[1] = find_parts(a, 1, prefix_total + h * own + first + seq_units(a, s, rg),
-                            div_up(seq_vis(a, s, rg), kKeys), run, i - rg * a.span, min(a.span, s.T - rg * a.span),
-                            token, h * a.g);
+      const int i0 = i / a.span * a.span;  // its item's first token
+      l.src[1] = find_parts(a, 1, prefix_total + h * own + first + seq_units(a, s, i0), tiles_of(seq_vis(a, s, i0)),
+                            run, i - i0, min(a.span, s.T - i0), token, h * a.g);
     }
   }
   l.n = l.src[0].n + l.src[1].n;
@@ -124,15 +123,18 @@ __device__ __forceinline__ void add_part(float4& acc, float w, float4 v) {
   acc.w = fmaf(w, any ? v.w : 0.f, acc.w);
 }
 
-// The largest maximum of a row's parts; o, ml: this lane's part of the first 32.
-__device__ __forceinline__ float row_max(const AttendArgs& a, const PartList& l, int r, int lane, float2 ml) {
-  float M = ml.x;
-  for (int e = lane + 32; e < l.n; e += 32) {
-    float2 x;
-    l.at(a, e, r, x);
-    M = fmaxf(M, x.x);
-  }
-  return ptx::redux_max(M);
+// The weight of this lane's next part: the largest maximum M, the lane's share L of the
+// sum and the output so far follow.
+__device__ __forceinline__ float next_weight(float& M, float& L, float4& acc, float2 ml) {
+  const float Mn = fmaxf(M, ptx::redux_max(ml.x)), ref = Mn == -INFINITY ? 0.f : Mn;
+  const float c = ptx::ex2(M - ref), w = ptx::ex2(ml.x - ref);
+  M = Mn;
+  L = fmaf(L, c, w > 0.f ? w * ml.y : 0.f);
+  acc.x *= c;
+  acc.y *= c;
+  acc.z *= c;
+  acc.w *= c;
+  return w;
 }
 
 template <typename T>
@@ -150,7 +152,7 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, int token, int hq
     a.lse[(int64_t)token * a.h_q + hq] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
-constexpr int kAhead = 8;  // sums whose loads are in flight
+constexpr int kAhead = 32 / kJoinWarps;  // sums whose loads a warp has in flight
 
 // One warp `per` rows of a (token, KV head).
 template <typename T>
@@ -166,24 +168,26 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   const int token = (int)(unit / a.h_kv), h = (int)(unit - (long long)token * a.h_kv);
   const int r0 = (int)(id - unit * split) * per, r1 = min(r0 + per, a.g);
   const PartList l = list_parts(a, token, h, lane);
-  float2 ml = make_float2(-INFINITY, 0.f), ml_next = ml;
-  const float *o = nullptr, *o_next = nullptr;
-  if (lane < l.n) o_next = l.at(a, lane, r0, ml_next);
-  for (int r = r0; r < r1; ++r) {
-    ml = ml_next;
-    o = o_next;
+  // (a row's first 32 parts are looked up while the row before it is summed)
+  float2 ml_next = make_float2(-INFINITY, 0.f);
+  const float* o_next = nullptr;
+#pragma unroll 1
+  for (int r = r0 - 1; r < r1; ++r) {
+    const float* o = o_next;
+    float2 ml = ml_next;
     if (lane < l.n && r + 1 < r1) o_next = l.at(a, lane, r + 1, ml_next);
-    const float M = row_max(a, l, r, lane, ml), ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
+    if (r < r0) continue;
+    float M = -INFINITY, L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
     for (int e0 = 0; e0 < l.n; e0 += 32) {
       if (e0 > 0) {
         ml = make_float2(-INFINITY, 0.f);
         if (e0 + lane < l.n) o = l.at(a, e0 + lane, r, ml);
       }
-      const float w = ptx::ex2(ml.x - ref);
-      L = fmaf(w, w > 0.f ? ml.y : 0.f, L);
+      const float w = next_weight(M, L, acc, ml);
       const int n = min(32, l.n - e0);
+#pragma unroll 2
       for (int k = 0; k < n; ++k) {
         const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, k));
         add_part(acc, __shfl_sync(0xffffffffu, w, k), *reinterpret_cast<const float4*>(ok + 4 * lane));
@@ -202,40 +206,29 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_row_kernel(const 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int token = blockIdx.x / a.h_q, hq = blockIdx.x - token * a.h_q, h = hq / a.g, r = hq - h * a.g;
   const PartList l = list_parts(a, token, h, lane);
-  float2 ml = make_float2(-INFINITY, 0.f);
-  const float* o = nullptr;
-  if (lane < l.n) o = l.at(a, lane, r, ml);
-  float4 v[kAhead];  // this warp's sums of the first 32
-#pragma unroll
-  for (int k = 0; k < kAhead; ++k) {
-    const int e = k * kJoinWarps + warp;
-    const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, e & 31));
-    v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (e < min(l.n, 32)) v[k] = *reinterpret_cast<const float4*>(ok + 4 * lane);
-  }
-  const float M = row_max(a, l, r, lane, ml), ref = M == -INFINITY ? 0.f : M;
-  float L = 0.f;
+  float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int e0 = 0; e0 < l.n; e0 += 32) {
-    if (e0 > 0) {
-      ml = make_float2(-INFINITY, 0.f);
-      if (e0 + lane < l.n) o = l.at(a, e0 + lane, r, ml);
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int e = k * kJoinWarps + warp;
-        const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, e & 31));
-        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (e0 + e < l.n && e < 32) v[k] = *reinterpret_cast<const float4*>(ok + 4 * lane);
-      }
-    }
-    const float w = ptx::ex2(ml.x - ref);
-    L = fmaf(w, w > 0.f ? ml.y : 0.f, L);
+  // (32 parts are looked up while those before them are summed)
+  float2 ml_next = make_float2(-INFINITY, 0.f);
+  const float* o_next = nullptr;
+#pragma unroll 1
+  for (int e0 = -32; e0 < l.n; e0 += 32) {
+    const float* o = o_next;
+    const float2 ml = ml_next;
+    ml_next = make_float2(-INFINITY, 0.f);
+    if (e0 + 32 + lane < l.n) o_next = l.at(a, e0 + 32 + lane, r, ml_next);
+    if (e0 < 0) continue;
+    float4 v[kAhead];  // this warp's sums of these 32
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int e = k * kJoinWarps + warp;
-      const float wk = __shfl_sync(0xffffffffu, w, e & 31);
-      add_part(acc, e < 32 ? wk : 0.f, v[k]);
+      const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, e));
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (e0 + e < l.n) v[k] = *reinterpret_cast<const float4*>(ok + 4 * lane);
     }
+    const float w = next_weight(M, L, acc, ml);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) add_part(acc, __shfl_sync(0xffffffffu, w, k * kJoinWarps + warp), v[k]);
   }
   sums[warp][lane] = acc;
   __syncthreads();
@@ -398,9 +391,10 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   a.scale_log2 = (float)(1.4426950408889634 * scale);
   a.timeout_ns = (p->timeout_us ? (unsigned long long)p->timeout_us : 2000000ull) * 1000ull;
   // units of every item, counted in 32 bits by the kernels
-  const long long groups = (a.tokens + a.span - 1) / a.span;
-  const long long of_cap = item_units(a, (a.cap + kKeys - 1) / kKeys, a.span),
-                  of_prefix = item_units(a, (a.prefix.rows + kKeys - 1) / kKeys, a.span);
+  a.groups = div_up(a.tokens, a.span);
+  a.last = a.tokens - (a.groups - 1) * a.span;
+  const long long groups = a.groups;
+  const long long of_cap = item_units(a, tiles_of(a.cap), a.span), of_prefix = item_units(a, tiles_of(a.prefix.rows), a.span);
   const long long units = a.h_kv * (groups * of_prefix + (groups + a.batch) * of_cap);
   if (units > 0x7fffffff || groups * of_cap > (1 << 25)) return ECOKV_ERR_UNSUPPORTED;
   char* w = static_cast<char*>(ws);

@@ -56,8 +56,9 @@ struct Maps {
 };
 
 // Bounded wait: false once this CTA has given up.  (The clock is read every 16th
-// try: reading it takes longer than a try.)
-__device__ __forceinline__ bool wait_bar(Smem& s, const AttendArgs& a, uint64_t* bar, uint32_t parity, unsigned where) {
+// try: reading it takes longer than a try.  One copy of this for all waits: inlined in
+// each, it was a fifth of the kernel's code.)
+__device__ __noinline__ bool wait_long(Smem& s, const AttendArgs& a, uint64_t* bar, uint32_t parity, unsigned where) {
   unsigned long long t0 = 0;
 #pragma unroll 1
   for (uint32_t i = 1; !mbar_try_wait(bar, parity); ++i) {
@@ -72,6 +73,9 @@ __device__ __forceinline__ bool wait_bar(Smem& s, const AttendArgs& a, uint64_t*
     }
   }
   return true;
+}
+__device__ __forceinline__ bool wait_bar(Smem& s, const AttendArgs& a, uint64_t* bar, uint32_t parity, unsigned where) {
+  return mbar_try_wait(bar, parity) || wait_long(s, a, bar, parity, where);
 }
 // A whole warp's wait.
 __device__ __forceinline__ bool wait_warp(Smem& s, const AttendArgs& a, uint64_t* bar, uint32_t parity,
