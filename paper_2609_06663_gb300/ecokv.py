@@ -486,11 +486,17 @@ def _dtype(t, *others) -> int:
 _codes = {}  # torch dtype -> code
 
 
+_int32 = None
+
+
 def _ints(x, shape, what):
-    import torch
+    global _int32
     if x is None:
         return None
-    if x.dtype is not torch.int32 or not x.is_cuda or not x.is_contiguous() or (shape and x.shape != shape):
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
+    if x.dtype is not _int32 or not x.is_cuda or not x.is_contiguous() or (shape and x.shape != shape):
         raise ValueError(f"{what}: a contiguous int32 CUDA tensor{f' of shape {shape}' if shape else ''} is wanted")
     return x.data_ptr()
 
@@ -511,19 +517,27 @@ def _heads(x, what):
 
 
 def _rows(x, y, norm, what):
-    tokens, heads, st, sh = _heads(x, what)
+    n, s = x.shape, x.stride()
+    if len(n) != 3 or n[2] != HEAD_DIM or s[2] != 1:
+        _heads(x, what)  # (raises)
+    tokens, heads, _ = n
     if norm is not None:
         if norm.numel() != HEAD_DIM or not norm.is_contiguous():
             raise ValueError(f"{what}: contiguous norm weights [{HEAD_DIM}] are wanted")
         norm = norm.data_ptr()
-    if y is None:
-        return ecokv_rows(x.data_ptr(), None, st, sh, 0, 0, norm, heads)
-    if y is x:
-        return ecokv_rows(x.data_ptr(), x.data_ptr(), st, sh, st, sh, norm, heads)
-    ty, hy, yt, yh = _heads(y, what)
-    if ty != tokens or hy != heads:
-        raise ValueError(f"{what}: the output has another shape")
-    return ecokv_rows(x.data_ptr(), y.data_ptr(), st, sh, yt, yh, norm, heads)
+    at, t = None, (0, 0)
+    if y is not None:
+        if y.shape != n:
+            raise ValueError(f"{what}: the output has another shape")
+        at, t = y.data_ptr(), y.stride()
+        if t[2] != 1:
+            _heads(y, what)
+    if tokens > 1 and heads > 1:
+        return ecokv_rows(x.data_ptr(), at, s[0], s[1], t[0], t[1], norm, heads)
+    # (a stride that is never taken counts as a row)
+    many, two = tokens > 1, heads > 1
+    return ecokv_rows(x.data_ptr(), at, s[0] if many else HEAD_DIM, s[1] if two else HEAD_DIM,
+                      t[0] if many else HEAD_DIM, t[1] if two else HEAD_DIM, norm, heads)
 
 
 _raw_stream = None
@@ -575,9 +589,9 @@ def _positions(rot, positions, tokens):
         return None
     if positions is None:
         raise ValueError("positions are wanted")
-    n = positions.shape
-    if n != (rot.axes, tokens) and not (n == (tokens,) and rot.axes == 1):
-        raise ValueError(f"positions: [{rot.axes}, {tokens}] is wanted")
+    n, axes = positions.shape, rot.axes
+    if n[-1] != tokens or (n[0] != axes or len(n) != 2) and (len(n) != 1 or axes != 1):
+        raise ValueError(f"positions: [{axes}, {tokens}] is wanted")
     return _ints(positions, None, "positions")
 
 
