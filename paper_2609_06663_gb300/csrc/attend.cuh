@@ -38,16 +38,16 @@ struct AttendArgs {
   int tpt;    // tokens a row tile holds
   int span;   // tokens an item holds (one or two row tiles)
   int groups, last;  // items that all tokens make, the last one's tokens
-  int parts;  // partial sums a CTA may have of a row: 2 where two row groups share the tiles
+  int parts;  // row tiles that an item may have
   int P;      // CTAs
   int lead;   // see lead_units()
   int stall;  // fault injection: no tile ever comes
   float scale_log2;
   unsigned long long timeout_ns;
   // workspace
-  float* first_o;   // [2 sources][parts][tokens * h_q][d]: an item's sum from its first tile on
+  float* first_o;   // [2 sources][tokens * h_q][d]: an item's sum from its first tile on
   float2* first_ml; //   maximum (log2 units) and sum
-  float* next_o;    // [P][parts][kTileRows][d]: of an item begun by an earlier CTA
+  float* next_o;    // [P][parts][kTileRows][d]: of an item that an earlier CTA began
   float2* next_ml;
   int* plan;        // see PLAN_*
   unsigned* status;
@@ -324,9 +324,10 @@ struct Walk {
   }
 };
 
-// Where CTA `cta` leaves row (token k of the item, head hq of all) of part j.
-__device__ __forceinline__ size_t first_row(const AttendArgs& a, int source, int j, int token, int hq) {
-  return ((size_t)(source * a.parts + j) * a.tokens + token) * a.h_q + hq;
+// Where the sum of a row (token, query head) goes from its item's first CTA, and that
+// of row `row` of row tile j of the item that CTA `cta` goes on with.
+__device__ __forceinline__ size_t first_row(const AttendArgs& a, int source, int token, int hq) {
+  return ((size_t)source * a.tokens + token) * a.h_q + hq;
 }
 __device__ __forceinline__ size_t next_row(const AttendArgs& a, int cta, int j, int row) {
   return ((size_t)cta * a.parts + j) * kTileRows + row;

@@ -33,37 +33,33 @@ __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float4 v
       make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
 
-// Partial sums of one source that a row has: of CTAs c0 .. c0 + n / nj - 1.
+// Partial sums of one source that a row has: one of each of n CTAs from c0 on.
 struct Parts {
-  int c0, n, nj, j0;
+  int c0, n, tile;
   size_t first;   // row of the first CTA's
-  int row;        // row within a continued item
+  int row;        // row of row tile `tile` of a continued item
 };
 
 // (unit: the item's first; nt: its tiles)
 __device__ __forceinline__ Parts find_parts(const AttendArgs& a, int source, int unit, int nt, int run, int k, int ntok,
                                             int token, int hq) {
-  Parts p{0, 0, 1, 0, 0, 0};
+  Parts p{0, 0, 0, 0, 0};
   if (nt <= 0) return p;
   unit += lead_units(a, ntok);
   p.c0 = unit / run;
-  const int ctas = (unit + (nt - 1) * tile_units(a, ntok)) / run - p.c0 + 1;
-  if (ntok > a.tpt) p.j0 = k / a.tpt;  // two row tiles: the row is in one of them
-  else p.nj = a.parts;
-  p.n = ctas * p.nj;
-  p.first = first_row(a, source, p.j0, token, hq);
-  p.row = (k % a.tpt) * a.g + hq % a.g;
+  p.n = (unit + (nt - 1) * tile_units(a, ntok)) / run - p.c0 + 1;
+  p.tile = k >= a.tpt ? 1 : 0;
+  p.first = first_row(a, source, token, hq);
+  p.row = (k - p.tile * a.tpt) * a.g + hq % a.g;
   return p;
 }
 
 __device__ __forceinline__ const float* part(const AttendArgs& a, const Parts& p, int e, float2& ml) {
-  const int c = e >> (p.nj - 1), j = e - c * p.nj;  // (nj: 1 or 2)
-  if (c == 0) {
-    const size_t at = p.first + (size_t)j * a.tokens * a.h_q;
-    ml = a.first_ml[at];
-    return a.first_o + at * kD;
+  if (e == 0) {
+    ml = a.first_ml[p.first];
+    return a.first_o + p.first * kD;
   }
-  const size_t at = next_row(a, p.c0 + c, p.j0 + j, p.row);
+  const size_t at = next_row(a, p.c0 + e, p.tile, p.row);
   ml = a.next_ml[at];
   return a.next_o + at * kD;
 }
@@ -84,7 +80,6 @@ struct PartList {
 
 __device__ __forceinline__ PartList list_parts(const AttendArgs& a, int token, int h, int lane) {
   PartList l{};
-  l.src[0].nj = l.src[1].nj = 1;
   int b = token;
   if (a.has_cache && a.starts != nullptr) {
     b = 0;
@@ -253,7 +248,7 @@ struct AttendLayout {
 };
 AttendLayout attend_layout(int32_t tokens, int32_t batch, int32_t h_q, int32_t h_kv, int parts) {
   AttendLayout L{};
-  const size_t first = 2ull * parts * tokens * h_q, next = (size_t)kMaxAttendSms * parts * kTileRows;
+  const size_t first = 2ull * tokens * h_q, next = (size_t)kMaxAttendSms * parts * kTileRows;
   size_t off = 256;  // the status word
   L.plan = off;
   off += align256(((size_t)PLAN_HEADS + h_kv + batch) * 4);

@@ -196,7 +196,7 @@ __device__ __forceinline__ void item_few(const AttendArgs& a, Smem& s, const Ite
     }
     const int k = r / a.g;
     const bool first = it.tile0 == 0;
-    const size_t to = first ? first_row(a, it.source, 0, it.tok0 + k, it.head * a.g + r - k * a.g)
+    const size_t to = first ? first_row(a, it.source, it.tok0 + k, it.head * a.g + r - k * a.g)
                             : next_row(a, blockIdx.x, 0, r);
     *reinterpret_cast<float4*>((first ? a.first_o : a.next_o) + to * kD + lane * 4) = acc;
     if (lane == 0) (first ? a.first_ml : a.next_ml)[to] = make_float2(M, L);
@@ -332,7 +332,7 @@ __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const It
     if (row < rows) {
       const int k = row / a.g;
       const bool first = it.tile0 == 0;
-      const size_t at = first ? first_row(a, it.source, 0, it.tok0 + k, it.head * a.g + row - k * a.g)
+      const size_t at = first ? first_row(a, it.source, it.tok0 + k, it.head * a.g + row - k * a.g)
                               : next_row(a, blockIdx.x, 0, row);
       float* dst = (first ? a.first_o : a.next_o) + at * kD;
       *reinterpret_cast<float4*>(dst + 4 * tx) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);

@@ -7,7 +7,7 @@
 // P V reads them; O stays in tensor memory through the item.  Two warpgroups ("streams") do
 // the softmax of alternating jobs, so that one's exponentials run beside the
 // other's products: the jobs of an item are its two row tiles on each key tile, or, with
-// one row tile, the key tiles in turn, whose sums then are two parts of the row.
+// one row tile, the key tiles in turn, whose sums are added at its end.
 // Weights refer to the maximum of the row's first 32 keys, and to another only when a
 // score exceeds it by 2^kRaise: bf16 has the range of fp32 and no weight is more
 // exact for being below one, so that a tile needs no pass for its maximum.
@@ -42,6 +42,8 @@ struct Smem {
   uint64_t full[3][kStages], empty[kStages];
   uint64_t qfull[2], qempty[2];
   uint64_t sfull[2], vready[2], pready[2], ofull[2];
+  uint64_t mready[4], mdone[4];  // between the streams' warps of the same rows
+  float2 ml[128];                // the second stream's references and sums, by row
   uint64_t ifull[kItems], iempty[kItems];
   uint64_t drained;
   Item items[kItems];
@@ -254,6 +256,7 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
   Item it;
   // jobs and tiles before the item; this stream's jobs, items and ragged tiles
   uint32_t n0 = 0, tile_n = 0, k = 0, ends = 0, tails = 0;
+  uint32_t merges = 0;  // items of which this warp's rows are in both streams
   while (items.next(s, a, it, lane)) {
     const bool two = it.ntok > a.tpt;
     const int p = (stream ^ (int)n0) & 1;  // which of the item's row tiles, or of its key tiles in turn
@@ -360,32 +363,68 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.pready[stream]);
     }
-    // the row's part
-    const bool any = t0 < it.ntiles;
+    // The row's part.  Where the streams have had an item's key tiles in turn, the one
+    // that had the first adds the other's sum to its own: a warp sees the tensor
+    // memory of its rows in both.  (Warps of the same rows wait for each other only,
+    // each time in both directions, so that neither's wait meets another phase.)
+    const bool any = t0 < it.ntiles, both = !two && it.ntiles > 1;
     if (any && !wait_warp(s, a, &s.ofull[stream], ends & 1, 10u)) return;
-    if (active) {
+    if (active && any) {
       tc_fence_after();
-      const bool first = it.tile0 == 0;
-      const int token = it.tok0 + tok + row_k, hq = it.head * a.g + row - row_k * a.g;
-      const size_t at = first ? first_row(a, it.source, p, token, hq) : next_row(a, blockIdx.x, p, row);
-      float* dst = (first ? a.first_o : a.next_o) + at * kD;
-      const bool mine = row < rows;
-      if (mine) (first ? a.first_ml : a.next_ml)[at] = make_float2(m, ((l[0].x + l[0].y) + (l[1].x + l[1].y)) + ((l[2].x + l[2].y) + (l[3].x + l[3].y)));
-      if (any) {
+      float sum = ((l[0].x + l[0].y) + (l[1].x + l[1].y)) + ((l[2].x + l[2].y) + (l[3].x + l[3].y));
+      if (both && p == 1) {
+        s.ml[row] = make_float2(m, sum);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.mready[warp]);
+        if (!wait_warp(s, a, &s.mdone[warp], merges & 1, 14u)) return;
+        tc_fence_after();
+      } else {
+        float f = 1.f, f2 = 0.f;
+        if (both) {
+          if (!wait_warp(s, a, &s.mready[warp], merges & 1, 14u)) return;
+          tc_fence_after();
+          const float2 ml = s.ml[row];
+          const float up = fmaxf(m, ml.x), ref = up == -INFINITY ? 0.f : up;
+          f = ex2(m - ref);
+          f2 = ex2(ml.x - ref);
+          sum = fmaf(sum, f, ml.y * f2);
+          m = up;
+        }
+        const bool first = it.tile0 == 0;
+        const int token = it.tok0 + tok + row_k, hq = it.head * a.g + row - row_k * a.g;
+        const size_t at = first ? first_row(a, it.source, token, hq) : next_row(a, blockIdx.x, p, row);
+        float* dst = (first ? a.first_o : a.next_o) + at * kD;
+        const bool mine = row < rows;
+        if (mine) (first ? a.first_ml : a.next_ml)[at] = make_float2(m, sum);
+        const uint32_t other = to ^ 256u;  // the other stream's sum of the same rows
 #pragma unroll 1
         for (int c = 0; c < kD; c += 32) {
-          uint32_t o[32];
+          uint32_t o[32], o2[32];
           tmem_ld_x32(to + c, o);
+          if (both) tmem_ld_x32(other + c, o2);
           tmem_wait_ld();
           tmem_landed(o);
+          if (both) {
+            tmem_landed(o2);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              // (without weight it counts nothing, whatever it holds)
+              const float own = f > 0.f ? __uint_as_float(o[j]) : 0.f, its = f2 > 0.f ? __uint_as_float(o2[j]) : 0.f;
+              o[j] = __float_as_uint(fmaf(its, f2, own * f));
+            }
+          }
           if (mine) {
 #pragma unroll
             for (int j = 0; j < 32; j += 8) store8(dst + c + j, o + j);
           }
         }
+        tc_fence_before();
+        __syncwarp();
+        if (both && lane == 0) mbar_arrive(&s.mdone[warp]);
       }
-      tc_fence_before();
     }
+    if (active && both) ++merges;
     if (any) ++ends;
     tile_n += it.ntiles;
     n0 += it.ntiles * (two ? 2 : 1);
@@ -413,6 +452,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&s.ifull[i], 1);
       mbar_init(&s.iempty[i], 11);  // the warps of the copies, the MMAs and the streams
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&s.mready[i], 1);
+      mbar_init(&s.mdone[i], 1);
     }
     mbar_init(&s.drained, 2);
     s.abort = 0;
