@@ -283,11 +283,11 @@ int attend_sms() {
 template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
-  // one CTA a row while all of them are resident (152 SMs of 8; 1792 rows, the whole
-  // call: 63.9 us so, 61.1 by warps), past that as many rows a warp as leave 10 warps
-  // an SM (3700 rows: 20.5 us at 20 warps, 18.4 at 10; 20600: 121.7 and 121.8, 128 at 100)
+  // one CTA a row while all of them are resident (152 SMs of 8; the whole call at 1024
+  // rows: 94.1 us so, 98.0 by warps; at 1792: 62.3 and 60.5), past that as many rows a
+  // warp as leave 20 warps an SM (3696 rows, the whole call: 26.3 us, 27.2 at 10)
   if (rows <= 152 * 8) return launch_behind(attend_join_row_kernel<T>, (unsigned)rows, 32 * kJoinWarps, 0, st, a);
-  const long long want = rows / (152 * 10);
+  const long long want = rows / (152 * 20);
   const int per = (int)(want < 1 ? 1 : want > a.g ? a.g : want), split = div_up(a.g, per);
   const long long warps = (long long)a.tokens * a.h_kv * split;
   return launch_behind(attend_join_heads_kernel<T>, (unsigned)((warps + kJoinWarps - 1) / kJoinWarps),
