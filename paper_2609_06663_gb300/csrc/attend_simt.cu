@@ -169,11 +169,11 @@ __device__ __forceinline__ void item_few(const AttendArgs& a, Smem& s, const Ite
         }
       }
       *reinterpret_cast<float4*>(out + r * kD + lane * 4) = o;
-      __syncwarp();
-      if (lane == 0) {
+      if (lane == 0) {  // (every lane has read the old ones, and sees these past the barrier: the next row may be this one)
         mx[r] = mn;
         sum[r] = l;
       }
+      __syncwarp();
     }
   }
   __syncthreads();

@@ -521,3 +521,14 @@ def test_attend_scores_that_jump(dt):
     heads[2][0][:64] = (-100 * u).to(T)                               # the first keys far below
     pre = E.Prefix(*(torch.stack([h[i] for h in heads]).cuda() for i in range(2)))
     check_attend(b, heads, pre, h_kv, dt, q=q)
+
+
+@pytest.mark.parametrize("dt,flags", [("f32", 0), ("bf16", E.ECOKV_FLAG_FORCE_SIMT)])
+@pytest.mark.parametrize("h,lens,rows", [(8, [700], 0), (32, [1, 129, 4000, 260], 1300), (1, [5000], 20000)])
+def test_attend_one_row_an_item_over_many_tiles(h, lens, rows, dt, flags):
+    """A head of its own a query head, one token a sequence: a row's maximum and sum pass from tile to tile with no other row between."""
+    b = Batch(29, h, [1] * len(lens), lens, 16, dt)
+    g = gen(71)
+    heads, pre = make_prefix(g, [rows] * h, dt, False)
+    q = (2 * torch.randn(len(lens), h, D, generator=g)).to(TYPES[dt])
+    check_attend(b, heads, pre if rows else None, h, dt, q=q, flags=flags)
