@@ -447,7 +447,8 @@ def evict_noalloc(p, K, V, Qwin, want_scores=False, stream=None):
 
 # ---------------------------------------------------------------- the decode step
 # A call runs on `stream` (a torch.cuda.Stream or a raw handle), by default on
-# torch's current one.  Tensors that are not given are allocated by the helper.
+# torch's current one.  Tensors that are not given are allocated by the helper on
+# that stream; those that are given the caller has ordered with it.
 def rotary(rot_dim=HEAD_DIM, base=10000.0, layout="half", scaling="none", factor=1.0, original=0, sections=None,
            inv_freq=None, magnitude=1.0) -> ecokv_rotary:
     """Rotary positions of a model, kept for its calls.  scaling: "none",
@@ -543,8 +544,8 @@ def _rows(x, y, norm, what):
 _raw_stream = None
 
 
-def _on(stream, t, *made):
-    """The raw stream to launch on; tensors made here are kept from reuse until it is done with them."""
+def _on(stream, t):
+    """The raw stream to launch on."""
     if stream is None:
         global _raw_stream
         if _raw_stream is None:
@@ -552,12 +553,29 @@ def _on(stream, t, *made):
             # (torch.cuda.current_stream builds an object: 2 us of a call of 8)
             _raw_stream = torch._C._cuda_getCurrentRawStream
         return _raw_stream(t.get_device())
-    if isinstance(stream, int):
-        return stream
-    for x in made:
-        if x is not None:
-            x.record_stream(stream)
-    return stream.cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _made(stream, t, make):
+    """What make() allocates for a call on `stream` beside the tensor t: with that
+    stream current, so that it belongs to it (a fill, and whoever had the memory
+    before, come ahead of the call's kernels; memory that is given back is not used
+    again ahead of them), and kept until the caller's current stream is done with it."""
+    if stream is None:
+        return make()
+    import torch
+    if isinstance(stream, int):  # (0 and 1: the legacy default stream, which is torch's default one)
+        stream = torch.cuda.default_stream(t.device) if stream in (0, 1) else \
+            torch.cuda.ExternalStream(stream, device=t.device)
+    caller = torch.cuda.current_stream(t.device)
+    with torch.cuda.stream(stream):
+        x = make()
+    x.record_stream(caller)
+    return x
+
+
+def _like(x, stream):
+    return _made(stream, x, lambda: x.new_empty(x.shape))
 
 
 def rotate(rot, positions, q, k=None, q_norm=None, k_norm=None, eps=1e-6, q_out=None, k_out=None, stream=None):
@@ -566,13 +584,10 @@ def rotate(rot, positions, q, k=None, q_norm=None, k_norm=None, eps=1e-6, q_out=
     positions int32 [axes, tokens] (or [tokens]).  Outputs may have any strides
     (k_out a view of the [heads, tokens, 128] that the eviction pass reads) or be
     the inputs.  Returns (q_out, k_out)."""
-    made = []
     if q_out is None:
-        q_out = q.new_empty(q.shape)
-        made.append(q_out)
+        q_out = _like(q, stream)
     if k is not None and k_out is None:
-        k_out = k.new_empty(k.shape)
-        made.append(k_out)
+        k_out = _like(k, stream)
     dt = _dtype(q, k, q_norm, k_norm, q_out, k_out)
     tokens = q.shape[0]
     if k is not None and k.shape[0] != tokens:
@@ -580,7 +595,7 @@ def rotate(rot, positions, q, k=None, q_norm=None, k_norm=None, eps=1e-6, q_out=
     pos = _positions(rot, positions, tokens)
     _check((_lib or lib()).ecokv_rotate(rot, dt, _rows(q, q_out, q_norm, "q"),
                               None if k is None else _rows(k, k_out, k_norm, "k"), pos, tokens, eps,
-                              _on(stream, q, *made)), "ecokv_rotate")
+                              _on(stream, q)), "ecokv_rotate")
     return q_out, k_out
 
 
@@ -640,9 +655,8 @@ def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm
     cache's slots, q (normed, rotated) to q_out, which is returned.  starts int32
     [batch + 1]: None = one token a sequence.  ws: a workspace whose status word
     takes device-side errors."""
-    made = None
     if q is not None and q_out is None:
-        made = q_out = q.new_empty(q.shape)
+        q_out = _like(q, stream)
     dt = _dtype(k, v, cache.k_pages, q, q_norm, k_norm, q_out)
     tokens = k.shape[0]
     if v.shape != k.shape or k.shape[1] != cache.h_kv or (q is not None and q.shape[0] != tokens):
@@ -650,7 +664,7 @@ def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm
     _check((_lib or lib()).ecokv_append(rotary, dt, None if q is None else _rows(q, q_out, q_norm, "q"),
                               _rows(k, None, k_norm, "k"), _rows(v, None, None, "v"), cache.c,
                               _positions(rotary, positions, tokens), _ints(starts, (cache.batch + 1,), "starts"), tokens,
-                              cache.batch, eps, _ptr(ws), 0 if ws is None else ws.numel(), _on(stream, k, made)),
+                              cache.batch, eps, _ptr(ws), 0 if ws is None else ws.numel(), _on(stream, k)),
            "ecokv_append")
     return q_out
 
@@ -668,10 +682,8 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
     """Run ecokv_attend: q [tokens, h_q, 128] over prefix (a Prefix or None) and
     cache (a PagedCache or None); returns out [tokens, h_q, 128].  starts int32
     [batch + 1]: None = one token a sequence.  lse: float32 [tokens, h_q] to fill."""
-    made = []
     if out is None:
-        out = q.new_empty(q.shape)
-        made.append(out)
+        out = _like(q, stream)
     if prefix is None and cache is None:
         raise ValueError("a prefix or a cache is wanted")
     dt = _dtype(q, out, None if prefix is None else prefix.k, None if cache is None else cache.k_pages)
@@ -685,11 +697,10 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
                             not lse.is_contiguous() or not lse.is_cuda):
         raise ValueError("lse: a contiguous float32 [tokens, h_q] CUDA tensor is wanted")
     if ws is None:
-        ws = alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device)
-        made.append(ws)
+        ws = _made(stream, q, lambda: alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device))
     p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, qt, qh, ot, oh, flags, timeout_us)
     _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
                               None if cache is None else cache.c,
                               None if cache is None else _ints(starts, (batch + 1,), "starts"), out.data_ptr(),
-                              _ptr(lse), ws.data_ptr(), ws.numel(), _on(stream, q, *made)), "ecokv_attend")
+                              _ptr(lse), ws.data_ptr(), ws.numel(), _on(stream, q)), "ecokv_attend")
     return out

@@ -532,3 +532,32 @@ def test_attend_one_row_an_item_over_many_tiles(h, lens, rows, dt, flags):
     heads, pre = make_prefix(g, [rows] * h, dt, False)
     q = (2 * torch.randn(len(lens), h, D, generator=g)).to(TYPES[dt])
     check_attend(b, heads, pre if rows else None, h, dt, q=q, flags=flags)
+
+
+@pytest.mark.parametrize("how", ["stream", "handle", "default"])
+def test_helpers_allocate_in_the_order_of_the_stream_they_are_given(how):
+    """No workspace and no outputs given, while torch's current stream is busy with readers of memory it has given back."""
+    b = Batch(37, 4, [1] * 9, [50 * i + 1 for i in range(9)], 16, "bf16")
+    _, pre = make_prefix(gen(3), [900] * 4, "bf16", False)
+    q = torch.randn(9, 28, D, generator=gen(1)).bfloat16().cuda()
+    r, pos = E.rotary(128, 1e6), torch.arange(9, device="cuda").int()
+    want = E.attend(q, pre, b.cache), E.rotate(r, pos, q)[0]
+    side = torch.cuda.Stream()
+    stream = {"stream": side, "handle": side.cuda_stream, "default": 0}[how]
+    busy = side if how == "default" else torch.cuda.current_stream()
+    big = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(busy):
+            for _ in range(20):
+                big @ big
+            old = [torch.ones(9, 28, D, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+            kept = [x.clone() for x in old]
+            del old
+            got = E.attend(q, pre, b.cache, stream=stream), E.rotate(r, pos, q, stream=stream)[0]
+            again = E.attend(got[1], pre, b.cache, stream=stream)  # (its workspace may be the one given back)
+        (torch.cuda.default_stream() if how == "default" else side).synchronize()
+        assert all(torch.equal(x, w) for x, w in zip(got, want))
+        assert torch.equal(again, E.attend(want[1], pre, b.cache))
+        torch.cuda.synchronize()
+        assert all(bool((x == 1).all()) for x in kept)

@@ -1,0 +1,142 @@
+"""What the helpers make for a call on another stream: tensors are allocated (and
+filled) with that stream current, so that the fill and whatever used the memory
+before come ahead of the kernels, and outputs are kept from reuse until the
+caller's own stream is done with them.  Tensors, streams and the library are stand-ins:
+nothing is launched."""
+import contextlib
+import math
+
+import pytest
+import torch
+
+from paper_2609_06663_gb300 import ecokv as E
+
+D = 128
+
+
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class World:
+    """Torch's current stream, and a library that notes the calls it gets."""
+
+    def __init__(self):
+        self.here = self.current = Stream(0)
+        self.made, self.calls = [], []
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        before, self.current = self.current, s
+        yield
+        self.current = before
+
+    def __getattr__(self, name):  # the library's functions; sizes are asked for, the rest is launched
+        def call(*args):
+            if "workspace_size" in name:
+                return 4096
+            if "params" not in name:
+                self.calls.append((name, args))
+            return 0
+        return call
+
+
+class Tensor:
+    def __init__(self, world, *shape, dtype=torch.bfloat16, device="cuda:0"):
+        self.world, self.shape, self.dtype, self.device = world, shape, dtype, torch.device(device)
+        self.made_on, self.kept_for, self.is_cuda = world.current, [], True
+        world.made.append(self)
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def stride(self):
+        return tuple(math.prod(self.shape[i + 1:]) for i in range(len(self.shape)))
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+    def new_empty(self, shape):
+        return Tensor(self.world, *shape, dtype=self.dtype)
+
+    def record_stream(self, s):
+        self.kept_for.append(s)
+
+
+@pytest.fixture
+def world(monkeypatch):
+    w = World()
+
+    def make(*shape, dtype=None, device=None):
+        return Tensor(w, *(shape[0] if isinstance(shape[0], tuple) else shape), dtype=dtype)
+
+    monkeypatch.setattr(E, "_lib", w)
+    monkeypatch.setattr(E, "_raw_stream", lambda dev: w.current.cuda_stream)
+    monkeypatch.setattr(torch, "zeros", make)
+    monkeypatch.setattr(torch, "empty", make)
+    monkeypatch.setattr(torch.cuda, "stream", w.stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: w.current)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda dev=None: w.here)
+
+    def external(handle, device=None):
+        assert handle != 0  # (to torch that means any stream of its pool)
+        return Stream(handle)
+
+    monkeypatch.setattr(torch.cuda, "ExternalStream", external)
+    return w
+
+
+def decode_calls(w, stream):
+    t = lambda *n, **kw: Tensor(w, *n, **kw)  # noqa: E731
+    i32 = dict(dtype=torch.int32)
+    q, k, v = t(3, 8, D), t(3, 4, D), t(3, 4, D)
+    cache = E.PagedCache(t(10, 4, 16, D), t(10, 4, 16, D), t(3, 5, **i32), t(3, **i32))
+    rot = E.ecokv_rotary(rot_dim=D, axes=1)
+    pos = t(1, 3, **i32)
+    del w.made[:]
+    yield "ecokv_rotate", lambda: E.rotate(rot, pos, q, k, stream=stream), 2
+    yield "ecokv_append", lambda: (E.append(cache, k, v, None, rot, pos, q, stream=stream),), 1
+    yield "ecokv_attend", lambda: (E.attend(q, None, cache, stream=stream),), 1
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_decode_helpers_make_tensors_on_the_stream_of_the_call(world, raw):
+    side = Stream(4096)
+    for name, call, outs in decode_calls(world, 4096 if raw else side):
+        got = call()
+        assert world.calls[-1][0] == name and world.calls[-1][1][-1] == 4096
+        assert len(world.made) >= outs and world.current is world.here
+        for x in world.made:
+            assert x.made_on.cuda_stream == 4096, name
+        for x in got:
+            assert x in world.made and world.here in x.kept_for, name
+        del world.made[:]
+
+
+def test_decode_helpers_without_a_stream_run_on_torchs_current_one(world):
+    side = Stream(8192)
+    for name, call, outs in decode_calls(world, None):
+        with world.stream(side):
+            call()
+        assert world.calls[-1][0] == name and world.calls[-1][1][-1] == 8192
+        assert len(world.made) >= outs and all(x.made_on is side for x in world.made)
+        del world.made[:]
+
+
+def test_a_raw_handle_of_the_default_stream(world):
+    side = Stream(8192)
+    for name, call, _ in decode_calls(world, 0):
+        with world.stream(side):
+            call()
+        assert world.calls[-1][1][-1] == 0 and all(x.made_on is world.here for x in world.made), name
+        del world.made[:]
