@@ -7,6 +7,7 @@ library; the first call does, and raises if it is missing.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -326,82 +327,116 @@ def alloc_workspace(p: ecokv_params, device="cuda"):
     return ws
 
 
+# A call runs on `stream` (a torch.cuda.Stream or a raw handle), by default on
+# torch's current one.  Tensors that are not given are allocated by the helper on
+# that stream; those that are given the caller has ordered with it.
+@contextlib.contextmanager
+def _running(stream, device):
+    """A call on `stream`, which is current within: what is allocated there belongs
+    to it (a fill, and whoever had the memory before, come ahead of the call's
+    kernels; memory that is given back is not used again ahead of them).  Yields the
+    stream's raw handle and keep(), which keeps a tensor's memory until the caller's
+    current stream is done with it too."""
+    import torch
+    caller = torch.cuda.current_stream(device)
+    if stream is None:
+        yield caller.cuda_stream, lambda x: x
+        return
+    if isinstance(stream, int):  # (0 and 1: the legacy default stream, which is torch's default one)
+        stream = torch.cuda.default_stream(device) if stream in (0, 1) else \
+            torch.cuda.ExternalStream(stream, device=device)
+
+    def keep(x):
+        x.record_stream(caller)
+        return x
+
+    with torch.cuda.stream(stream):
+        yield stream.cuda_stream, keep
+
+
 def score(p, K, Qwin, ws=None, dbg=False, stream=None):
     """Run ecokv_score; returns (S [L,H,N-W], lambda [L,H], dbg or None)."""
     import torch
-    ws = alloc_workspace(p, K.device) if ws is None else ws
-    S = torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device)
-    lam = torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device)
-    D = torch.empty(p.n_layers, p.h_kv, 5, p.n - p.window, dtype=torch.float32, device=K.device) if dbg else None
-    _check(ecokv_score(p, dtype_code(K), K, Qwin, S, lam, D, ws, ws.numel(), stream), "ecokv_score")
-    return S, lam, D
+    with _running(stream, K.device) as (on, keep):
+        ws = alloc_workspace(p, K.device) if ws is None else ws
+        S = keep(torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device))
+        lam = keep(torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device))
+        D = keep(torch.empty(p.n_layers, p.h_kv, 5, p.n - p.window, dtype=torch.float32, device=K.device)) \
+            if dbg else None
+        _check(ecokv_score(p, dtype_code(K), K, Qwin, S, lam, D, ws, ws.numel(), on), "ecokv_score")
+        return S, lam, D
 
 
 def select(p, S, stream=None):
     import torch
-    idx = torch.empty(p.n_layers, p.h_kv, min(p.budget, p.n), dtype=torch.int32, device=S.device)
-    _check(ecokv_select(p, S, idx, None, 0, stream), "ecokv_select")
-    return idx
+    with _running(stream, S.device) as (on, keep):
+        idx = keep(torch.empty(p.n_layers, p.h_kv, min(p.budget, p.n), dtype=torch.int32, device=S.device))
+        _check(ecokv_select(p, S, idx, None, 0, on), "ecokv_select")
+        return idx
 
 
 def compact(p, K, V, idx, ws=None, stream=None):
     import torch
-    n_keep = min(p.budget, p.n)
-    Ko = torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device)
-    Vo = torch.empty_like(Ko)
-    _check(ecokv_compact(p, dtype_code(K), K, V, idx, Ko, Vo, ws, 0 if ws is None else ws.numel(), stream),
-           "ecokv_compact")
-    return Ko, Vo
+    with _running(stream, K.device) as (on, keep):
+        n_keep = min(p.budget, p.n)
+        Ko = keep(torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device))
+        Vo = keep(torch.empty_like(Ko))
+        _check(ecokv_compact(p, dtype_code(K), K, V, idx, Ko, Vo, ws, 0 if ws is None else ws.numel(), on),
+               "ecokv_compact")
+        return Ko, Vo
 
 
 def evict(p, K, V, Qwin, ws=None, want_scores=False, stream=None):
     """Run ecokv_evict; returns (idx, K_out, V_out, S or None, lambda)."""
     import torch
-    ws = alloc_workspace(p, K.device) if ws is None else ws
-    n_keep = min(p.budget, p.n)
-    idx = torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32, device=K.device)
-    Ko = torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device)
-    Vo = torch.empty_like(Ko)
-    S = torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device) \
-        if want_scores else None
-    lam = torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device)
-    _check(ecokv_evict(p, dtype_code(K), K, V, Qwin, idx, Ko, Vo, S, lam, ws, ws.numel(), stream),
-           "ecokv_evict")
-    return idx, Ko, Vo, S, lam
+    with _running(stream, K.device) as (on, keep):
+        ws = alloc_workspace(p, K.device) if ws is None else ws
+        n_keep = min(p.budget, p.n)
+        idx = keep(torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32, device=K.device))
+        Ko = keep(torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device))
+        Vo = keep(torch.empty_like(Ko))
+        S = keep(torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device)) \
+            if want_scores else None
+        lam = keep(torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device))
+        _check(ecokv_evict(p, dtype_code(K), K, V, Qwin, idx, Ko, Vo, S, lam, ws, ws.numel(), on),
+               "ecokv_evict")
+        return idx, Ko, Vo, S, lam
 
 
 def evict_adaptive(p, K, V, Qwin, ws=None, stream=None):
     """Run ecokv_evict_adaptive (layer-wide budget); returns (idx [L][h_kv*B],
     head_off [L][h_kv+1], K_out, V_out [L][h_kv*B][d], lambda)."""
     import torch
-    ws = alloc_workspace(p, K.device) if ws is None else ws
-    rows = p.h_kv * min(p.budget, p.n)
-    idx = torch.empty(p.n_layers, rows, dtype=torch.int32, device=K.device)
-    off = torch.empty(p.n_layers, p.h_kv + 1, dtype=torch.int32, device=K.device)
-    Ko = torch.empty(p.n_layers, rows, p.d, dtype=K.dtype, device=K.device)
-    Vo = torch.empty_like(Ko)
-    lam = torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device)
-    _check(ecokv_evict_adaptive(p, dtype_code(K), K, V, Qwin, idx, off, Ko, Vo, lam, ws, ws.numel(), stream),
-           "ecokv_evict_adaptive")
-    return idx, off, Ko, Vo, lam
+    with _running(stream, K.device) as (on, keep):
+        ws = alloc_workspace(p, K.device) if ws is None else ws
+        rows = p.h_kv * min(p.budget, p.n)
+        idx = keep(torch.empty(p.n_layers, rows, dtype=torch.int32, device=K.device))
+        off = keep(torch.empty(p.n_layers, p.h_kv + 1, dtype=torch.int32, device=K.device))
+        Ko = keep(torch.empty(p.n_layers, rows, p.d, dtype=K.dtype, device=K.device))
+        Vo = keep(torch.empty_like(Ko))
+        lam = keep(torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device))
+        _check(ecokv_evict_adaptive(p, dtype_code(K), K, V, Qwin, idx, off, Ko, Vo, lam, ws, ws.numel(), on),
+               "ecokv_evict_adaptive")
+        return idx, off, Ko, Vo, lam
 
 
 def evict_layered(p, K, V, Qwin, budgets, ws=None, want_scores=False, stream=None):
     """Run ecokv_evict_layered with budgets[l] for layer l (p.budget is the
     per-head stride, at least max(budgets)); returns as evict()."""
     import torch
-    ws = alloc_workspace(p, K.device) if ws is None else ws
-    n_keep = min(p.budget, p.n)
-    lb = torch.tensor(list(budgets), dtype=torch.int32)
-    idx = torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32, device=K.device)
-    Ko = torch.zeros(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device)
-    Vo = torch.zeros_like(Ko)
-    S = torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device) \
-        if want_scores else None
-    lam = torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device)
-    _check(ecokv_evict_layered(p, dtype_code(K), K, V, Qwin, lb.data_ptr(), idx, Ko, Vo, S, lam, ws, ws.numel(),
-                               stream), "ecokv_evict_layered")
-    return idx, Ko, Vo, S, lam
+    with _running(stream, K.device) as (on, keep):
+        ws = alloc_workspace(p, K.device) if ws is None else ws
+        n_keep = min(p.budget, p.n)
+        lb = torch.tensor(list(budgets), dtype=torch.int32)
+        idx = keep(torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32, device=K.device))
+        Ko = keep(torch.zeros(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device))
+        Vo = keep(torch.zeros_like(Ko))
+        S = keep(torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device)) \
+            if want_scores else None
+        lam = keep(torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device))
+        _check(ecokv_evict_layered(p, dtype_code(K), K, V, Qwin, lb.data_ptr(), idx, Ko, Vo, S, lam, ws, ws.numel(),
+                                   on), "ecokv_evict_layered")
+        return idx, Ko, Vo, S, lam
 
 
 def alloc_workspace_host(p, dtype, device="cuda"):
@@ -417,38 +452,37 @@ def evict_host(p, K, V, Qwin, ws=None, stream=None):
     """Run ecokv_evict_host on pinned host tensors; returns pinned host
     (idx, K_out, V_out, lambda), valid once the stream has been synchronised."""
     import torch
-    dt = dtype_code(K)
-    ws = alloc_workspace_host(p, dt) if ws is None else ws
-    n_keep = min(p.budget, p.n)
-    idx = torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32).pin_memory()
-    Ko = torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype).pin_memory()
-    Vo = torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype).pin_memory()
-    lam = torch.empty(p.n_layers, p.h_kv, dtype=torch.float32).pin_memory()
-    _check(ecokv_evict_host(p, dt, K, V, Qwin, idx, Ko, Vo, lam, ws, ws.numel(), stream), "ecokv_evict_host")
-    return idx, Ko, Vo, lam
+    with _running(stream, "cuda") as (on, _):
+        dt = dtype_code(K)
+        ws = alloc_workspace_host(p, dt) if ws is None else ws
+        n_keep = min(p.budget, p.n)
+        idx = torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32).pin_memory()
+        Ko = torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype).pin_memory()
+        Vo = torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype).pin_memory()
+        lam = torch.empty(p.n_layers, p.h_kv, dtype=torch.float32).pin_memory()
+        _check(ecokv_evict_host(p, dt, K, V, Qwin, idx, Ko, Vo, lam, ws, ws.numel(), on), "ecokv_evict_host")
+        return idx, Ko, Vo, lam
 
 
 def evict_noalloc(p, K, V, Qwin, want_scores=False, stream=None):
     """Run ecokv_evict_noalloc (library-held scratch, no workspace argument);
     returns (idx, K_out, V_out, S or None, lambda, device status code)."""
     import torch
-    n_keep = min(p.budget, p.n)
-    idx = torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32, device=K.device)
-    Ko = torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device)
-    Vo = torch.empty_like(Ko)
-    S = torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device) \
-        if want_scores else None
-    lam = torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device)
-    code = torch.full((1,), -1, dtype=torch.int32, device=K.device)
-    _check(ecokv_evict_noalloc(p, dtype_code(K), K, V, Qwin, idx, Ko, Vo, S, lam, code, stream),
-           "ecokv_evict_noalloc")
-    return idx, Ko, Vo, S, lam, int(code.item())
+    with _running(stream, K.device) as (on, keep):
+        n_keep = min(p.budget, p.n)
+        idx = keep(torch.empty(p.n_layers, p.h_kv, n_keep, dtype=torch.int32, device=K.device))
+        Ko = keep(torch.empty(p.n_layers, p.h_kv, n_keep, p.d, dtype=K.dtype, device=K.device))
+        Vo = keep(torch.empty_like(Ko))
+        S = keep(torch.empty(p.n_layers, p.h_kv, p.n - p.window, dtype=torch.float32, device=K.device)) \
+            if want_scores else None
+        lam = keep(torch.empty(p.n_layers, p.h_kv, dtype=torch.float32, device=K.device))
+        code = keep(torch.full((1,), -1, dtype=torch.int32, device=K.device))
+        _check(ecokv_evict_noalloc(p, dtype_code(K), K, V, Qwin, idx, Ko, Vo, S, lam, code, on),
+               "ecokv_evict_noalloc")
+        return idx, Ko, Vo, S, lam, int(code.item())
 
 
 # ---------------------------------------------------------------- the decode step
-# A call runs on `stream` (a torch.cuda.Stream or a raw handle), by default on
-# torch's current one.  Tensors that are not given are allocated by the helper on
-# that stream; those that are given the caller has ordered with it.
 def rotary(rot_dim=HEAD_DIM, base=10000.0, layout="half", scaling="none", factor=1.0, original=0, sections=None,
            inv_freq=None, magnitude=1.0) -> ecokv_rotary:
     """Rotary positions of a model, kept for its calls.  scaling: "none",
@@ -557,21 +591,11 @@ def _on(stream, t):
 
 
 def _made(stream, t, make):
-    """What make() allocates for a call on `stream` beside the tensor t: with that
-    stream current, so that it belongs to it (a fill, and whoever had the memory
-    before, come ahead of the call's kernels; memory that is given back is not used
-    again ahead of them), and kept until the caller's current stream is done with it."""
+    """What make() allocates for a call on `stream`, beside the tensor t."""
     if stream is None:
         return make()
-    import torch
-    if isinstance(stream, int):  # (0 and 1: the legacy default stream, which is torch's default one)
-        stream = torch.cuda.default_stream(t.device) if stream in (0, 1) else \
-            torch.cuda.ExternalStream(stream, device=t.device)
-    caller = torch.cuda.current_stream(t.device)
-    with torch.cuda.stream(stream):
-        x = make()
-    x.record_stream(caller)
-    return x
+    with _running(stream, t.device) as (_, keep):
+        return keep(make())
 
 
 def _like(x, stream):

@@ -72,18 +72,38 @@ class Tensor:
     def record_stream(self, s):
         self.kept_for.append(s)
 
+    def item(self):
+        assert self.world.current.cuda_stream == self.world.calls[-1][1][-1]  # else it would not wait for the call
+        return 0
+
+
+class Host:
+    """A tensor in host memory: not of any stream."""
+    dtype = torch.bfloat16
+
+    def pin_memory(self):
+        return self
+
+    def data_ptr(self):
+        return 1 << 20
+
 
 @pytest.fixture
 def world(monkeypatch):
     w = World()
 
     def make(*shape, dtype=None, device=None):
+        if device is None:
+            return Host()
         return Tensor(w, *(shape[0] if isinstance(shape[0], tuple) else shape), dtype=dtype)
 
     monkeypatch.setattr(E, "_lib", w)
     monkeypatch.setattr(E, "_raw_stream", lambda dev: w.current.cuda_stream)
     monkeypatch.setattr(torch, "zeros", make)
     monkeypatch.setattr(torch, "empty", make)
+    monkeypatch.setattr(torch, "full", lambda shape, value, dtype, device: make(shape, dtype=dtype, device=device))
+    for like in ("empty_like", "zeros_like"):
+        monkeypatch.setattr(torch, like, lambda x: x.new_empty(x.shape))
     monkeypatch.setattr(torch.cuda, "stream", w.stream)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: w.current)
     monkeypatch.setattr(torch.cuda, "default_stream", lambda dev=None: w.here)
@@ -139,4 +159,40 @@ def test_a_raw_handle_of_the_default_stream(world):
         with world.stream(side):
             call()
         assert world.calls[-1][1][-1] == 0 and all(x.made_on is world.here for x in world.made), name
+        del world.made[:]
+
+
+def evict_calls(w, stream):
+    p = E.ecokv_params(n_layers=1, h_kv=4, h_q=8, n=500, d=D, window=4, budget=50)
+    K, Q, S, idx = Tensor(w, 1, 4, 500, D), Tensor(w, 1, 8, 4, D), Tensor(w, 1, 4, 496), Tensor(w, 1, 4, 50)
+    kw = dict(stream=stream)
+    del w.made[:]
+    yield "ecokv_score", lambda: E.score(p, K, Q, dbg=True, **kw)
+    yield "ecokv_select", lambda: (E.select(p, S, **kw),)
+    yield "ecokv_compact", lambda: E.compact(p, K, K, idx, **kw)
+    yield "ecokv_evict", lambda: E.evict(p, K, K, Q, want_scores=True, **kw)
+    yield "ecokv_evict_adaptive", lambda: E.evict_adaptive(p, K, K, Q, **kw)
+    yield "ecokv_evict_layered", lambda: E.evict_layered(p, K, K, Q, [50], want_scores=True, **kw)
+    yield "ecokv_evict_host", lambda: E.evict_host(p, Host(), Host(), Host(), **kw)
+    yield "ecokv_evict_noalloc", lambda: E.evict_noalloc(p, K, K, Q, want_scores=True, **kw)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_eviction_helpers_make_tensors_on_the_stream_of_the_call(world, raw):
+    for name, call in evict_calls(world, 4096 if raw else Stream(4096)):
+        got = call()
+        assert world.calls[-1][0] == name and world.calls[-1][1][-1] == 4096 and world.current is world.here
+        assert world.made and all(x.made_on.cuda_stream == 4096 for x in world.made), name
+        outs = [x for x in got if isinstance(x, Tensor)]
+        assert (outs or name == "ecokv_evict_host") and all(world.here in x.kept_for for x in outs), name
+        del world.made[:]
+
+
+def test_eviction_helpers_without_a_stream_run_on_torchs_current_one(world):
+    side = Stream(8192)
+    for name, call in evict_calls(world, None):
+        with world.stream(side):
+            call()
+        assert world.calls[-1][0] == name and world.calls[-1][1][-1] == 8192, name
+        assert world.made and all(x.made_on is side for x in world.made), name
         del world.made[:]
