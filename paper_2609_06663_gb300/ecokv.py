@@ -327,6 +327,19 @@ def alloc_workspace(p: ecokv_params, device="cuda"):
     return ws
 
 
+_get_device = None
+
+
+def _current(dev):
+    """The library launches on the current device: dev is to be that one."""
+    global _get_device
+    if _get_device is None:
+        import torch
+        _get_device = torch._C._cuda_getDevice
+    if dev != _get_device():
+        raise ValueError(f"tensors on cuda:{dev}, while cuda:{_get_device()} is the current device")
+
+
 # A call runs on `stream` (a torch.cuda.Stream or a raw handle), by default on
 # torch's current one.  Tensors that are not given are allocated by the helper on
 # that stream; those that are given the caller has ordered with it.
@@ -338,6 +351,8 @@ def _running(stream, device):
     stream's raw handle and keep(), which keeps a tensor's memory until the caller's
     current stream is done with it too."""
     import torch
+    if device != "cuda":
+        _current(device.index)
     caller = torch.cuda.current_stream(device)
     if stream is None:
         yield caller.cuda_stream, lambda x: x
@@ -524,16 +539,26 @@ _codes = {}  # torch dtype -> code
 _int32 = None
 
 
-def _ints(x, shape, what):
+def _ints(x, shape, what, dev):
     global _int32
     if x is None:
         return None
     if _int32 is None:
         import torch
         _int32 = torch.int32
-    if x.dtype is not _int32 or not x.is_cuda or not x.is_contiguous() or (shape and x.shape != shape):
-        raise ValueError(f"{what}: a contiguous int32 CUDA tensor{f' of shape {shape}' if shape else ''} is wanted")
+    if x.dtype is not _int32 or x.get_device() != dev or not x.is_contiguous() or (shape and x.shape != shape):
+        of = f" of shape {shape}" if shape else ""
+        raise ValueError(f"{what}: a contiguous int32 tensor{of} on cuda:{dev} is wanted")
     return x.data_ptr()
+
+
+def _workspace(ws, dev):
+    """A workspace's address and bytes."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev:
+        raise ValueError(f"the workspace is on {ws.device}, the tensors on cuda:{dev}")
+    return ws.data_ptr(), ws.numel()
 
 
 def _strides(x):
@@ -580,13 +605,15 @@ _raw_stream = None
 
 def _on(stream, t):
     """The raw stream to launch on."""
+    dev = t.get_device()
+    _current(dev)
     if stream is None:
         global _raw_stream
         if _raw_stream is None:
             import torch
             # (torch.cuda.current_stream builds an object: 2 us of a call of 8)
             _raw_stream = torch._C._cuda_getCurrentRawStream
-        return _raw_stream(t.get_device())
+        return _raw_stream(dev)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -616,14 +643,14 @@ def rotate(rot, positions, q, k=None, q_norm=None, k_norm=None, eps=1e-6, q_out=
     tokens = q.shape[0]
     if k is not None and k.shape[0] != tokens:
         raise ValueError("q and k have different numbers of tokens")
-    pos = _positions(rot, positions, tokens)
+    pos = _positions(rot, positions, tokens, q.get_device())
     _check((_lib or lib()).ecokv_rotate(rot, dt, _rows(q, q_out, q_norm, "q"),
                               None if k is None else _rows(k, k_out, k_norm, "k"), pos, tokens, eps,
                               _on(stream, q)), "ecokv_rotate")
     return q_out, k_out
 
 
-def _positions(rot, positions, tokens):
+def _positions(rot, positions, tokens, dev):
     if rot is None:
         return None
     if positions is None:
@@ -631,7 +658,7 @@ def _positions(rot, positions, tokens):
     n, axes = positions.shape, rot.axes
     if n[-1] != tokens or (n[0] != axes or len(n) != 2) and (len(n) != 1 or axes != 1):
         raise ValueError(f"positions: [{axes}, {tokens}] is wanted")
-    return _ints(positions, None, "positions")
+    return _ints(positions, None, "positions", dev)
 
 
 class PagedCache:
@@ -642,6 +669,7 @@ class PagedCache:
 
     def __init__(self, k_pages, v_pages, table, lengths):
         _dtype(k_pages, v_pages)
+        dev = k_pages.get_device()
         s = _strides(k_pages)
         if k_pages.dim() != 4 or k_pages.shape[3] != HEAD_DIM or s[3] != 1:
             raise ValueError(f"pages [n_pages, h_kv, page_size, {HEAD_DIM}] with the last axis contiguous are wanted")
@@ -652,8 +680,8 @@ class PagedCache:
         self.k_pages, self.v_pages, self.table, self.lengths = k_pages, v_pages, table, lengths
         self.batch, self.h_kv = table.shape[0], k_pages.shape[1]
         self.c = ecokv_pages(k_pages.data_ptr(), v_pages.data_ptr(), s[0], s[1], s[2], k_pages.shape[0],
-                             k_pages.shape[2], _ints(table, None, "table"), table.shape[1],
-                             _ints(lengths, None, "lengths"))
+                             k_pages.shape[2], _ints(table, None, "table", dev), table.shape[1],
+                             _ints(lengths, None, "lengths", dev))
 
 
 class Prefix:
@@ -670,7 +698,7 @@ class Prefix:
         self.k, self.v, self.head_off = k, v, head_off
         self.h_kv = k.shape[0] if head_off is None else head_off.shape[0] - 1
         self.c = ecokv_prefix(k.data_ptr(), v.data_ptr(), s[0] if head_off is None else 0, s[-2], k.shape[-2],
-                              _ints(head_off, None, "head_off"))
+                              _ints(head_off, None, "head_off", k.get_device()))
 
 
 def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm=None, k_norm=None, eps=1e-6,
@@ -685,10 +713,13 @@ def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm
     tokens = k.shape[0]
     if v.shape != k.shape or k.shape[1] != cache.h_kv or (q is not None and q.shape[0] != tokens):
         raise ValueError("k, v and q do not fit together or the cache")
+    dev = k.get_device()
+    at, n = _workspace(ws, dev)
     _check((_lib or lib()).ecokv_append(rotary, dt, None if q is None else _rows(q, q_out, q_norm, "q"),
                               _rows(k, None, k_norm, "k"), _rows(v, None, None, "v"), cache.c,
-                              _positions(rotary, positions, tokens), _ints(starts, (cache.batch + 1,), "starts"), tokens,
-                              cache.batch, eps, _ptr(ws), 0 if ws is None else ws.numel(), _on(stream, k)),
+                              _positions(rotary, positions, tokens, dev),
+                              _ints(starts, (cache.batch + 1,), "starts", dev), tokens, cache.batch, eps, at, n,
+                              _on(stream, k)),
            "ecokv_append")
     return q_out
 
@@ -717,14 +748,16 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
     if to != tokens or ho != h_q or (prefix is not None and prefix.h_kv != h_kv):
         raise ValueError("out or the prefix does not fit")
     batch = 1 if cache is None else cache.batch
+    dev = q.get_device()
     if lse is not None and (str(lse.dtype) != "torch.float32" or tuple(lse.shape) != (tokens, h_q) or
-                            not lse.is_contiguous() or not lse.is_cuda):
-        raise ValueError("lse: a contiguous float32 [tokens, h_q] CUDA tensor is wanted")
+                            not lse.is_contiguous() or lse.get_device() != dev):
+        raise ValueError(f"lse: a contiguous float32 [tokens, h_q] tensor on cuda:{dev} is wanted")
     if ws is None:
         ws = _made(stream, q, lambda: alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device))
+    at, n = _workspace(ws, dev)
     p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, qt, qh, ot, oh, flags, timeout_us)
     _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
                               None if cache is None else cache.c,
-                              None if cache is None else _ints(starts, (batch + 1,), "starts"), out.data_ptr(),
-                              _ptr(lse), ws.data_ptr(), ws.numel(), _on(stream, q)), "ecokv_attend")
+                              None if cache is None else _ints(starts, (batch + 1,), "starts", dev), out.data_ptr(),
+                              _ptr(lse), at, n, _on(stream, q)), "ecokv_attend")
     return out

@@ -1,8 +1,10 @@
-"""What the helpers make for a call on another stream: tensors are allocated (and
-filled) with that stream current, so that the fill and whatever used the memory
-before come ahead of the kernels, and outputs are kept from reuse until the
-caller's own stream is done with them.  Tensors, streams and the library are stand-ins:
-nothing is launched."""
+"""Streams and devices of the helpers' calls.
+
+What the helpers make for a call on another stream is allocated (and filled)
+with that stream current, so that the fill and whatever used the memory before come
+ahead of the kernels, and outputs are kept from reuse until the caller's own stream is
+done with them.  Calls on another device than the current one are refused.  Tensors,
+streams and the library are stand-ins: nothing is launched."""
 import contextlib
 import math
 
@@ -24,7 +26,7 @@ class World:
 
     def __init__(self):
         self.here = self.current = Stream(0)
-        self.made, self.calls = [], []
+        self.made, self.calls, self.device = [], [], 0
 
     @contextlib.contextmanager
     def stream(self, s):
@@ -61,7 +63,7 @@ class Tensor:
         return 1 << 20
 
     def get_device(self):
-        return 0
+        return -1 if self.device.type == "cpu" else self.device.index
 
     def is_contiguous(self):
         return True
@@ -99,6 +101,7 @@ def world(monkeypatch):
 
     monkeypatch.setattr(E, "_lib", w)
     monkeypatch.setattr(E, "_raw_stream", lambda dev: w.current.cuda_stream)
+    monkeypatch.setattr(E, "_get_device", lambda: w.device, raising=False)
     monkeypatch.setattr(torch, "zeros", make)
     monkeypatch.setattr(torch, "empty", make)
     monkeypatch.setattr(torch, "full", lambda shape, value, dtype, device: make(shape, dtype=dtype, device=device))
@@ -196,3 +199,48 @@ def test_eviction_helpers_without_a_stream_run_on_torchs_current_one(world):
         assert world.calls[-1][0] == name and world.calls[-1][1][-1] == 8192, name
         assert world.made and all(x.made_on is side for x in world.made), name
         del world.made[:]
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_calls_on_another_device_than_the_current_one_are_refused(world, own_stream):
+    """The library launches on the current device: a stream of another one's tensors would not be that device's."""
+    stream = Stream(4096) if own_stream else None
+    calls = [c[:2] for c in decode_calls(world, stream)]
+    calls += [c for c in evict_calls(world, stream) if c[0] != "ecokv_evict_host"]  # (host tensors)
+    world.device = 1
+    for name, call in calls:
+        with pytest.raises(ValueError):
+            call()
+        assert not world.calls, name
+
+
+@pytest.mark.parametrize("where", ["cuda:1", "cpu"])
+def test_every_tensor_of_a_call_is_on_its_device(world, where):
+    t = lambda *n, **kw: Tensor(world, *n, **kw)  # noqa: E731
+    i32, there = dict(dtype=torch.int32), dict(device=where)
+    u8, f32 = dict(dtype=torch.uint8), dict(dtype=torch.float32)
+    q, k = t(3, 8, D), t(3, 4, D)
+    pages, table, lengths = t(10, 4, 16, D), t(3, 5, **i32), t(3, **i32)
+    cache = E.PagedCache(pages, pages, table, lengths)
+    rot, pos = E.ecokv_rotary(rot_dim=D, axes=1), t(1, 3, **i32)
+    refused = [
+        lambda: E.rotate(rot, t(1, 3, **i32, **there), q),
+        lambda: E.append(cache, k, k, None, rot, t(1, 3, **i32, **there)),
+        lambda: E.append(cache, k, k, t(4, **i32, **there)),
+        lambda: E.append(cache, k, k, ws=t(4096, **u8, **there)),
+        lambda: E.attend(q, None, cache, t(4, **i32, **there)),
+        lambda: E.attend(q, None, cache, lse=t(3, 8, **f32, **there)),
+        lambda: E.attend(q, None, cache, ws=t(4096, **u8, **there)),
+        lambda: E.PagedCache(pages, pages, t(3, 5, **i32, **there), lengths),
+        lambda: E.PagedCache(pages, pages, table, t(3, **i32, **there)),
+        lambda: E.Prefix(t(30, D), t(30, D), t(5, **i32, **there)),
+    ]
+    for i, call in enumerate(refused):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(str(i))
+        assert not world.calls, i
+    E.rotate(rot, pos, q)
+    E.append(cache, k, k, t(4, **i32), rot, pos, ws=t(4096, **u8))
+    E.attend(q, None, cache, t(4, **i32), lse=t(3, 8, **f32), ws=t(4096, **u8))
+    assert len(world.calls) == 3
