@@ -18,7 +18,8 @@
  * `stream`, device-side errors in the workspace's status word
  * (ecokv_device_status), calls that share a workspace ordered on one stream.
  * Rows are d = 128 contiguous elements at 16-byte aligned addresses; strides
- * count elements and are positive multiples of 16 bytes.  Data on the device
+ * count elements and are positive multiples of 16 bytes (those of ecokv_rows' x, which
+ * is only read, may be zero or negative too).  An output's rows do not overlap.  Data on the device
  * (positions, lengths, page numbers) is read on the device, so a call can be captured
  * in a graph and replayed as they change.  A call of no tokens does nothing, whatever
  * its pointers.
@@ -75,7 +76,7 @@ ecokv_status ecokv_rotary_sections(ecokv_rotary* r, const int32_t* counts, int32
 typedef struct {
   const void* x;
   void* y;
-  int64_t x_token, x_head; /* strides of x */
+  int64_t x_token, x_head; /* strides of x; 0: one row for all */
   int64_t y_token, y_head; /* strides of y */
   const void* norm;        /* [d] weights (dtype) of x / sqrt(mean(x^2) + eps) * weight, or NULL: no norm */
   int32_t heads;

@@ -377,7 +377,9 @@ bool rows_ok(const ecokv_rows* s, size_t e, bool out) {
   if (s == nullptr) return true;
   if (s->heads < 1 || s->heads > (1 << 16) || !s->x || !aligned16(s->x) || !aligned16(s->norm)) return false;
   if (!stride_ok(s->x_token, e) || !stride_ok(s->x_head, e)) return false;
-  if (out && (!s->y || !aligned16(s->y) || !stride_ok(s->y_token, e) || !stride_ok(s->y_head, e))) return false;
+  if (out && (!s->y || !aligned16(s->y) || s->y_token <= 0 || s->y_head <= 0 || !stride_ok(s->y_token, e) ||
+              !stride_ok(s->y_head, e)))
+    return false;
   return true;
 }
 

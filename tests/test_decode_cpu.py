@@ -182,3 +182,12 @@ def test_helpers_want_cuda_tensors():
         E.PagedCache(torch.zeros(3, 4, 8, 128), torch.zeros(3, 4, 8, 128), torch.zeros(2, 2, dtype=torch.int32),
                      torch.zeros(2, dtype=torch.int32))
     assert ctypes.sizeof(E.ecokv_rotary) == 16 + 64 * 8 + 64
+
+
+@pytest.mark.parametrize("kw", [dict(y_token=0), dict(y_head=0), dict(y_token=-512), dict(y_head=-128)])
+def test_outputs_have_positive_strides(kw):
+    """A stride of zero would have an output's rows race for one address."""
+    r, c = E.rotary(), pages()
+    assert E.ecokv_rotate(r, 1, rows(**kw), None, FAKE, 3, 1e-6) == 1
+    assert E.ecokv_rotate(r, 1, None, rows(**kw), FAKE, 3, 1e-6) == 1
+    assert E.ecokv_append(r, 1, rows(**kw), rows(), rows(), c, FAKE, None, 2, 2, 1e-6, FAKE, 256) == 1

@@ -561,3 +561,23 @@ def test_helpers_allocate_in_the_order_of_the_stream_they_are_given(how):
         assert torch.equal(again, E.attend(want[1], pre, b.cache))
         torch.cuda.synchronize()
         assert all(bool((x == 1).all()) for x in kept)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_rows_that_are_read_may_be_broadcast(dt):
+    """One row for every token, or every head: the same as their copies.  An output cannot be one."""
+    g, T = gen(81), TYPES[dt]
+    r, pos = E.rotary(128, 1e4), torch.arange(40).int().cuda()
+    w = (1 + 0.3 * torch.randn(D, generator=g)).to(T).cuda()
+    for shape in ((1, 6, D), (40, 1, D), (1, 1, D)):
+        x = torch.randn(shape, generator=g).to(T).cuda().expand(40, 6, D)
+        want = E.rotate(r, pos, x.contiguous(), q_norm=w)[0]
+        assert torch.equal(E.rotate(r, pos, x, q_norm=w)[0], want)
+        b = [Batch(83, 6, [40], [50], 16, dt) for _ in range(2)]
+        for c, k in zip(b, (x, x.contiguous())):
+            E.append(c.cache, k, k, c.starts.cuda(), r, pos)
+        assert torch.equal(b[0].dk.nan_to_num(), b[1].dk.nan_to_num())
+        assert torch.equal(b[0].dv.nan_to_num(), b[1].dv.nan_to_num())
+        with pytest.raises(E.EcokvError) as e:
+            E.rotate(r, pos, want, q_out=x)
+        assert e.value.code == E.ECOKV_ERR_INVALID_ARG
