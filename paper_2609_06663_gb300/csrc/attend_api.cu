@@ -7,6 +7,7 @@
 
 #include "attend.cuh"
 #include "decode_ptx.cuh"
+#include "tc_tile.cuh"
 
 namespace ecokv {
 namespace {
@@ -143,8 +144,11 @@ __device__ __forceinline__ void store_row(const AttendArgs& a, int token, int hq
   acc.z *= inv;
   acc.w *= inv;
   store4(static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)hq * a.out_head + 4 * lane, acc);
-  if (a.lse != nullptr && lane == 0)
-    a.lse[(int64_t)token * a.h_q + hq] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  if (a.lse != nullptr && lane == 0) {
+    // (L is at least 1/2 unless it is 0; infinite or NaN only where an input was)
+    const float x = L < INFINITY ? log2_sum(M, L) : L;
+    a.lse[(int64_t)token * a.h_q + hq] = L == 0.f ? -INFINITY : x * 0.6931471805599453f;
+  }
 }
 
 constexpr int kAhead = 32 / kJoinWarps;  // sums whose loads a warp has in flight

@@ -581,3 +581,36 @@ def test_rows_that_are_read_may_be_broadcast(dt):
         with pytest.raises(E.EcokvError) as e:
             E.rotate(r, pos, want, q_out=x)
         assert e.value.code == E.ECOKV_ERR_INVALID_ARG
+
+
+def jump_rows(dt, low, at=(40, 77, 149), own=(1.0, 1.0, 1.0), heads=33):
+    """One KV head, a query head a row, scores exact in any order of sums: `low` for the first 40 keys, then three of
+    a row's own (`own` / 16 times -16 .. 16), in units of log2 at the scale returned with them."""
+    scale = float(torch.tensor(0.0625 / math.log2(math.e), dtype=torch.float32))
+    assert float(torch.tensor(math.log2(math.e) * scale, dtype=torch.float32)) == 0.0625
+    T, n = TYPES[dt], 150
+    q = torch.zeros(1, heads, D)
+    q[0, :, 0] = torch.arange(heads) - heads // 2
+    q[0, :, 1] = 32
+    k = torch.zeros(n, D)
+    k[:, 1] = low / 2            # 32 x low / 2 / 16
+    k[list(at), 0] = torch.tensor(own)
+    k[list(at), 1] = 0
+    return q.to(T), k.to(T), scale
+
+
+@pytest.mark.parametrize("dt,flags", [("bf16", 0), ("bf16", E.ECOKV_FLAG_FORCE_SIMT), ("f32", 0)])
+@pytest.mark.parametrize("low", [-63, -60, -15, -3])
+def test_attend_log_sum_near_zero(low, dt, flags):
+    """Sums near one whose first keys lie far below: the logarithm is rounded as a number of its own size, not of the
+    first keys'.  An exponential is off by 2^-22, a sum of the few weights that count by 3 u and the lower ones'
+    share, the logarithm of a mantissa by 2 u, the result (2 at most, times ln 2) by 4 u more."""
+    # (in one tile of keys: the largest of another's would be the reference)
+    q, k, scale = jump_rows(dt, low, (40, 77, 120), (1.0, 2.0, -1.0))
+    v = torch.randn(k.shape, generator=gen(91)).to(TYPES[dt])
+    pre = E.Prefix(k[None].cuda(), v[None].cuda())
+    lse = torch.zeros(1, q.shape[1], device="cuda")
+    E.attend(q.cuda(), pre, None, scale=scale, lse=lse, flags=flags)
+    want = torch.logsumexp(q[0].double() @ k.double().t() * scale, -1)
+    err = (lse[0].cpu().double() - want).abs()
+    assert bool((err <= 2.0 ** -22 + 9 * U + 150 * U * 2.0 ** (low + 1)).all()), float(err.max())
