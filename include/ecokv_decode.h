@@ -162,7 +162,9 @@ size_t ecokv_attend_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, i
  * A row that sees no key: out = 0, lse = -inf.  Scores, maxima, sums and the
  * output are fp32; for bf16 the softmax weights are rounded to bf16 for the
  * second product, as their factor V is.  q, the prefix and the slots in use must
- * be finite.  The result is deterministic.  A page number out of range reads as
+ * be finite, and V below 2^86 in magnitude (fp32, and bf16 on CUDA cores: 2^102): the
+ * sums before the division are fp32, of weights up to 2^16 (there: 1).  The result is
+ * deterministic.  A page number out of range reads as
  * zeros, a length out of range is clamped, offsets out of order are clamped;
  * each sets ECOKV_ERR_DEVICE_INDEX in the workspace's status word.
  * ECOKV_ERR_UNSUPPORTED: d != 128, h_q / h_kv > 64, more than 2^31 tiles of 128

@@ -30,7 +30,9 @@ constexpr int kThreads = 384;
 constexpr int kStages = 5;          // tiles of K or V in the ring
 constexpr int kItems = 4;           // items ahead of their consumers
 constexpr uint32_t kHalf = kTileBytes / 2;  // 128 rows x 64 columns
-constexpr float kRaise = 64.f;      // log2 units: weights up to 2^64, sums of 2^24 of them far below 2^127
+// log2 units: weights up to 2^16, so that a sum of 2^25 of them (the prefix's keys and a
+// sequence's own) with values below 2^86 stays below 2^127
+constexpr float kRaise = 16.f;
 
 struct Smem {
   uint8_t q[2][kTileBytes];

@@ -614,3 +614,13 @@ def test_attend_log_sum_near_zero(low, dt, flags):
     want = torch.logsumexp(q[0].double() @ k.double().t() * scale, -1)
     err = (lse[0].cpu().double() - want).abs()
     assert bool((err <= 2.0 ** -22 + 9 * U + 150 * U * 2.0 ** (low + 1)).all()), float(err.max())
+
+
+@pytest.mark.parametrize("dt,flags", [("bf16", 0), ("bf16", E.ECOKV_FLAG_FORCE_SIMT), ("f32", 0)])
+@pytest.mark.parametrize("low", [-63, -40, -17, -16, -15.5, -8])
+def test_attend_large_values_after_a_jump(low, dt, flags):
+    """Values near the bound of the header where the scores rise: the unnormalised sums stay finite."""
+    q, k, scale = jump_rows(dt, low)
+    v = (torch.randn(k.shape, generator=gen(92)).clamp(-4, 4) * 2.0 ** 83).to(TYPES[dt])
+    b = Batch(93, 1, [1], [0], 16, dt)
+    check_attend(b, [(k, v)], E.Prefix(k[None].cuda(), v[None].cuda()), q.shape[1], dt, q=q, flags=flags, scale=scale)
