@@ -167,8 +167,12 @@ size_t ecokv_attend_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, i
  * deterministic.  A page number out of range reads as
  * zeros, a length out of range is clamped, offsets out of order are clamped;
  * each sets ECOKV_ERR_DEVICE_INDEX in the workspace's status word.
- * ECOKV_ERR_UNSUPPORTED: d != 128, h_q / h_kv > 64, more than 2^31 tiles of 128
- * keys. */
+ * ECOKV_ERR_UNSUPPORTED: d != 128, h_q / h_kv > 64, or more work than 31 bits count:
+ *   h_kv (n u(rows) + (n + batch) u(page_size * table_stride)) >= 2^31, where
+ *   n = ceil(tokens / (2 floor(128 / group))) and u(keys) = 2 ceil(keys / 128) + 4
+ *   (fp32, and bf16 on CUDA cores: ceil(tokens / floor(64 / group)) and
+ *   ceil(keys / 128)); u(0) = 0, group = h_q / h_kv.  The room of the table counts,
+ *   not the lengths, which the host does not see. */
 ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const void* q, const ecokv_prefix* prefix,
                           const ecokv_pages* cache, const int32_t* starts, void* out, float* lse, void* ws,
                           size_t ws_bytes, void* stream);

@@ -150,7 +150,7 @@ struct Walk {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int u = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += u;
+      if (lane >= o) v = (int)((unsigned)v + (unsigned)u);  // (may wrap where begin() drops the sequences)
     }
     return v;
   }
@@ -197,9 +197,11 @@ struct Walk {
       for (int c = 0; c < a.batch; c += 32) {
         chunk(a, c, lead);
         if (lead && c + lane < a.batch) a.plan[PLAN_HEADS + a.h_kv + c + lane] = (int)sum + upto - w;
-        sum += __shfl_sync(0xffffffffu, upto, 31);
+        // (in 64 bits: starts that overlap may have every sequence hold all of the tokens)
+        sum += __reduce_add_sync(0xffffffffu, (unsigned)w & 0xffffu) +
+               ((long long)__reduce_add_sync(0xffffffffu, (unsigned)w >> 16) << 16);
       }
-      // (valid starts and lengths stay below this, as the host has checked)
+      // (valid starts stay below this, as the host has checked)
       if (sum * a.h_kv > 0x7fffffff - prefix_total) {
         if (lead && lane == 0) note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)a.batch);
         sum = 0;

@@ -366,8 +366,6 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
     a.cap = cache->page_size * cache->table_stride;
     a.starts = starts;
   }
-  if (ws == nullptr || !aligned16(ws) || ws_bytes < attend_layout(p->tokens, p->batch, p->h_q, p->h_kv, 2).total)
-    return ECOKV_ERR_WORKSPACE;
   a.q = q;
   a.out = out;
   a.lse = lse;
@@ -385,17 +383,19 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   a.parts = tc ? 2 : 1;
   a.lead = tc ? 1 : 0;
   a.stall = (p->flags & ECOKV_FLAG_TEST_STALL) ? 1 : 0;
-  a.P = attend_sms();
   const double scale = p->scale > 0.f ? (double)p->scale : 1.0 / sqrt((double)kD);
   a.scale_log2 = (float)(1.4426950408889634 * scale);
   a.timeout_ns = (p->timeout_us ? (unsigned long long)p->timeout_us : 2000000ull) * 1000ull;
-  // units of every item, counted in 32 bits by the kernels
-  a.groups = div_up(a.tokens, a.span);
+  // Units of every item, counted in 32 bits by the kernels: as many as there can be of the
+  // sequences' slots.  (A sequence's tokens make an item more than their share of the groups.)
+  a.groups = (a.tokens - 1) / a.span + 1;
   a.last = a.tokens - (a.groups - 1) * a.span;
-  const long long groups = a.groups;
-  const long long of_cap = item_units(a, tiles_of(a.cap), a.span), of_prefix = item_units(a, tiles_of(a.prefix.rows), a.span);
-  const long long units = a.h_kv * (groups * of_prefix + (groups + a.batch) * of_cap);
-  if (units > 0x7fffffff || groups * of_cap > (1 << 25)) return ECOKV_ERR_UNSUPPORTED;
+  const double groups = a.groups, of_cap = item_units(a, tiles_of(a.cap), a.span);
+  const double of_prefix = item_units(a, tiles_of(a.prefix.rows), a.span);
+  if (a.h_kv * (groups * of_prefix + (groups + a.batch) * of_cap) > 0x7fffffff) return ECOKV_ERR_UNSUPPORTED;
+  if (ws == nullptr || !aligned16(ws) || ws_bytes < attend_layout(p->tokens, p->batch, p->h_q, p->h_kv, 2).total)
+    return ECOKV_ERR_WORKSPACE;
+  a.P = attend_sms();
   char* w = static_cast<char*>(ws);
   const AttendLayout L = attend_layout(a.tokens, a.batch, a.h_q, a.h_kv, a.parts);
   a.status = reinterpret_cast<unsigned*>(w);

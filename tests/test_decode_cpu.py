@@ -191,3 +191,24 @@ def test_outputs_have_positive_strides(kw):
     assert E.ecokv_rotate(r, 1, rows(**kw), None, FAKE, 3, 1e-6) == 1
     assert E.ecokv_rotate(r, 1, None, rows(**kw), FAKE, 3, 1e-6) == 1
     assert E.ecokv_append(r, 1, rows(**kw), rows(), rows(), c, FAKE, None, 2, 2, 1e-6, FAKE, 256) == 1
+
+
+@pytest.mark.parametrize("dtype,flags", [(1, 0), (1, E.ECOKV_FLAG_FORCE_SIMT), (0, 0)])
+@pytest.mark.parametrize("group", [1, 7, 8, 64])
+@pytest.mark.parametrize("tokens,page,cols,rows", [(100000, 4096, 256, 0), (4096, 4096, 4096, 0), (1, 8, 1, 0),
+                                                   (10000, 16, 8192, 131072)])
+def test_attend_size_limit(tokens, page, cols, rows, group, dtype, flags):
+    """The header's count of work, met and passed by one sequence (no workspace is given: nothing is launched)."""
+    tc = dtype == 1 and not flags
+    n = -(-tokens // (2 * (128 // group) if tc else 64 // group))
+    u = lambda keys: (2 * -(-keys // 128) + 4 if tc else -(-keys // 128)) if keys else 0  # noqa: E731
+    h_kv = 2
+    most = ((2 ** 31 - 1) // h_kv - n * u(rows)) // u(page * cols) - n
+    assert most > 0
+    for batch, code in ((most, 3), (most + 1, 2)):
+        if batch >= 2 ** 31:
+            continue
+        p = params(h_q=h_kv * group, h_kv=h_kv, tokens=tokens, batch=batch, flags=flags)
+        c = pages(page_size=page, table_stride=cols, page_stride=h_kv * page * 128, head_stride=page * 128)
+        pre = prefix(rows=rows, head_stride=max(rows, 1) * 128)
+        assert E.ecokv_attend(p, dtype, FAKE, pre, c, FAKE, FAKE, None, FAKE, 0) == code, batch

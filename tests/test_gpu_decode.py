@@ -624,3 +624,34 @@ def test_attend_large_values_after_a_jump(low, dt, flags):
     v = (torch.randn(k.shape, generator=gen(92)).clamp(-4, 4) * 2.0 ** 83).to(TYPES[dt])
     b = Batch(93, 1, [1], [0], 16, dt)
     check_attend(b, [(k, v)], E.Prefix(k[None].cuda(), v[None].cuda()), q.shape[1], dt, q=q, flags=flags, scale=scale)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attend_room_of_the_table_does_not_count(dt):
+    """A table with room for 2^21 slots a sequence and many tokens: the same bits as with a table of the slots in use."""
+    g, page, n = gen(97), 4096, 4500
+    k, v = torch.randn(2, 4, 1, page, D, generator=g).to(TYPES[dt]).cuda()
+    q = torch.randn(n, 64, D, generator=g).to(TYPES[dt]).cuda()
+    lengths, starts = torch.tensor([5000, 10]).int().cuda(), torch.tensor([0, n - 10, n]).int().cuda()
+    out = []
+    for cols in (2, 512):
+        table = torch.full((2, cols), 2 ** 30, dtype=torch.int32)
+        table[0, :2], table[1, 0] = torch.tensor([2, 1]), 3
+        out.append(E.attend(q, None, E.PagedCache(k, v, table.cuda(), lengths), starts))
+    assert torch.equal(out[0], out[1]) and bool(out[0].float().abs().max() > 0.1)
+
+
+def test_attend_starts_that_overlap_past_32_bits():
+    """Starts that go up and down, so that each of many sequences holds all tokens: said in the status, no slot is read."""
+    # (16 of 32 sequences of 16384 tokens over 2^22 slots: 2^32 units of work and more, were they walked)
+    n, page, cols, batch = 16384, 4096, 1024, 32
+    k, v = torch.randn(2, 1, 1, page, D, generator=gen(98)).bfloat16().cuda()
+    q = torch.randn(n, 64, D, generator=gen(99)).bfloat16().cuda()
+    starts = torch.tensor([0, n] * (batch // 2) + [0]).int().cuda()
+    cache = E.PagedCache(k, v, torch.zeros(batch, cols, dtype=torch.int32, device="cuda"),
+                         torch.full((batch,), cols * page, dtype=torch.int32, device="cuda"))
+    ws = E.alloc_attend_workspace(n, batch, 64, 1, torch.bfloat16)
+    lse = torch.zeros(n, 64, device="cuda")
+    out = E.attend(q, None, cache, starts, ws=ws, lse=lse)
+    assert E.ecokv_device_status(ws) == E.ECOKV_ERR_DEVICE_INDEX
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
