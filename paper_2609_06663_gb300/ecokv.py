@@ -661,11 +661,20 @@ def _positions(rot, positions, tokens, dev):
     return _ints(positions, None, "positions", dev)
 
 
-class PagedCache:
+class _Handle:
+    """What the library was given the address of stays: a tensor in its place would not be read."""
+
+    def __setattr__(self, name, x):
+        if self.__dict__.get(name, x) is not x:
+            raise AttributeError(f"{name}: write into the tensor, or make a new {type(self).__name__}")
+        self.__dict__[name] = x
+
+
+class PagedCache(_Handle):
     """A paged cache: k_pages, v_pages [n_pages, h_kv, page_size, 128] (views of
     any strides, the same for both, the last axis contiguous), table int32
     [batch, pages a sequence], lengths int32 [batch].  Holds its tensors; table and
-    lengths are read on the device by every call."""
+    lengths are read on the device by every call, and written in place between them."""
 
     def __init__(self, k_pages, v_pages, table, lengths):
         _dtype(k_pages, v_pages)
@@ -684,7 +693,7 @@ class PagedCache:
                              _ints(lengths, None, "lengths", dev))
 
 
-class Prefix:
+class Prefix(_Handle):
     """The shared prefix of one layer: k, v [h_kv, rows, 128] as evict() returns a
     layer, or [rows, 128] with head_off int32 [h_kv + 1] as evict_adaptive() does."""
 

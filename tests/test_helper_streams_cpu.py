@@ -244,3 +244,17 @@ def test_every_tensor_of_a_call_is_on_its_device(world, where):
     E.append(cache, k, k, t(4, **i32), rot, pos, ws=t(4096, **u8))
     E.attend(q, None, cache, t(4, **i32), lse=t(3, 8, **f32), ws=t(4096, **u8))
     assert len(world.calls) == 3
+
+
+def test_handles_keep_the_tensors_whose_addresses_they_hold(world):
+    t = lambda *n, **kw: Tensor(world, *n, **kw)  # noqa: E731
+    i32 = dict(dtype=torch.int32)
+    cache = E.PagedCache(t(10, 4, 16, D), t(10, 4, 16, D), t(3, 5, **i32), t(3, **i32))
+    prefix = E.Prefix(t(30, D), t(30, D), t(5, **i32))
+    for handle, names in ((cache, ("k_pages", "v_pages", "table", "lengths")), (prefix, ("k", "v", "head_off"))):
+        for name in names:
+            x = getattr(handle, name)
+            with pytest.raises(AttributeError):
+                setattr(handle, name, t(*x.shape, dtype=x.dtype))
+            assert getattr(handle, name) is x
+            setattr(handle, name, x)  # (what an operation in place does: cache.lengths += 1)
