@@ -335,6 +335,10 @@ __device__ __forceinline__ size_t next_row(const AttendArgs& a, int cta, int j, 
   return ((size_t)cta * a.parts + j) * kTileRows + row;
 }
 
+// Argument checks of the decode step's entry points: addresses and strides (of elements
+// of e bytes) in whole 16 bytes.
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline bool stride_ok(int64_t s, size_t e) { return ((uint64_t)s * e & 15u) == 0; }
 ecokv_status check_pages(const ecokv_pages* c, int32_t batch, ecokv_dtype dt);
 cudaError_t launch_attend_simt(const AttendArgs& a, ecokv_dtype dt, cudaStream_t st);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st);

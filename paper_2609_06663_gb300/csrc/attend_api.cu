@@ -243,8 +243,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_row_kernel(const 
   store_row<T>(a, token, hq, lane, acc, M, L);
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-bool stride_ok(int64_t s, size_t e) { return ((uint64_t)s * e & 15u) == 0; }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct AttendLayout {

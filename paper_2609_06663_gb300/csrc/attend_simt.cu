@@ -203,8 +203,9 @@ __device__ __forceinline__ void item_few(const AttendArgs& a, Smem& s, const Ite
   }
 }
 
-template <typename T, int R>
+template <typename T>
 __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const Item& it) {
+  constexpr int R = kRows / 16;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31, warp = tid >> 5;
   const int rows = it.ntok * a.g;
   // queries
@@ -364,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_c
     if (s.more == 0) break;
     const Item it = s.item;
     if (it.ntok * a.g <= kFew) item_few<T>(a, s, it);
-    else item_rows<T, 4>(a, s, it);
+    else item_rows<T>(a, s, it);
   }
   ptx::grid_trigger();
 }

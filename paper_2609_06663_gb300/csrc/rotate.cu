@@ -360,9 +360,6 @@ __global__ void __launch_bounds__(kThreads, kResident) rotate_kernel(const __gri
   }
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-bool stride_ok(int64_t s, size_t e) { return ((uint64_t)s * e & 15u) == 0; }
-
 bool rotary_ok(const ecokv_rotary& r) {
   if (r.rot_dim < 16 || r.rot_dim > kD || r.rot_dim % 16 != 0) return false;
   if (r.layout != ECOKV_ROTARY_HALF && r.layout != ECOKV_ROTARY_INTERLEAVED) return false;
