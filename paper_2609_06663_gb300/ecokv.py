@@ -519,8 +519,8 @@ def rotary(rot_dim=HEAD_DIM, base=10000.0, layout="half", scaling="none", factor
     return r
 
 
-def _dtype(t, *others) -> int:
-    """Their common dtype's code; all of them on one CUDA device."""
+def _dtype(t, *others):
+    """Their common dtype's code and CUDA device."""
     dt, dev = t.dtype, t.get_device()
     if dev < 0:
         raise ValueError("CUDA tensors are wanted")
@@ -530,7 +530,7 @@ def _dtype(t, *others) -> int:
     code = _codes.get(dt)
     if code is None:
         code = _codes[dt] = dtype_code(t)
-    return code
+    return code, dev
 
 
 _codes = {}  # torch dtype -> code
@@ -550,15 +550,6 @@ def _ints(x, shape, what, dev):
         of = f" of shape {shape}" if shape else ""
         raise ValueError(f"{what}: a contiguous int32 tensor{of} on cuda:{dev} is wanted")
     return x.data_ptr()
-
-
-def _workspace(ws, dev):
-    """A workspace's address and bytes."""
-    if ws is None:
-        return None, 0
-    if ws.get_device() != dev:
-        raise ValueError(f"the workspace is on {ws.device}, the tensors on cuda:{dev}")
-    return ws.data_ptr(), ws.numel()
 
 
 def _strides(x):
@@ -603,10 +594,10 @@ def _rows(x, y, norm, what):
 _raw_stream = None
 
 
-def _on(stream, t):
+def _on(stream, dev):
     """The raw stream to launch on."""
-    dev = t.get_device()
-    _current(dev)
+    if _get_device is None or dev != _get_device():
+        _current(dev)
     if stream is None:
         global _raw_stream
         if _raw_stream is None:
@@ -639,14 +630,14 @@ def rotate(rot, positions, q, k=None, q_norm=None, k_norm=None, eps=1e-6, q_out=
         q_out = _like(q, stream)
     if k is not None and k_out is None:
         k_out = _like(k, stream)
-    dt = _dtype(q, k, q_norm, k_norm, q_out, k_out)
+    dt, dev = _dtype(q, k, q_norm, k_norm, q_out, k_out)
     tokens = q.shape[0]
     if k is not None and k.shape[0] != tokens:
         raise ValueError("q and k have different numbers of tokens")
-    pos = _positions(rot, positions, tokens, q.get_device())
+    pos = _positions(rot, positions, tokens, dev)
     _check((_lib or lib()).ecokv_rotate(rot, dt, _rows(q, q_out, q_norm, "q"),
                               None if k is None else _rows(k, k_out, k_norm, "k"), pos, tokens, eps,
-                              _on(stream, q)), "ecokv_rotate")
+                              _on(stream, dev)), "ecokv_rotate")
     return q_out, k_out
 
 
@@ -677,8 +668,7 @@ class PagedCache(_Handle):
     lengths are read on the device by every call, and written in place between them."""
 
     def __init__(self, k_pages, v_pages, table, lengths):
-        _dtype(k_pages, v_pages)
-        dev = k_pages.get_device()
+        _, dev = _dtype(k_pages, v_pages)
         s = _strides(k_pages)
         if k_pages.dim() != 4 or k_pages.shape[3] != HEAD_DIM or s[3] != 1:
             raise ValueError(f"pages [n_pages, h_kv, page_size, {HEAD_DIM}] with the last axis contiguous are wanted")
@@ -698,7 +688,7 @@ class Prefix(_Handle):
     layer, or [rows, 128] with head_off int32 [h_kv + 1] as evict_adaptive() does."""
 
     def __init__(self, k, v, head_off=None):
-        _dtype(k, v)
+        _, dev = _dtype(k, v)
         s = _strides(k)
         if k.dim() != (3 if head_off is None else 2) or k.shape[-1] != HEAD_DIM or s[-1] != 1:
             raise ValueError(f"prefix: [h_kv, rows, {HEAD_DIM}], or [rows, {HEAD_DIM}] with head_off, is wanted")
@@ -707,7 +697,7 @@ class Prefix(_Handle):
         self.k, self.v, self.head_off = k, v, head_off
         self.h_kv = k.shape[0] if head_off is None else head_off.shape[0] - 1
         self.c = ecokv_prefix(k.data_ptr(), v.data_ptr(), s[0] if head_off is None else 0, s[-2], k.shape[-2],
-                              _ints(head_off, None, "head_off", k.get_device()))
+                              _ints(head_off, None, "head_off", dev))
 
 
 def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm=None, k_norm=None, eps=1e-6,
@@ -718,17 +708,17 @@ def append(cache, k, v, starts=None, rotary=None, positions=None, q=None, q_norm
     takes device-side errors."""
     if q is not None and q_out is None:
         q_out = _like(q, stream)
-    dt = _dtype(k, v, cache.k_pages, q, q_norm, k_norm, q_out)
+    dt, dev = _dtype(k, v, cache.k_pages, q, q_norm, k_norm, q_out)
     tokens = k.shape[0]
     if v.shape != k.shape or k.shape[1] != cache.h_kv or (q is not None and q.shape[0] != tokens):
         raise ValueError("k, v and q do not fit together or the cache")
-    dev = k.get_device()
-    at, n = _workspace(ws, dev)
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"the workspace is on {ws.device}, the tensors on cuda:{dev}")
     _check((_lib or lib()).ecokv_append(rotary, dt, None if q is None else _rows(q, q_out, q_norm, "q"),
                               _rows(k, None, k_norm, "k"), _rows(v, None, None, "v"), cache.c,
                               _positions(rotary, positions, tokens, dev),
-                              _ints(starts, (cache.batch + 1,), "starts", dev), tokens, cache.batch, eps, at, n,
-                              _on(stream, k)),
+                              _ints(starts, (cache.batch + 1,), "starts", dev), tokens, cache.batch, eps, _ptr(ws),
+                              0 if ws is None else ws.numel(), _on(stream, dev)),
            "ecokv_append")
     return q_out
 
@@ -750,23 +740,23 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
         out = _like(q, stream)
     if prefix is None and cache is None:
         raise ValueError("a prefix or a cache is wanted")
-    dt = _dtype(q, out, None if prefix is None else prefix.k, None if cache is None else cache.k_pages)
+    dt, dev = _dtype(q, out, None if prefix is None else prefix.k, None if cache is None else cache.k_pages)
     tokens, h_q, qt, qh = _heads(q, "q")
     to, ho, ot, oh = _heads(out, "out")
     h_kv = prefix.h_kv if cache is None else cache.h_kv
     if to != tokens or ho != h_q or (prefix is not None and prefix.h_kv != h_kv):
         raise ValueError("out or the prefix does not fit")
     batch = 1 if cache is None else cache.batch
-    dev = q.get_device()
     if lse is not None and (str(lse.dtype) != "torch.float32" or tuple(lse.shape) != (tokens, h_q) or
                             not lse.is_contiguous() or lse.get_device() != dev):
         raise ValueError(f"lse: a contiguous float32 [tokens, h_q] tensor on cuda:{dev} is wanted")
     if ws is None:
         ws = _made(stream, q, lambda: alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device))
-    at, n = _workspace(ws, dev)
+    if ws.get_device() != dev:
+        raise ValueError(f"the workspace is on {ws.device}, the tensors on cuda:{dev}")
     p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, qt, qh, ot, oh, flags, timeout_us)
     _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
                               None if cache is None else cache.c,
                               None if cache is None else _ints(starts, (batch + 1,), "starts", dev), out.data_ptr(),
-                              _ptr(lse), at, n, _on(stream, q)), "ecokv_attend")
+                              _ptr(lse), ws.data_ptr(), ws.numel(), _on(stream, dev)), "ecokv_attend")
     return out
