@@ -156,17 +156,19 @@ size_t ecokv_attend_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, i
  * head's prefix and the slots j <= lengths[b] - T_b + i of the token's own
  * sequence: position enters through the rotation only.
  *   q, out : [tokens][h_q][d] (dtype), strides as in *p
- *   prefix : NULL = none
+ *   prefix : NULL = none.  One for all sequences of a call: sequences with prompts
+ *            of their own take a call each
  *   cache  : NULL = none (then starts is not used)
  *   lse    : out, float32 [tokens][h_q], ln of the sum of exponentials; may be NULL
- * A row that sees no key: out = 0, lse = -inf.  Scores, maxima, sums and the
- * output are fp32; for bf16 the softmax weights are rounded to bf16 for the
- * second product, as their factor V is.  q, the prefix and the slots in use must
- * be finite, and V below 2^86 in magnitude (fp32, and bf16 on CUDA cores: 2^102): the
- * sums before the division are fp32, of weights up to 2^16 (there: 1).  The result is
- * deterministic.  A page number out of range reads as
- * zeros, a length out of range is clamped, offsets out of order are clamped;
- * each sets ECOKV_ERR_DEVICE_INDEX in the workspace's status word.
+ * A row that sees no key: out = 0, lse = -inf; a token of no sequence (starts that do
+ * not reach it) sees the prefix alone.  Scores, maxima, sums and the output are fp32;
+ * for bf16 (but with ECOKV_FLAG_FORCE_SIMT) the softmax weights are rounded to bf16 for
+ * the second product, as their factor V is: 2^-9 of a weight.  q, the prefix and the
+ * slots in use must be finite, and V below 2^86 in magnitude (fp32, and bf16 on CUDA
+ * cores: 2^102): the sums before the division are fp32, of weights up to 2^16 (there: 1).
+ * The result is deterministic.  A page number out of range reads as zeros, a length
+ * out of range is clamped, offsets out of order are clamped; each sets
+ * ECOKV_ERR_DEVICE_INDEX in the workspace's status word.
  * ECOKV_ERR_UNSUPPORTED: d != 128, h_q / h_kv > 64, or more work than 31 bits count:
  *   h_kv (n u(rows) + (n + batch) u(page_size * table_stride)) >= 2^31, where
  *   n = ceil(tokens / (2 floor(128 / group))) and u(keys) = 2 ceil(keys / 128) + 4

@@ -286,8 +286,9 @@ template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
   // one CTA a row while all of them are resident (152 SMs of 8; the whole call at 1024
-  // rows: 94.1 us so, 98.0 by warps; at 1792: 62.3 and 60.5), past that as many rows a
-  // warp as leave 20 warps an SM (3696 rows, the whole call: 26.3 us, 27.2 at 10)
+  // rows, 32 tokens over 131072 keys: 93.8 us so, 97.5 by warps; at 1792, 64 sequences of
+  // up to 4096 slots: 62.4 and 60.5), past that as many rows a warp as leave 20 warps an SM
+  // (3696 rows, 132 single tokens over 3277: 32.6 us, 34.2 at 10)
   if (rows <= 152 * 8) return launch_behind(attend_join_row_kernel<T>, (unsigned)rows, 32 * kJoinWarps, 0, st, a);
   const long long want = rows / (152 * 20);
   const int per = (int)(want < 1 ? 1 : want > a.g ? a.g : want), split = div_up(a.g, per);

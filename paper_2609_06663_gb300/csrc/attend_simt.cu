@@ -8,12 +8,15 @@
 // 4c .. 4c + 3 of the sixteen rows of V.  Bound by those loads: the next tile's K is
 // on its way from the moment that this one's last scores are there.  The loop over
 // rows stays rolled, its sums in shared memory: a call of a few tiles runs its code
-// but once, and fetching code takes longer than running it (8 sequences of 8 heads,
-// three tokens each over 128 rows: 17.0 us, unrolled for eight rows with the sums in
-// registers 22.2; 13 single tokens over 1369 rows and 1252 of their own 40.7 and 89).
+// but once, and fetching code takes longer than running it (8 heads: 8 sequences of up
+// to three tokens over 128 rows 16.5 us, unrolled for eight rows with the sums in
+// registers 22.2; 13 single tokens over 1369 rows and up to 1252 of their own 40.3 and
+// 89).  A row is one chain of products, shuffles and exponential behind the other, and
+// a tile takes as long as its rows do, which the dealing does not count.
 //
-// Items of more rows, in groups of 64: a CTA of 256 threads holds an item's queries, a tile of 128 keys and its values
-// in shared memory as fp32.  Thread (ty, tx) of 16 x 16 forms the scores of its rows
+// Items of more rows, in groups of 64: a CTA of 256 threads holds an item's queries, a
+// tile of 128 keys and its values in shared memory as fp32 (82 tokens of 8 sequences, 28
+// heads over 4, 1369 rows and up to 300 of their own: 93 us, 19 TFLOP/s).  Thread (ty, tx) of 16 x 16 forms the scores of its rows
 // ty R .. ty R + R - 1 with the keys tx + 16 j, a row's maximum and sum are four
 // shuffles away, and the same thread then sums columns 4 tx .. and 64 + 4 tx .. of
 // its rows' outputs over the tile, which stay in registers through the item.
