@@ -11,6 +11,17 @@
  *   ecokv_attend   attention of the batch's new tokens over the shared prefix and
  *                  each sequence's own pages
  *
+ * Drafted tokens (speculative decoding) go through the same cache as a tree a sequence:
+ *
+ *   ecokv_tree_mask    which drafts each one sees: itself and its ancestors
+ *   ecokv_attend_tree  ecokv_attend with that mask in place of the causal one
+ *   ecokv_commit       the rows of the accepted drafts move to the front, the others are given up
+ *
+ * and a cache that has grown is made smaller again:
+ *
+ *   ecokv_weigh    adds the attention weight that each key gets to what it has had so far
+ *   ecokv_prune    keeps the heaviest slots of each head, the first ones and the last ones
+ *
  * The paper has no counterpart: they are the operators next to its pass.
  *
  * Conventions as in ecokv.h: device pointers of the caller's, no allocation,
@@ -22,7 +33,7 @@
  * is only read, may be zero or negative too).  An output's rows do not overlap.  Data on the device
  * (positions, lengths, page numbers) is read on the device, so a call can be captured
  * in a graph and replayed as they change.  A call of no tokens does nothing, whatever
- * its pointers.
+ * its pointers (ecokv_commit apart, whose sequences have lengths all the same).
  */
 #ifndef ECOKV_DECODE_H
 #define ECOKV_DECODE_H
@@ -178,6 +189,122 @@ size_t ecokv_attend_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, i
 ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const void* q, const ecokv_prefix* prefix,
                           const ecokv_pages* cache, const int32_t* starts, void* out, float* lse, void* ws,
                           size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ drafted tokens
+ * A sequence's new tokens i < T_b are drafts that follow each other as a tree: draft i
+ * goes on from draft parents[t] < i of its sequence, or, at -1, from the last token
+ * before them.  Its position is its parent's and one; its slot lengths[b] - T_b + i as
+ * for any new token, so ecokv_append puts it into the cache. */
+
+/* mask[t][words]: bit j % 64 of word j / 64 is set where draft t sees draft j of its
+ * sequence: j is t itself or an ancestor.
+ *   parents : int32 [tokens]
+ *   mask    : out, uint64 [tokens][words], 1 <= words <= 64
+ * Rows of tokens of no sequence are left as they were.  A parent out of range (not -1 ..
+ * i - 1) counts as -1, a draft from 64 * words on gets a row of zeros, and each sets
+ * ECOKV_ERR_DEVICE_INDEX in the status word of ws (may be NULL, else at least 256
+ * bytes). */
+ecokv_status ecokv_tree_mask(const int32_t* parents, const int32_t* starts, int32_t tokens, int32_t batch,
+                             uint64_t* mask, int32_t words, void* ws, size_t ws_bytes, void* stream);
+
+/* As ecokv_attend (its arguments, workspace and limits), where token i of sequence b sees
+ * the prefix, the slots below lengths[b] - T_b and those of the tokens j of its
+ * sequence whose bit is set in mask[t] (uint64 [tokens][words]): any bits, those of
+ * later tokens too.  Bits of j >= T_b are not read, tokens j >= 64 * words are not seen.
+ * cache and mask are wanted.  ECOKV_ERR_UNSUPPORTED: words > 64 too. */
+ecokv_status ecokv_attend_tree(const ecokv_attend_params* p, ecokv_dtype dtype, const void* q,
+                               const ecokv_prefix* prefix, const ecokv_pages* cache, const int32_t* starts,
+                               const uint64_t* mask, int32_t words, void* out, float* lse, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/* A float32 number of each row of a cache or a prefix (the attention weight that its key
+ * has had): of row (page, head, row) at page * page_stride + head * head_stride + row *
+ * slot_stride of w, of a prefix's row r of head h at h * head_stride + r * slot_stride (with
+ * head_off r * slot_stride).  Strides count elements and are positive. */
+typedef struct {
+  float* w;
+  int64_t page_stride, head_stride, slot_stride;
+} ecokv_weights;
+
+/* Accepted drafts: row lengths[b] - T_b + accepted[b][i] of K, V and, where given, the
+ * weights moves to row lengths[b] - T_b + i, i < counts[b], and lengths_out[b] = lengths[b]
+ * - T_b + counts[b].
+ *   accepted    : int32 [batch][stride], the drafts' numbers in their sequence, ascending
+ *                 (a path from the root does)
+ *   counts      : int32 [batch], 0 <= counts[b] <= T_b, stride
+ *   weights     : of the cache, or NULL
+ *   lengths_out : int32 [batch]; may be the cache's lengths, else it does not overlap them
+ * A sequence's pages with new tokens are its own.  A sequence with numbers out of
+ * range or out of order keeps none of its drafts (as with counts[b] = 0), a row whose
+ * page number is out of range is not moved, and each sets ECOKV_ERR_DEVICE_INDEX in the
+ * status word of ws (may be NULL, else at least 256 bytes).
+ * ECOKV_ERR_UNSUPPORTED: batch * h_kv > 2^29. */
+ecokv_status ecokv_commit(ecokv_dtype dtype, const ecokv_pages* cache, int32_t h_kv, const int32_t* accepted,
+                          int32_t stride, const int32_t* counts, const int32_t* starts, int32_t tokens, int32_t batch,
+                          const ecokv_weights* weights, int32_t* lengths_out, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ attention weights of keys */
+typedef struct {
+  int32_t h_q, h_kv, d, tokens, batch;  /* as in ecokv_attend_params */
+  float scale;
+  float decay;                          /* of the weights so far, finite, >= 0 */
+  int64_t q_token, q_head;
+  uint32_t flags;                       /* as in ecokv_attend_params */
+  uint32_t timeout_us;
+} ecokv_weigh_params;
+
+/* Bytes of workspace for `tokens` tokens of `batch` sequences (0: invalid). */
+size_t ecokv_weigh_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, int32_t h_kv, ecokv_dtype dtype);
+
+/* What every key is given by the new tokens' attention, added over the query heads of
+ * its KV head and the tokens that see it as in ecokv_attend:
+ *   A = decay * A + sum_{t,h} exp(scale q_t,h . k - lse[t][h])
+ * for every row of the prefix (over the tokens of all sequences) and every slot in
+ * use, where a new token's own slot starts at 0.  lse is what ecokv_attend has left; for
+ * drafts, once they are committed, that of the accepted ones (their ancestors are
+ * the tokens before them).  A row whose lse is -inf gives nothing, nor does a token of no
+ * sequence (without a cache: every token counts).
+ *   prefix, cache                    : either may be NULL; v is not read
+ *   prefix_weights, weights          : theirs, wanted where the prefix (cache) is; weights of slots
+ *                                      from lengths[b] on are left as they were
+ * Slots in use belong to one sequence each.  Sums are fp32 and in a fixed order: the
+ * result is deterministic.  q, lse and the keys in use must be finite (lse: or -inf).
+ * A call of no tokens changes nothing.
+ * Page numbers, lengths and offsets out of range: as for ecokv_attend; a slot without a
+ * page has no weight.  ECOKV_ERR_UNSUPPORTED: d, h_q / h_kv as for ecokv_attend, and
+ * more work than 62 bits count. */
+ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const void* q, const float* lse,
+                         const ecokv_prefix* prefix, const ecokv_pages* cache, const int32_t* starts,
+                         const ecokv_weights* prefix_weights, const ecokv_weights* weights, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* ------------------------------------------------------------------ pruning
+ * A sequence of more than `limit` slots keeps `budget` of them in each head: the
+ * `first` first ones, the `recent` last ones and between them the ones of the
+ * largest weights (of equal ones the lower slot; NaN counts below every number); its
+ * other heads choose for themselves.  The rows kept, in their order, take slots 0 ..
+ * of the same cache, or of another one.
+ *   0 <= first, 0 <= recent, first + recent <= budget, 1 <= budget <= limit
+ *   to          : NULL = the same cache; else one of the same dtype whose pages in use are no
+ *                 pages in use of `cache`; its table has entries for the rows kept, its
+ *                 lengths are not read.  Sequences of up to `limit` slots are copied whole.
+ *   to_weights  : where the kept rows' weights go (may be `weights`, in the same
+ *                 cache), NULL = they are not moved
+ *   idx         : out, int32 [batch][h_kv][limit], the kept slots, then -1
+ *   lengths_out : int32 [batch], min(budget or lengths[b]); may be the lengths of either cache
+ * Slots in use belong to one sequence each.  A slot whose page number is out of range has
+ * weight -inf and its row is not moved; a length out of range is clamped; each sets
+ * ECOKV_ERR_DEVICE_INDEX in the status word of ws (may be NULL, else at least 256
+ * bytes).  The result is deterministic.
+ * ECOKV_ERR_UNSUPPORTED: batch * h_kv > 2^29. */
+typedef struct {
+  int32_t h_kv, batch;
+  int32_t budget, limit, first, recent;
+} ecokv_prune_params;
+
+ecokv_status ecokv_prune(const ecokv_prune_params* p, ecokv_dtype dtype, const ecokv_pages* cache,
+                         const ecokv_weights* weights, const ecokv_pages* to, const ecokv_weights* to_weights,
+                         int32_t* idx, int32_t* lengths_out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

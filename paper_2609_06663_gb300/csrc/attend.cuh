@@ -15,6 +15,8 @@
 // exponentials; a second kernel joins them row by row.  Partial sums are fp32.
 #pragma once
 
+#include <cuda.h>
+
 #include "ecokv_decode.h"
 #include "ecokv_internal.cuh"
 
@@ -35,6 +37,8 @@ struct AttendArgs {
   ecokv_pages cache;
   int has_cache, page_shift, cap;  // cap: slots a sequence can have
   const int32_t* starts;
+  const uint32_t* mask;  // a tree's: [tokens][words] of 32 bits, NULL: causal
+  int words;
   int tpt;    // tokens a row tile holds
   int span;   // tokens an item holds (one or two row tiles)
   int groups, last;  // items that all tokens make, the last one's tokens
@@ -65,7 +69,8 @@ struct Item {
   int source;         // 0 prefix, 1 own
   int head, seq;
   int tok0, ntok;     // tokens of the call
-  int lim0, slope;    // token k of the item sees lim0 + k slope keys (at least 0)
+  int lim0, slope;    // token k of the item sees lim0 + k slope keys (at least 0); a tree's also
+                      // those from lim0 on whose bit is set
   int vis;            // the most keys any of them sees
   int tile0, ntiles;  // this CTA's tiles of the item
   int row0;           // first row of the head's prefix (head_off)
@@ -113,7 +118,7 @@ __host__ __device__ inline int prefix_units(const AttendArgs& a, int tiles) {
 // Keys that a sequence's item from its token i on sees at most, the item's units, and
 // those of all its items from tokens below `until`.
 __device__ __forceinline__ int seq_vis(const AttendArgs& a, const Seq& s, int i) {
-  return max(s.L - s.T + min(s.T, i + a.span), 0);
+  return a.mask != nullptr ? s.L : max(s.L - s.T + min(s.T, i + a.span), 0);
 }
 __device__ __forceinline__ int seq_item(const AttendArgs& a, const Seq& s, int i) {
   return item_units(a, tiles_of(seq_vis(a, s, i)), min(s.T - i, a.span));
@@ -310,8 +315,8 @@ struct Walk {
       it.seq = b0 + l;
       it.tok0 = q.start + i;
       it.ntok = min(a.span, q.T - i);
-      it.lim0 = q.L - q.T + i + 1;
-      it.slope = 1;
+      it.lim0 = a.mask != nullptr ? q.L - q.T : q.L - q.T + i + 1;
+      it.slope = a.mask != nullptr ? 0 : 1;
       it.vis = seq_vis(a, q, i);
       it.row0 = 0;
       nt = tiles_of(it.vis);
@@ -326,6 +331,12 @@ struct Walk {
   }
 };
 
+// Word w (32 drafts) of a token's row of the tree's mask; what lies before its sequence's
+// drafts is seen.
+__device__ __forceinline__ uint32_t tree_word(const AttendArgs& a, const uint32_t* row, int w) {
+  return w < 0 ? ~0u : w < a.words ? row[w] : 0u;
+}
+
 // Where the sum of a row (token, query head) goes from its item's first CTA, and that
 // of row `row` of row tile j of the item that CTA `cta` goes on with.
 __device__ __forceinline__ size_t first_row(const AttendArgs& a, int source, int token, int hq) {
@@ -339,6 +350,12 @@ __device__ __forceinline__ size_t next_row(const AttendArgs& a, int cta, int j, 
 // of e bytes) in whole 16 bytes.
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool stride_ok(int64_t s, size_t e) { return ((uint64_t)s * e & 15u) == 0; }
+// A tensor of bf16 rows of 128 for TMA, the axes after the first `strides` elements apart, in
+// boxes of 64 columns with the 128-byte swizzle.
+bool map_of(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const int64_t* strides,
+            const uint32_t* box);
+// CTAs of the persistent kernels: the current device's SMs.
+int attend_sms();
 ecokv_status check_pages(const ecokv_pages* c, int32_t batch, ecokv_dtype dt);
 cudaError_t launch_attend_simt(const AttendArgs& a, ecokv_dtype dt, cudaStream_t st);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st);

@@ -269,19 +269,6 @@ bool sizes_ok(int32_t tokens, int32_t batch, int32_t h_q, int32_t h_kv) {
   return tokens >= 0 && batch >= 1 && h_q >= 1 && h_kv >= 1 && h_q % h_kv == 0 && h_q <= (1 << 16);
 }
 
-// CTAs of the attention kernels: the current device's SMs (cached per device; a
-// racing thread repeats the query).
-int attend_sms() {
-  static std::atomic<int> cached[64];
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 152;
-  if ((n = cached[dev].load()) == 0) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 152;
-    cached[dev].store(n);
-  }
-  return n < kMaxAttendSms ? n : kMaxAttendSms;
-}
-
 template <typename T>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.tokens * a.h_q;
@@ -298,6 +285,18 @@ cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
 }
 
 }  // namespace
+
+// (cached per device; a racing thread repeats the query)
+int attend_sms() {
+  static std::atomic<int> cached[64];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 152;
+  if ((n = cached[dev].load()) == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 152;
+    cached[dev].store(n);
+  }
+  return n < kMaxAttendSms ? n : kMaxAttendSms;
+}
 
 ecokv_status check_pages(const ecokv_pages* c, int32_t batch, ecokv_dtype dt) {
   if (c == nullptr || batch < 1) return ECOKV_ERR_INVALID_ARG;
@@ -330,9 +329,11 @@ size_t ecokv_attend_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, i
   return attend_layout(tokens, batch, h_q, h_kv, 2).total;
 }
 
-ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const void* q, const ecokv_prefix* prefix,
-                          const ecokv_pages* cache, const int32_t* starts, void* out, float* lse, void* ws,
-                          size_t ws_bytes, void* stream) {
+}  // extern "C"
+
+static ecokv_status attend(const ecokv_attend_params* p, ecokv_dtype dtype, const void* q, const ecokv_prefix* prefix,
+                           const ecokv_pages* cache, const int32_t* starts, const uint64_t* mask, int32_t words,
+                           void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
   if (p == nullptr || !sizes_ok(p->tokens, p->batch, p->h_q, p->h_kv) || p->d < 1) return ECOKV_ERR_INVALID_ARG;
   if (dtype != ECOKV_F32 && dtype != ECOKV_BF16) return ECOKV_ERR_INVALID_ARG;
   const size_t e = dtype == ECOKV_F32 ? 4 : 2;
@@ -365,6 +366,8 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
     a.cap = cache->page_size * cache->table_stride;
     a.starts = starts;
   }
+  a.mask = reinterpret_cast<const uint32_t*>(mask);  // (both machines' words are little-endian)
+  a.words = 2 * words;
   a.q = q;
   a.out = out;
   a.lse = lse;
@@ -406,6 +409,25 @@ ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((tc ? launch_attend_tc(a, s) : launch_attend_simt(a, dtype, s)) != cudaSuccess) return ECOKV_ERR_CUDA;
   return launch_attend_join(a, dtype, s) == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
+}
+
+extern "C" {
+
+ecokv_status ecokv_attend(const ecokv_attend_params* p, ecokv_dtype dtype, const void* q, const ecokv_prefix* prefix,
+                          const ecokv_pages* cache, const int32_t* starts, void* out, float* lse, void* ws,
+                          size_t ws_bytes, void* stream) {
+  return attend(p, dtype, q, prefix, cache, starts, nullptr, 0, out, lse, ws, ws_bytes, stream);
+}
+
+ecokv_status ecokv_attend_tree(const ecokv_attend_params* p, ecokv_dtype dtype, const void* q,
+                               const ecokv_prefix* prefix, const ecokv_pages* cache, const int32_t* starts,
+                               const uint64_t* mask, int32_t words, void* out, float* lse, void* ws, size_t ws_bytes,
+                               void* stream) {
+  if (words < 1) return ECOKV_ERR_INVALID_ARG;
+  if (words > 64) return ECOKV_ERR_UNSUPPORTED;
+  if (p != nullptr && p->tokens != 0 && (cache == nullptr || mask == nullptr || ((uintptr_t)mask & 7u)))
+    return ECOKV_ERR_INVALID_ARG;
+  return attend(p, dtype, q, prefix, cache, starts, mask, words, out, lse, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

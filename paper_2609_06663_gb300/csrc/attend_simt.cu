@@ -74,11 +74,20 @@ __device__ __forceinline__ int64_t key_offset(const AttendArgs& a, const Item& i
          (int64_t)(j & (a.cache.page_size - 1)) * a.cache.slot_stride;
 }
 
+// Whether token k of the item sees key j of its tile.
+template <bool kTree>
+__device__ __forceinline__ bool sees(const AttendArgs& a, const Item& it, int k, int j) {
+  if (!kTree || it.source == 0) return j < it.lim0 + k * it.slope;
+  const int d = j - it.lim0;
+  return j < it.vis &&
+         (d < 0 || (tree_word(a, a.mask + (int64_t)(it.tok0 + k) * a.words, d >> 5) >> (d & 31) & 1u) != 0u);
+}
+
 constexpr int kFew = 32;              // rows of an item whose keys are split between the warps
 constexpr int kWarps = kThreads / 32;
 constexpr int kOwn = kKeys / kWarps;  // keys of a tile that a warp has
 
-template <typename T>
+template <typename T, bool kTree>
 __device__ __forceinline__ void item_few(const AttendArgs& a, Smem& s, const Item& it) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, kk = lane >> 1, half = lane & 1;
   const int rows = it.ntok * a.g;
@@ -148,7 +157,7 @@ __device__ __forceinline__ void item_few(const AttendArgs& a, Smem& s, const Ite
           if (at >= 0) kr[i] = load4(K + at + (2 * i + half) * 4);
         }
       }
-      const float y = j < it.lim0 + r / a.g * it.slope ? e * a.scale_log2 : -INFINITY;
+      const float y = sees<kTree>(a, it, r / a.g, j) ? e * a.scale_log2 : -INFINITY;
       const float m = mx[r], mn = fmaxf(m, ptx::redux_max(y)), ref = mn == -INFINITY ? 0.f : mn;
       const float corr = ptx::ex2(m - ref);
       float l = sum[r] * corr;
@@ -207,7 +216,7 @@ __device__ __forceinline__ void item_few(const AttendArgs& a, Smem& s, const Ite
   }
 }
 
-template <typename T>
+template <typename T, bool kTree>
 __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const Item& it) {
   constexpr int R = kRows / 16;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31, warp = tid >> 5;
@@ -284,7 +293,9 @@ __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const It
       float mx = -INFINITY;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        x[r][c] = t * kKeys + tx + 16 * c < lim[r] ? x[r][c] * a.scale_log2 : -INFINITY;
+        const int j = t * kKeys + tx + 16 * c;
+        const bool seen = kTree ? sees<true>(a, it, min((ty * R + r) / a.g, it.ntok - 1), j) : j < lim[r];
+        x[r][c] = seen ? x[r][c] * a.scale_log2 : -INFINITY;
         mx = fmaxf(mx, x[r][c]);
       }
 #pragma unroll
@@ -347,7 +358,7 @@ __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const It
   }
 }
 
-template <typename T>
+template <typename T, bool kTree>
 __global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Smem& s = *reinterpret_cast<Smem*>(smem_raw);
@@ -368,13 +379,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt_kernel(const __grid_c
     __syncthreads();
     if (s.more == 0) break;
     const Item it = s.item;
-    if (it.ntok * a.g <= kFew) item_few<T>(a, s, it);
-    else item_rows<T>(a, s, it);
+    if (it.ntok * a.g <= kFew) item_few<T, kTree>(a, s, it);
+    else item_rows<T, kTree>(a, s, it);
   }
   ptx::grid_trigger();
 }
 
-template <typename T>
+template <typename T, bool kTree>
 cudaError_t launch(const AttendArgs& a, cudaStream_t st) {
   static std::atomic<bool> set[64];  // a racing thread repeats the idempotent setting
   int dev = 0;
@@ -382,17 +393,18 @@ cudaError_t launch(const AttendArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!set[dev].load()) {
-    e = cudaFuncSetAttribute(attend_simt_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+    e = cudaFuncSetAttribute(attend_simt_kernel<T, kTree>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
     if (e != cudaSuccess) return e;
     set[dev].store(true);
   }
-  return launch_behind(attend_simt_kernel<T>, (unsigned)a.P, kThreads, sizeof(Smem), st, a);
+  return launch_behind(attend_simt_kernel<T, kTree>, (unsigned)a.P, kThreads, sizeof(Smem), st, a);
 }
 
 }  // namespace
 
 cudaError_t launch_attend_simt(const AttendArgs& a, ecokv_dtype dt, cudaStream_t st) {
-  return dt == ECOKV_F32 ? launch<float>(a, st) : launch<__nv_bfloat16>(a, st);
+  if (a.mask != nullptr) return dt == ECOKV_F32 ? launch<float, true>(a, st) : launch<__nv_bfloat16, true>(a, st);
+  return dt == ECOKV_F32 ? launch<float, false>(a, st) : launch<__nv_bfloat16, false>(a, st);
 }
 
 }  // namespace ecokv

@@ -253,6 +253,7 @@ __device__ __forceinline__ void multiply(Smem& s, const AttendArgs& a, uint32_t 
   }
 }
 
+template <bool kTree>
 __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tmem, int stream) {
   const int lane = threadIdx.x & 31, row = threadIdx.x & 127, warp = row >> 5;
   const uint32_t ts = tmem + (uint32_t)stream * 256u + ((uint32_t)(warp * 32) << 16), to = ts + 128u;
@@ -278,6 +279,16 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
     for (int t = t0; t < it.ntiles; t += step, ++k) {
       const int from = (it.tile0 + t) * kKeys;
       const int nv = it.vis - from;  // keys of the tile that are there (128 or more: all)
+      uint32_t see[5];  // a tree: bits of 32 keys each, from the 32 drafts of the tile's first key on
+      int turn = 0;
+      const bool drafts = kTree && it.source != 0 && from + kKeys > it.lim0;
+      if (drafts) {  // (loaded while the scores are on their way)
+        const int d = from - it.lim0;
+        const uint32_t* bits = a.mask + (int64_t)min(it.tok0 + tok + row_k, a.tokens - 1) * a.words;
+        turn = d & 31;
+#pragma unroll
+        for (int q = 0; q < 5; ++q) see[q] = tree_word(a, bits, (d >> 5) + q);
+      }
       if (!wait_warp(s, a, &s.sfull[stream], k & 1, 8u)) return;
       tc_fence_after();
       const int nc = min(nv + 31, kKeys) >> 5;  // blocks of 32 keys that are there
@@ -295,7 +306,17 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
           tmem_ld_x32(ts + 32 * b, x);
           tmem_wait_ld();
           tmem_landed(x);
-          const int here = seen - 32 * b;
+          const int here = (kTree && it.source != 0 ? nv : seen) - 32 * b;
+          if (drafts) {
+            const uint32_t lo = b == 0 ? see[0] : b == 1 ? see[1] : b == 2 ? see[2] : see[3];
+            const uint32_t hi = b == 0 ? see[1] : b == 1 ? see[2] : b == 2 ? see[3] : see[4];
+            const uint32_t bits = __funnelshift_r(lo, hi, turn);
+            if (__any_sync(0xffffffffu, bits != ~0u)) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                if ((bits >> c & 1u) == 0u) x[c] = 0xff800000u;  // -inf
+            }
+          }
           if (__any_sync(0xffffffffu, here < 32)) {
 #pragma unroll
             for (int c = 0; c < 32; ++c)
@@ -440,6 +461,7 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
   }
 }
 
+template <bool kTree>
 __global__ void __launch_bounds__(kThreads, 1)
     attend_tc_kernel(const __grid_constant__ Maps m, const __grid_constant__ AttendArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -485,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = s.tmem;
   Issued d;
   if (warp >= 4) {
-    soften(s, a, tmem, (warp >> 2) - 1);
+    soften<kTree>(s, a, tmem, (warp >> 2) - 1);
   } else {
     if (warp == 0) {
       // (the injected stall: no tile ever comes)
@@ -555,8 +577,8 @@ EncodeTiledFn encode_fn() {
   return f;
 }
 
-// A tensor of bf16 rows of 128, the axes after the first `strides` elements apart, in
-// boxes of 64 columns with the 128-byte swizzle.
+}  // namespace
+
 bool map_of(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const int64_t* strides,
             const uint32_t* box) {
   const EncodeTiledFn enc = encode_fn();
@@ -573,8 +595,6 @@ bool map_of(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, co
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-}  // namespace
 
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st) {
   int dev = 0;
@@ -607,11 +627,14 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t st) {
   }
   const int smem = (int)sizeof(Smem) + 1024;
   if (!g_attr_set[dev].load()) {  // a racing thread repeats the idempotent setting
-    e = cudaFuncSetAttribute(attend_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    e = cudaFuncSetAttribute(attend_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(attend_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     g_attr_set[dev].store(true);
   }
-  return launch_behind(attend_tc_kernel, (unsigned)a.P, kThreads, (size_t)smem, st, m, a);
+  return a.mask != nullptr ? launch_behind(attend_tc_kernel<true>, (unsigned)a.P, kThreads, (size_t)smem, st, m, a)
+                           : launch_behind(attend_tc_kernel<false>, (unsigned)a.P, kThreads, (size_t)smem, st, m, a);
 }
 
 }  // namespace ecokv

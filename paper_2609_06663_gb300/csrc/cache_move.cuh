@@ -1,0 +1,148 @@
+// Rows of a paged cache that move to the front of their sequence, or to another cache
+// (drafts.cu, prune.cu).
+//
+// What bounds it is memory: every row is read and written once, 16 bytes a lane.  In
+// one cache a row may lie where another one goes: row i of a list comes from slot
+// src(i) >= dst(i) and the sources ascend, so a row that is written over is one that the list
+// has passed, or one of those at hand.  A unit (sequence, head, K or V) takes its list
+// in chunks, all of a chunk read before any of it is written; with few units a
+// cluster of CTAs shares a chunk, its barrier between the two.
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "attend.cuh"
+#include "decode_ptx.cuh"
+
+namespace ecokv {
+
+constexpr int kMoveThreads = 256;
+constexpr int kMoveRows = 8;  // rows whose pieces a thread has in flight
+
+struct MoveArgs {
+  ecokv_pages from, to;           // the same pages in one cache
+  ecokv_weights w_from, w_to;     // w NULL: none
+  int from_shift, to_shift;
+  int h_kv, batch;
+  int ctas;                       // of a unit
+  int in_place;                   // these are a cluster
+  unsigned* status;               // may be NULL
+};
+
+__device__ __forceinline__ void flag(unsigned* status, unsigned detail) {
+  if (status != nullptr && atomicCAS(status, 0u, (unsigned)ECOKV_ERR_DEVICE_INDEX) == 0u) status[1] = detail;
+}
+
+// Place of a sequence's slot; page -1: out of range.
+struct Place {
+  int page, row;
+};
+__device__ __forceinline__ Place place_of(const ecokv_pages& c, int shift, int b, int slot, unsigned* status) {
+  Place p;
+  p.row = slot & (c.page_size - 1);
+  p.page = -1;
+  const int col = slot >> shift;
+  if (col < c.table_stride) p.page = c.table[(int64_t)b * c.table_stride + col];
+  if (p.page < 0 || p.page >= c.n_pages) {
+    flag(status, (unsigned)b);
+    p.page = -1;
+  }
+  return p;
+}
+__device__ __forceinline__ int64_t offset_of(const ecokv_pages& c, Place p, int h) {
+  return (int64_t)p.page * c.page_stride + (int64_t)h * c.head_stride + (int64_t)p.row * c.slot_stride;
+}
+__device__ __forceinline__ int64_t offset_of(const ecokv_weights& w, Place p, int h) {
+  return (int64_t)p.page * w.page_stride + (int64_t)h * w.head_stride + (int64_t)p.row * w.slot_stride;
+}
+
+// One CTA's share of the rows [i0, n) of unit (b, h, kv): row i from slot src(i) to slot dst0 +
+// i.  src: row number -> slot, the same in every CTA.  E: bytes an element.
+template <int E, typename Src>
+__device__ __forceinline__ void move_rows(const MoveArgs& a, int b, int h, int kv, int rank, int i0, int n, int dst0,
+                                          Src src) {
+  constexpr int kLanes = kD * E / 16;               // lanes a row
+  constexpr int kAtOnce = kMoveThreads / kLanes;    // rows a step of the CTA
+  constexpr int kChunk = kAtOnce * kMoveRows;
+  const int lane = threadIdx.x % kLanes, r0 = threadIdx.x / kLanes;
+  const char* x = static_cast<const char*>(kv == 0 ? a.from.k : a.from.v);
+  char* y = static_cast<char*>(kv == 0 ? a.to.k : a.to.v);
+  const bool weights = kv == 0 && a.w_to.w != nullptr;
+#pragma unroll 1
+  for (int base = i0; base < n; base += kChunk * a.ctas) {
+    const int c0 = base + rank * kChunk;
+    uint4 v[kMoveRows];
+    int64_t at[kMoveRows];  // where each goes, negative: nowhere
+#pragma unroll
+    for (int k = 0; k < kMoveRows; ++k) {
+      const int i = c0 + r0 + k * kAtOnce;
+      at[k] = -1;
+      if (i >= n) continue;
+      const int s = src(i);
+      if (a.in_place && s == dst0 + i) continue;
+      const Place p = place_of(a.from, a.from_shift, b, s, a.status);
+      const Place q = place_of(a.to, a.to_shift, b, dst0 + i, a.status);
+      if (p.page < 0 || q.page < 0) continue;
+      at[k] = offset_of(a.to, q, h) * E;
+      v[k] = *reinterpret_cast<const uint4*>(x + offset_of(a.from, p, h) * E + lane * 16);
+    }
+    float w = 0.f;
+    float* w_at = nullptr;
+    if (weights && threadIdx.x < kChunk && c0 + (int)threadIdx.x < n) {
+      const int i = c0 + threadIdx.x, s = src(i);
+      const Place p = place_of(a.from, a.from_shift, b, s, a.status);
+      const Place q = place_of(a.to, a.to_shift, b, dst0 + i, a.status);
+      if (p.page >= 0 && q.page >= 0) {
+        w_at = a.w_to.w + offset_of(a.w_to, q, h);
+        w = a.w_from.w[offset_of(a.w_from, p, h)];
+      }
+    }
+    if (a.in_place) {
+      if (a.ctas > 1) cooperative_groups::this_cluster().sync();
+      else __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kMoveRows; ++k)
+      if (at[k] >= 0) *reinterpret_cast<uint4*>(y + at[k] + lane * 16) = v[k];
+    if (w_at != nullptr) *w_at = w;
+  }
+}
+
+// Launch `kernel` with a.ctas CTAs a unit, as clusters where they wait for each other.
+template <typename... A>
+cudaError_t launch_move(void (*kernel)(A...), const MoveArgs& a, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(a.batch * a.h_kv * 2 * a.ctas));
+  cfg.blockDim = dim3(kMoveThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.in_place ? (unsigned)a.ctas : 1u;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// CTAs a unit of up to `rows` rows has: as many as it has chunks for, while all units'
+// CTAs together are no more than two an SM (152 SMs), a power of two up to a cluster's eight.
+inline int move_ctas(int64_t units, int64_t rows, ecokv_dtype dt) {
+  const int64_t chunk = (int64_t)kMoveThreads * 16 / (kD * (dt == ECOKV_F32 ? 4 : 2)) * kMoveRows;
+  int c = 1;
+  while (c < 8 && units * c < 152 && chunk * c < rows) c *= 2;
+  return c;
+}
+
+inline bool weights_ok(const ecokv_weights* w) {
+  return w->w != nullptr && ((uintptr_t)w->w & 3u) == 0 && w->page_stride > 0 && w->head_stride > 0 &&
+         w->slot_stride > 0;
+}
+// lengths_out is the lengths, or apart from them.
+inline bool lengths_ok(const int32_t* lengths, const int32_t* out, int32_t batch) {
+  const uintptr_t x = (uintptr_t)lengths, y = (uintptr_t)out, n = (uintptr_t)batch * 4;
+  return out != nullptr && (y & 3u) == 0 && (x == y || x + n <= y || y + n <= x);
+}
+
+}  // namespace ecokv

@@ -36,7 +36,8 @@ EXPORTS = ("ecokv_params_default", "ecokv_check_params", "ecokv_workspace_size",
            "ecokv_evict_noalloc", "ecokv_set_stage_events", "ecokv_workspace_size_host", "ecokv_evict_host",
            "ecokv_evict_adaptive", "ecokv_evict_layered", "ecokv_pyramid_budgets",
            "ecokv_rotary_init", "ecokv_rotary_set", "ecokv_rotary_sections", "ecokv_rotate", "ecokv_append",
-           "ecokv_attend_workspace_size", "ecokv_attend")
+           "ecokv_attend_workspace_size", "ecokv_attend", "ecokv_tree_mask", "ecokv_attend_tree", "ecokv_commit",
+           "ecokv_weigh_workspace_size", "ecokv_weigh", "ecokv_prune")
 ROTARY_LAYOUT = {"half": 0, "interleaved": 1}
 ROTARY_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 HEAD_DIM = 128
@@ -90,6 +91,20 @@ class ecokv_attend_params(ctypes.Structure):
     _fields_ = [("h_q", _i32), ("h_kv", _i32), ("d", _i32), ("tokens", _i32), ("batch", _i32),
                 ("scale", ctypes.c_float), ("q_token", _i64), ("q_head", _i64), ("out_token", _i64),
                 ("out_head", _i64), ("flags", ctypes.c_uint32), ("timeout_us", ctypes.c_uint32)]
+
+
+class ecokv_weights(ctypes.Structure):
+    _fields_ = [("w", _vp), ("page_stride", _i64), ("head_stride", _i64), ("slot_stride", _i64)]
+
+
+class ecokv_weigh_params(ctypes.Structure):
+    _fields_ = [("h_q", _i32), ("h_kv", _i32), ("d", _i32), ("tokens", _i32), ("batch", _i32),
+                ("scale", ctypes.c_float), ("decay", ctypes.c_float), ("q_token", _i64), ("q_head", _i64),
+                ("flags", ctypes.c_uint32), ("timeout_us", ctypes.c_uint32)]
+
+
+class ecokv_prune_params(ctypes.Structure):
+    _fields_ = [("h_kv", _i32), ("batch", _i32), ("budget", _i32), ("limit", _i32), ("first", _i32), ("recent", _i32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -148,6 +163,22 @@ def lib() -> ctypes.CDLL:
                                    ctypes.POINTER(ecokv_prefix), ctypes.POINTER(ecokv_pages), _vp, _vp, _vp, _vp,
                                    _sz, _vp]
         L.ecokv_attend.restype = ctypes.c_int
+        pages, pre, wts = ctypes.POINTER(ecokv_pages), ctypes.POINTER(ecokv_prefix), ctypes.POINTER(ecokv_weights)
+        L.ecokv_tree_mask.argtypes = [_vp, _vp, _i32, _i32, _vp, _i32, _vp, _sz, _vp]
+        L.ecokv_tree_mask.restype = ctypes.c_int
+        L.ecokv_attend_tree.argtypes = [ctypes.POINTER(ecokv_attend_params), ctypes.c_int, _vp, pre, pages, _vp, _vp,
+                                        _i32, _vp, _vp, _vp, _sz, _vp]
+        L.ecokv_attend_tree.restype = ctypes.c_int
+        L.ecokv_commit.argtypes = [ctypes.c_int, pages, _i32, _vp, _i32, _vp, _vp, _i32, _i32, wts, _vp, _vp, _sz, _vp]
+        L.ecokv_commit.restype = ctypes.c_int
+        L.ecokv_weigh_workspace_size.argtypes = [_i32, _i32, _i32, _i32, ctypes.c_int]
+        L.ecokv_weigh_workspace_size.restype = _sz
+        L.ecokv_weigh.argtypes = [ctypes.POINTER(ecokv_weigh_params), ctypes.c_int, _vp, _vp, pre, pages, _vp, wts,
+                                  wts, _vp, _sz, _vp]
+        L.ecokv_weigh.restype = ctypes.c_int
+        L.ecokv_prune.argtypes = [ctypes.POINTER(ecokv_prune_params), ctypes.c_int, pages, wts, pages, wts, _vp, _vp,
+                                  _vp, _sz, _vp]
+        L.ecokv_prune.restype = ctypes.c_int
         L.ecokv_device_status.argtypes = [_vp, _vp]
         L.ecokv_device_status.restype = ctypes.c_int
         L.ecokv_status_string.argtypes = [ctypes.c_int]
@@ -290,6 +321,36 @@ def ecokv_attend_workspace_size(tokens, batch, h_q, h_kv, dtype) -> int:
 def ecokv_attend(p, dtype, q, prefix, cache, starts, out, lse, ws, ws_bytes, stream=None) -> int:
     return lib().ecokv_attend(p, dtype, _ptr(q), prefix, cache, _ptr(starts), _ptr(out), _ptr(lse), _ptr(ws),
                               ws_bytes, _stream(stream))
+
+
+def ecokv_tree_mask(parents, starts, tokens, batch, mask, words, ws=None, ws_bytes=0, stream=None) -> int:
+    return lib().ecokv_tree_mask(_ptr(parents), _ptr(starts), tokens, batch, _ptr(mask), words, _ptr(ws), ws_bytes,
+                                 _stream(stream))
+
+
+def ecokv_attend_tree(p, dtype, q, prefix, cache, starts, mask, words, out, lse, ws, ws_bytes, stream=None) -> int:
+    return lib().ecokv_attend_tree(p, dtype, _ptr(q), prefix, cache, _ptr(starts), _ptr(mask), words, _ptr(out),
+                                   _ptr(lse), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def ecokv_commit(dtype, cache, h_kv, accepted, stride, counts, starts, tokens, batch, weights, lengths_out, ws=None,
+                 ws_bytes=0, stream=None) -> int:
+    return lib().ecokv_commit(dtype, cache, h_kv, _ptr(accepted), stride, _ptr(counts), _ptr(starts), tokens, batch,
+                              weights, _ptr(lengths_out), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def ecokv_weigh_workspace_size(tokens, batch, h_q, h_kv, dtype) -> int:
+    return lib().ecokv_weigh_workspace_size(tokens, batch, h_q, h_kv, dtype)
+
+
+def ecokv_weigh(p, dtype, q, lse, prefix, cache, starts, prefix_weights, weights, ws, ws_bytes, stream=None) -> int:
+    return lib().ecokv_weigh(p, dtype, _ptr(q), _ptr(lse), prefix, cache, _ptr(starts), prefix_weights, weights,
+                             _ptr(ws), ws_bytes, _stream(stream))
+
+
+def ecokv_prune(p, dtype, cache, weights, to, to_weights, idx, lengths_out, ws=None, ws_bytes=0, stream=None) -> int:
+    return lib().ecokv_prune(p, dtype, cache, weights, to, to_weights, _ptr(idx), _ptr(lengths_out), _ptr(ws),
+                             ws_bytes, _stream(stream))
 
 
 def ecokv_device_status(ws, stream=None) -> int:
@@ -732,10 +793,9 @@ def alloc_attend_workspace(tokens, batch, h_q, h_kv, dtype, device="cuda"):
     return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
-def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None, flags=0, timeout_us=0, stream=None):
-    """Run ecokv_attend: q [tokens, h_q, 128] over prefix (a Prefix or None) and
-    cache (a PagedCache or None); returns out [tokens, h_q, 128].  starts int32
-    [batch + 1]: None = one token a sequence.  lse: float32 [tokens, h_q] to fill."""
+def _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us, stream):
+    """The arguments of ecokv_attend but for its last three: parameters, dtype, tensors and out; the workspace; the
+    stream; out itself."""
     if out is None:
         out = _like(q, stream)
     if prefix is None and cache is None:
@@ -747,16 +807,201 @@ def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None
     if to != tokens or ho != h_q or (prefix is not None and prefix.h_kv != h_kv):
         raise ValueError("out or the prefix does not fit")
     batch = 1 if cache is None else cache.batch
-    if lse is not None and (str(lse.dtype) != "torch.float32" or tuple(lse.shape) != (tokens, h_q) or
-                            not lse.is_contiguous() or lse.get_device() != dev):
-        raise ValueError(f"lse: a contiguous float32 [tokens, h_q] tensor on cuda:{dev} is wanted")
+    if lse is not None:
+        _lse(lse, tokens, h_q, dev)
     if ws is None:
         ws = _made(stream, q, lambda: alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device))
-    if ws.get_device() != dev:
-        raise ValueError(f"the workspace is on {ws.device}, the tensors on cuda:{dev}")
+    _same_device(ws, dev)
     p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, qt, qh, ot, oh, flags, timeout_us)
-    _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), None if prefix is None else prefix.c,
-                              None if cache is None else cache.c,
-                              None if cache is None else _ints(starts, (batch + 1,), "starts", dev), out.data_ptr(),
-                              _ptr(lse), ws.data_ptr(), ws.numel(), _on(stream, dev)), "ecokv_attend")
+    return p, dt, None if prefix is None else prefix.c, None if cache is None else cache.c, \
+        None if cache is None else _ints(starts, (batch + 1,), "starts", dev), ws, _on(stream, dev), out
+
+
+def _lse(lse, tokens, h_q, dev):
+    if str(lse.dtype) != "torch.float32" or tuple(lse.shape) != (tokens, h_q) or not lse.is_contiguous() or \
+            lse.get_device() != dev:
+        raise ValueError(f"lse: a contiguous float32 [tokens, h_q] tensor on cuda:{dev} is wanted")
+
+
+def _same_device(ws, dev):
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"the workspace is on {ws.device}, the tensors on cuda:{dev}")
+
+
+def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None, flags=0, timeout_us=0, stream=None):
+    """Run ecokv_attend: q [tokens, h_q, 128] over prefix (a Prefix or None) and
+    cache (a PagedCache or None); returns out [tokens, h_q, 128].  starts int32
+    [batch + 1]: None = one token a sequence.  lse: float32 [tokens, h_q] to fill."""
+    p, dt, pre, pages, starts, ws, on, out = _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us,
+                                                     stream)
+    _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), pre, pages, starts, out.data_ptr(), _ptr(lse),
+                                        ws.data_ptr(), ws.numel(), on), "ecokv_attend")
     return out
+
+
+# ---------------------------------------------------------------- drafted tokens
+def _mask(mask, tokens, dev):
+    """Words of a tree's mask."""
+    if str(mask.dtype) != "torch.int64" or mask.dim() != 2 or mask.shape[0] != tokens or not mask.is_contiguous() or \
+            mask.get_device() != dev:
+        raise ValueError(f"mask: a contiguous int64 [tokens, words] tensor on cuda:{dev} is wanted")
+    return mask.shape[1]
+
+
+def tree_mask(parents, starts=None, mask=None, words=None, ws=None, stream=None):
+    """Run ecokv_tree_mask: which drafts of its sequence each draft sees, itself and
+    its ancestors.  parents int32 [tokens]: the draft each one follows, a number
+    within its sequence, -1 for the last token before the drafts; starts int32
+    [batch + 1]: None = one draft a sequence.  Returns mask, int64 [tokens, words], 64 bits
+    a word.  words (or mask's): enough for the longest sequence; by default for
+    as many drafts as the call has.  ws: a workspace whose status word takes device-side errors."""
+    dev = parents.get_device()
+    if dev < 0:
+        raise ValueError("CUDA tensors are wanted")
+    tokens = parents.numel()
+    if mask is None:
+        n = words or (min(max(1, -(-tokens // 64)), 64) if starts is not None else 1)
+        mask = _made(stream, parents, lambda: parents.new_empty((tokens, n), dtype=_torch().int64))
+    n = _mask(mask, tokens, dev)
+    if words is not None and n != words:
+        raise ValueError(f"a mask of {n} words, {words} were asked for")
+    if starts is not None and (starts.dim() != 1 or starts.shape[0] < 2):
+        raise ValueError("starts [batch + 1] are wanted")
+    batch = tokens if starts is None else starts.shape[0] - 1
+    _same_device(ws, dev)
+    if tokens:
+        _check((_lib or lib()).ecokv_tree_mask(_ints(parents, (tokens,), "parents", dev),
+                                               _ints(starts, None, "starts", dev), tokens, batch, mask.data_ptr(), n,
+                                               _ptr(ws), 0 if ws is None else ws.numel(), _on(stream, dev)),
+               "ecokv_tree_mask")
+    return mask
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def attend_tree(q, prefix, cache, mask, starts=None, scale=0.0, out=None, lse=None, ws=None, flags=0, timeout_us=0,
+                stream=None):
+    """Run ecokv_attend_tree: as attend(), where a token sees its sequence's slots
+    before the new tokens and those of the new ones whose bit is set in its row of mask
+    (int64 [tokens, words], from tree_mask() or any other)."""
+    if cache is None:
+        raise ValueError("a cache is wanted")
+    p, dt, pre, pages, starts, ws, on, out = _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us,
+                                                     stream)
+    words = _mask(mask, p.tokens, q.get_device())
+    _check((_lib or lib()).ecokv_attend_tree(p, dt, q.data_ptr(), pre, pages, starts, mask.data_ptr(), words,
+                                             out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(), on),
+           "ecokv_attend_tree")
+    return out
+
+
+def _weights(w, shape, what, dev):
+    """Weights [n_pages, h_kv, page_size] of a cache, [h_kv, rows] or [rows] of a prefix."""
+    if str(w.dtype) != "torch.float32" or tuple(w.shape) != tuple(shape) or w.get_device() != dev:
+        raise ValueError(f"{what}: a float32 tensor of shape {tuple(shape)} on cuda:{dev} is wanted")
+    # (a stride that is never taken counts as one)
+    s = tuple(x if n > 1 else 1 for n, x in zip(w.shape, w.stride()))
+    return ecokv_weights(w.data_ptr(), *((1,) * (3 - len(s)) + s))
+
+
+def commit(cache, accepted, counts, starts=None, weights=None, lengths_out=None, tokens=None, ws=None, stream=None):
+    """Run ecokv_commit: the first counts[b] drafts of accepted[b] (numbers within
+    their sequence, ascending) move to the front of sequence b's drafts, with their weights
+    [n_pages, h_kv, page_size] where given.  accepted int32 [batch, most], counts int32
+    [batch]; starts as in attend_tree() (tokens: starts' last; by default no limit but
+    theirs).  Returns the new lengths, lengths_out where given (the cache's own lengths too)."""
+    dt, dev = _dtype(cache.k_pages)
+    batch = cache.batch
+    if accepted.dim() != 2 or accepted.shape[0] != batch or accepted.shape[1] < 1:
+        raise ValueError("accepted [batch, most] is wanted")
+    if lengths_out is None:
+        lengths_out = _like(cache.lengths, stream)
+    if tokens is None:
+        tokens = batch if starts is None else 2 ** 31 - 1
+    _same_device(ws, dev)
+    _check((_lib or lib()).ecokv_commit(
+        dt, cache.c, cache.h_kv, _ints(accepted, None, "accepted", dev), accepted.shape[1],
+        _ints(counts, (batch,), "counts", dev), _ints(starts, (batch + 1,), "starts", dev), tokens, batch,
+        None if weights is None else _weights(weights, cache.k_pages.shape[:3], "weights", dev),
+        _ints(lengths_out, (batch,), "lengths_out", dev), _ptr(ws), 0 if ws is None else ws.numel(),
+        _on(stream, dev)), "ecokv_commit")
+    return lengths_out
+
+
+# ---------------------------------------------------------------- a cache that shrinks
+def alloc_weigh_workspace(tokens, batch, h_q, h_kv, dtype, device="cuda"):
+    """Workspace of weigh() for up to `tokens` tokens of `batch` sequences (dtype: torch's)."""
+    import torch
+    n = ecokv_weigh_workspace_size(tokens, batch, h_q, h_kv, ECOKV_F32 if dtype == torch.float32 else ECOKV_BF16)
+    if n == 0:
+        raise EcokvError(ECOKV_ERR_INVALID_ARG, "ecokv_weigh_workspace_size")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def weigh(q, lse, prefix, cache, prefix_weights=None, weights=None, starts=None, scale=0.0, decay=1.0, ws=None,
+          flags=0, timeout_us=0, stream=None):
+    """Run ecokv_weigh: what the attention of q [tokens, h_q, 128] gives each key of
+    prefix and cache (either may be None), from the lse that attend() has left, is added to
+    prefix_weights (float32, of the shape of the prefix's k without its last axis) and to
+    weights [n_pages, h_kv, page_size], which are multiplied by decay first.  starts int32
+    [batch + 1]: None = one token a sequence.  Returns (prefix_weights, weights)."""
+    if prefix is None and cache is None:
+        raise ValueError("a prefix or a cache is wanted")
+    dt, dev = _dtype(q, None if prefix is None else prefix.k, None if cache is None else cache.k_pages)
+    tokens, h_q, qt, qh = _heads(q, "q")
+    h_kv = prefix.h_kv if cache is None else cache.h_kv
+    if prefix is not None and prefix.h_kv != h_kv:
+        raise ValueError("the prefix does not fit")
+    batch = 1 if cache is None else cache.batch
+    _lse(lse, tokens, h_q, dev)
+    pw = w = None
+    if prefix is not None:
+        if prefix_weights is None:
+            raise ValueError("prefix_weights are wanted")
+        pw = _weights(prefix_weights, prefix.k.shape[:-1], "prefix_weights", dev)
+    if cache is not None:
+        if weights is None:
+            raise ValueError("weights are wanted")
+        w = _weights(weights, cache.k_pages.shape[:3], "weights", dev)
+    if ws is None:
+        ws = _made(stream, q, lambda: alloc_weigh_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device))
+    _same_device(ws, dev)
+    p = ecokv_weigh_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, decay, qt, qh, flags, timeout_us)
+    _check((_lib or lib()).ecokv_weigh(p, dt, q.data_ptr(), lse.data_ptr(), None if prefix is None else prefix.c,
+                                       None if cache is None else cache.c,
+                                       None if cache is None else _ints(starts, (batch + 1,), "starts", dev), pw, w,
+                                       ws.data_ptr(), ws.numel(), _on(stream, dev)), "ecokv_weigh")
+    return prefix_weights, weights
+
+
+def prune(cache, weights, budget, limit=None, first=0, recent=0, to=None, to_weights=None, lengths_out=None, idx=None,
+          ws=None, stream=None):
+    """Run ecokv_prune: sequences of more than `limit` slots (default: budget) keep
+    `budget` of them in each head, the `first` first, the `recent` last and between
+    them those of the largest weights [n_pages, h_kv, page_size].  They take slots 0 .. of
+    the same cache, or of `to` (a PagedCache), their weights of to_weights (None: they
+    are not moved; `weights` itself in the same cache).  Returns (new lengths, idx int32
+    [batch, h_kv, limit]: the slots kept, then -1); lengths_out may be either cache's lengths."""
+    limit = budget if limit is None else limit
+    dt, dev = _dtype(cache.k_pages, None if to is None else to.k_pages)
+    batch, h_kv = cache.batch, cache.h_kv
+    if to is not None and (to.batch != batch or to.h_kv != h_kv):
+        raise ValueError("the caches do not fit")
+    if limit < 1:
+        raise ValueError("a limit of one slot at least is wanted")
+    w = _weights(weights, cache.k_pages.shape[:3], "weights", dev)
+    tw = None if to_weights is None else _weights(to_weights, (to or cache).k_pages.shape[:3], "to_weights", dev)
+    if lengths_out is None:
+        lengths_out = _like(cache.lengths, stream)
+    if idx is None:
+        idx = _made(stream, cache.lengths, lambda: cache.lengths.new_empty((batch, h_kv, limit)))
+    _same_device(ws, dev)
+    p = ecokv_prune_params(h_kv, batch, budget, limit, first, recent)
+    _check((_lib or lib()).ecokv_prune(p, dt, cache.c, w, None if to is None else to.c, tw,
+                                       _ints(idx, (batch, h_kv, limit), "idx", dev),
+                                       _ints(lengths_out, (batch,), "lengths_out", dev), _ptr(ws),
+                                       0 if ws is None else ws.numel(), _on(stream, dev)), "ecokv_prune")
+    return lengths_out, idx
