@@ -6,7 +6,8 @@
 // src(i) >= dst(i) and the sources ascend, so a row that is written over is one that the list
 // has passed, or one of those at hand.  A unit (sequence, head, K or V) takes its list
 // in chunks, all of a chunk read before any of it is written; with few units a
-// cluster of CTAs shares a chunk, its barrier between the two.
+// cluster of CTAs shares a chunk, its barrier between the two.  Where a chunk's rows are is
+// looked up, a thread a row, while those of the chunk before it are on their way.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -64,47 +65,59 @@ __device__ __forceinline__ void move_rows(const MoveArgs& a, int b, int h, int k
   constexpr int kLanes = kD * E / 16;               // lanes a row
   constexpr int kAtOnce = kMoveThreads / kLanes;    // rows a step of the CTA
   constexpr int kChunk = kAtOnce * kMoveRows;
+  // bytes from k or v, from and to; from < 0: the row stays.  (Three chunks': while a warp
+  // looks the next up, another may still write the one before.)
+  __shared__ longlong2 places[3][kChunk];
   const int lane = threadIdx.x % kLanes, r0 = threadIdx.x / kLanes;
-  const char* x = static_cast<const char*>(kv == 0 ? a.from.k : a.from.v);
-  char* y = static_cast<char*>(kv == 0 ? a.to.k : a.to.v);
+  const char* x = static_cast<const char*>(kv == 0 ? a.from.k : a.from.v) + lane * 16;
+  char* y = static_cast<char*>(kv == 0 ? a.to.k : a.to.v) + lane * 16;
   const bool weights = kv == 0 && a.w_to.w != nullptr;
-#pragma unroll 1
-  for (int base = i0; base < n; base += kChunk * a.ctas) {
-    const int c0 = base + rank * kChunk;
-    uint4 v[kMoveRows];
-    int64_t at[kMoveRows];  // where each goes, negative: nowhere
-#pragma unroll
-    for (int k = 0; k < kMoveRows; ++k) {
-      const int i = c0 + r0 + k * kAtOnce;
-      at[k] = -1;
-      if (i >= n) continue;
-      const int s = src(i);
-      if (a.in_place && s == dst0 + i) continue;
-      const Place p = place_of(a.from, a.from_shift, b, s, a.status);
-      const Place q = place_of(a.to, a.to_shift, b, dst0 + i, a.status);
-      if (p.page < 0 || q.page < 0) continue;
-      at[k] = offset_of(a.to, q, h) * E;
-      v[k] = *reinterpret_cast<const uint4*>(x + offset_of(a.from, p, h) * E + lane * 16);
-    }
-    float w = 0.f;
-    float* w_at = nullptr;
-    if (weights && threadIdx.x < kChunk && c0 + (int)threadIdx.x < n) {
-      const int i = c0 + threadIdx.x, s = src(i);
+  float w = 0.f;
+  float* w_at = nullptr;
+  auto look_up = [&](int base, int buf) {
+    const int i = base + rank * kChunk + (int)threadIdx.x;
+    if (threadIdx.x >= kChunk) return;
+    longlong2 at = make_longlong2(-1, -1);
+    if (weights) w_at = nullptr;
+    const int s = i < n ? src(i) : 0;
+    if (i < n && !(a.in_place && s == dst0 + i)) {
       const Place p = place_of(a.from, a.from_shift, b, s, a.status);
       const Place q = place_of(a.to, a.to_shift, b, dst0 + i, a.status);
       if (p.page >= 0 && q.page >= 0) {
-        w_at = a.w_to.w + offset_of(a.w_to, q, h);
-        w = a.w_from.w[offset_of(a.w_from, p, h)];
+        at = make_longlong2(offset_of(a.from, p, h) * E, offset_of(a.to, q, h) * E);
+        if (weights) {
+          w_at = a.w_to.w + offset_of(a.w_to, q, h);
+          w = a.w_from.w[offset_of(a.w_from, p, h)];
+        }
       }
     }
-    if (a.in_place) {
-      if (a.ctas > 1) cooperative_groups::this_cluster().sync();
-      else __syncthreads();
-    }
+    places[buf][threadIdx.x] = at;
+  };
+  if (i0 >= n) return;
+  look_up(i0, 0);
+  __syncthreads();
+  int buf = 0;
+#pragma unroll 1
+  for (int base = i0; base < n; base += kChunk * a.ctas) {
+    const int next = buf == 2 ? 0 : buf + 1;
+    uint4 v[kMoveRows];
 #pragma unroll
-    for (int k = 0; k < kMoveRows; ++k)
-      if (at[k] >= 0) *reinterpret_cast<uint4*>(y + at[k] + lane * 16) = v[k];
-    if (w_at != nullptr) *w_at = w;
+    for (int k = 0; k < kMoveRows; ++k) {
+      const int64_t at = places[buf][r0 + k * kAtOnce].x;
+      if (at >= 0) v[k] = *reinterpret_cast<const uint4*>(x + at);
+    }
+    const float w_now = w;
+    float* const w_to = w_at;
+    if (base + kChunk * a.ctas < n) look_up(base + kChunk * a.ctas, next);
+    if (a.in_place && a.ctas > 1) cooperative_groups::this_cluster().sync();
+    else __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kMoveRows; ++k) {
+      const longlong2 at = places[buf][r0 + k * kAtOnce];
+      if (at.x >= 0) *reinterpret_cast<uint4*>(y + at.y) = v[k];
+    }
+    if (weights && threadIdx.x < kChunk && w_to != nullptr) *w_to = w_now;
+    buf = next;
   }
 }
 

@@ -112,7 +112,7 @@ __device__ __forceinline__ Path read_path(const CommitArgs& a, int b) {
 }
 
 template <int E>
-__global__ void __launch_bounds__(kMoveThreads) commit_kernel(const __grid_constant__ CommitArgs a) {
+__global__ void __launch_bounds__(kMoveThreads, 4) commit_kernel(const __grid_constant__ CommitArgs a) {
   ptx::grid_trigger();
   ptx::grid_wait();
   const int unit = blockIdx.x / a.m.ctas, rank = blockIdx.x - unit * a.m.ctas;

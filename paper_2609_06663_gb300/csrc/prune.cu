@@ -37,6 +37,7 @@ __device__ __forceinline__ unsigned order_of(float x) {
 constexpr int kSelectThreads = 512;
 constexpr int kSelectWarps = kSelectThreads / 32;
 constexpr int kBins = 2048;
+constexpr int kAhead = 8;
 
 __global__ void __launch_bounds__(kSelectThreads) prune_select_kernel(const __grid_constant__ PruneArgs a) {
   extern __shared__ unsigned keys[];
@@ -59,11 +60,16 @@ __global__ void __launch_bounds__(kSelectThreads) prune_select_kernel(const __gr
   for (int i = tid; i < a.recent; i += kSelectThreads) out[a.budget - a.recent + i] = L - a.recent + i;
   const int need = a.budget - a.first - a.recent, n = L - a.first - a.recent;  // need < n
   if (need == 0) return;
-  auto load = [&](int i) {
-    const Place p = place_of(a.m.from, a.m.from_shift, b, a.first + i, a.m.status);
-    return order_of(p.page < 0 ? -INFINITY : a.w.w[offset_of(a.w, p, h)]);
+  const int* table = a.m.from.table + (int64_t)b * a.m.from.table_stride;
+  const float* weights = a.w.w + (int64_t)h * a.w.head_stride;
+  auto page_of = [&](int i) { return table[(a.first + i) >> a.m.from_shift]; };
+  auto load = [&](int i, int page) {
+    const int row = (a.first + i) & (a.m.from.page_size - 1);
+    return page < 0 || page >= a.m.from.n_pages
+               ? -INFINITY
+               : weights[(int64_t)page * a.w.page_stride + (int64_t)row * a.w.slot_stride];
   };
-  auto key = [&](int i) { return i < a.cached ? keys[i] : load(i); };
+  auto key = [&](int i) { return i < a.cached ? keys[i] : order_of(load(i, page_of(i))); };
 
   unsigned top = 0;       // the key's digits so far
   unsigned left = need;   // keys of these digits that stay
@@ -73,17 +79,31 @@ __global__ void __launch_bounds__(kSelectThreads) prune_select_kernel(const __gr
     const int width = pass == 2 ? 10 : 11;
     for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
     __syncthreads();
-#pragma unroll 4
-    for (int i = tid; i < n; i += kSelectThreads) {
-      unsigned k;
-      if (pass == 0) {
-        k = load(i);
-        if (i < a.cached) keys[i] = k;
-      } else {
-        k = key(i);
-        if (((k ^ top) >> (low + width)) != 0) continue;
+    if (pass == 0) {
+#pragma unroll 1
+      for (int i0 = tid; i0 < n; i0 += kAhead * kSelectThreads) {  // (as many loads at once)
+        int page[kAhead];
+        float x[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) page[j] = page_of(min(i0 + j * kSelectThreads, n - 1));
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) x[j] = load(min(i0 + j * kSelectThreads, n - 1), page[j]);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int i = i0 + j * kSelectThreads;
+          if (i >= n) break;
+          if (page[j] < 0 || page[j] >= a.m.from.n_pages) flag(a.m.status, (unsigned)b);
+          const unsigned k = order_of(x[j]);
+          if (i < a.cached) keys[i] = k;
+          atomicAdd(&bins[k >> 21], 1u);
+        }
       }
-      atomicAdd(&bins[(k >> low) & ((1u << width) - 1)], 1u);
+    } else {
+#pragma unroll 4
+      for (int i = tid; i < n; i += kSelectThreads) {
+        const unsigned k = key(i);
+        if (((k ^ top) >> (low + width)) == 0) atomicAdd(&bins[(k >> low) & ((1u << width) - 1)], 1u);
+      }
     }
     __syncthreads();
     // from the top bin down: the one in which the count reaches `left`
@@ -147,7 +167,7 @@ __global__ void __launch_bounds__(kSelectThreads) prune_select_kernel(const __gr
 }
 
 template <int E>
-__global__ void __launch_bounds__(kMoveThreads) prune_move_kernel(const __grid_constant__ PruneArgs a) {
+__global__ void __launch_bounds__(kMoveThreads, 4) prune_move_kernel(const __grid_constant__ PruneArgs a) {
   ptx::grid_trigger();
   ptx::grid_wait();
   const int unit = blockIdx.x / a.m.ctas, rank = blockIdx.x - unit * a.m.ctas;

@@ -60,6 +60,7 @@ struct WeighWalk {
   long long x, end, prefix_total, own;
   int live, lane;
   int b0, head;
+  int left;          // keys of the head and sequence behind the item before, if that was met to its end
   long long before;  // units of the sequences before b0
   Seq s;
   long long n, upto;
@@ -113,6 +114,7 @@ struct WeighWalk {
     }
     before = 0;
     head = 0;
+    left = 0;
     const long long total = prefix_total + a.h_kv * own;
     // (a tile's units at least: no CTA between an item's first and last is without a tile of it)
     const long long run = max((total + a.P - 1) / a.P, (long long)max(w.unit[0], w.unit[1]));
@@ -134,6 +136,11 @@ struct WeighWalk {
     const AttendArgs& a = w.a;
     long long y;
     int keys;
+    if (left > 0) {  // the item behind the one before
+      it.key0 += w.span;
+      it.nkeys = min(left, w.span);
+      return part(w, it, 0, left);
+    }
     if (x < prefix_total) {
       it.source = 0;
       it.seq = 0;
@@ -193,33 +200,44 @@ struct WeighWalk {
       it.ntok = __shfl_sync(0xffffffffu, s.T, l);
       it.base = keys - it.ntok;
     }
-    const int per = weigh_per(w, it.source, it.ntok), i = (int)(y / per), u = w.unit[it.source];
+    const int per = weigh_per(w, it.source, it.ntok), i = (int)(y / per);
     it.key0 = i * w.span;
     it.nkeys = min(keys - it.key0, w.span);
-    if (it.nkeys <= 0) return false;
-    // the tiles whose first unit lies within this CTA's part of the item, y .. z - 1
-    y -= (long long)i * per;
-    const long long z = min((long long)per, y + end - x);
-    it.tile0 = (int)((max(y - w.lead, 0ll) + u - 1) / u);
-    it.ntiles = (int)((max(z - w.lead, 0ll) + u - 1) / u) - it.tile0;
+    return part(w, it, (int)(y - (long long)i * per), keys - it.key0);
+  }
+  // The tiles of an item whose first unit lies within this CTA's part of it, y .. z - 1; the
+  // item and what lies behind it of its head and sequence have `keys` keys.
+  __device__ __forceinline__ bool part(const WeighArgs& w, WeighItem& it, int y, int keys) {
+    const int per = weigh_per(w, it.source, it.ntok), u = w.unit[it.source];
+    const int z = (int)min((long long)per, y + end - x);
+    it.tile0 = (max(y - w.lead, 0) + u - 1) / u;
+    it.ntiles = (max(z - w.lead, 0) + u - 1) / u - it.tile0;
     x += z - y;
-    return z > y;  // (else nothing would move on)
+    left = z == per ? max(keys - w.span, 0) : 0;
+    return z > y && keys > 0;  // (else nothing would move on)
   }
 };
 
-// Where the weight of key j of the item's source is; NULL: a slot without a page.
-__device__ __forceinline__ float* weight_at(const WeighArgs& w, const WeighItem& it, int j) {
+// Where the weight of key j of the item's source is, whose page is `page`; NULL: a slot without
+// a page.
+__device__ __forceinline__ int weight_page(const WeighArgs& w, const WeighItem& it, int j) {
+  const AttendArgs& a = w.a;
+  return it.source == 0 ? 0 : a.cache.table[(int64_t)it.seq * a.cache.table_stride + (j >> a.page_shift)];
+}
+__device__ __forceinline__ float* weight_at(const WeighArgs& w, const WeighItem& it, int j, int page) {
   const AttendArgs& a = w.a;
   if (it.source == 0)
     return w.pw.w + (a.prefix.head_off ? 0 : (int64_t)it.head * w.pw.head_stride) +
            ((int64_t)it.row0 + j) * w.pw.slot_stride;
-  const int page = a.cache.table[(int64_t)it.seq * a.cache.table_stride + (j >> a.page_shift)];
   if (page < 0 || page >= a.cache.n_pages) {
     note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)it.seq);
     return nullptr;
   }
   return w.w.w + (int64_t)page * w.w.page_stride + (int64_t)it.head * w.w.head_stride +
          (int64_t)(j & (a.cache.page_size - 1)) * w.w.slot_stride;
+}
+__device__ __forceinline__ float* weight_at(const WeighArgs& w, const WeighItem& it, int j) {
+  return weight_at(w, it, j, weight_page(w, it, j));
 }
 // The weight that the item's sum is added to: a new token's own slot starts at 0.
 __device__ __forceinline__ float weight_before(const WeighArgs& w, const WeighItem& it, const float* at, int j) {

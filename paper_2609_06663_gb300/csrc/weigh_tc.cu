@@ -117,32 +117,41 @@ struct Issued {
 __device__ __forceinline__ void produce(Smem& s, const WeighArgs& w, const Maps& m, int lane, Issued& d) {
   const AttendArgs& a = w.a;
   ItemReader items;
-  WeighItem it;
+  WeighItem next{};
   Ring<kKeyTiles> kr;
   Ring<kRowTiles> qr;
-  while (items.next(s, a, it, lane)) {
+  int pages[2] = {0, 0};  // this lane's of the next item's key tiles
+  auto look_up = [&]() {
+    if (next.source == 0) return;
+    const int* table = a.cache.table + (int64_t)next.seq * a.cache.table_stride;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int from = next.key0 + p * kKeys, to = min(from + kKeys, next.key0 + next.nkeys);
+      const int c = (from >> a.page_shift) + lane;
+      if (from < to && c <= (to - 1) >> a.page_shift) pages[p] = table[c];
+    }
+  };
+  bool more = items.next(s, a, next, lane);
+  if (more) look_up();
+  while (more) {
+    const WeighItem it = next;
     const bool own = it.source != 0;
     const int head = own || a.prefix.head_off == nullptr ? it.head : 0;
     const uint32_t box = own ? (uint32_t)min(a.cache.page_size, kKeys) : kKeys;
     const uint32_t at = own ? (((uint32_t)lane << a.page_shift) & (kKeys - 1)) * 128u : lane * kHalf;
-    const int* table = a.cache.table + (int64_t)it.seq * a.cache.table_stride;
     const int nk = key_tiles(it);
-    for (int p = 0; p < nk; ++p) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      if (p >= nk) break;
       const int from = it.key0 + p * kKeys, to = min(from + kKeys, it.key0 + it.nkeys);
-      int n = 2, page = 0;
-      if (own) {
-        const int c0 = from >> a.page_shift;
-        n = ((to - 1) >> a.page_shift) - c0 + 1;
-        if (lane < n) {
-          page = table[c0 + lane];
-          if (page < 0 || page >= a.cache.n_pages) {
-            note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)it.seq);
-            page = a.cache.n_pages;  // out of the map's bounds: zeros
-          }
-        }
-      }
+      const int n = own ? ((to - 1) >> a.page_shift) - (from >> a.page_shift) + 1 : 2;
       const int row = own ? from & (a.cache.page_size - 1) : it.row0 + from;
       if (!wait_warp(s, a, &s.kempty[kr.at], kr.phase ^ 1, 2u)) return;
+      int page = pages[p];
+      if (own && lane < n && (page < 0 || page >= a.cache.n_pages)) {
+        note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)it.seq);
+        page = a.cache.n_pages;  // out of the map's bounds: zeros
+      }
       uint8_t* dst = s.k[kr.at] + at;
       uint64_t* bar = &s.kfull[kr.at];
       if (lane == 0) mbar_expect_tx(bar, own ? box * n * 256u : kTileBytes);
@@ -158,6 +167,9 @@ __device__ __forceinline__ void produce(Smem& s, const WeighArgs& w, const Maps&
       kr.step();
       ++d.k;
     }
+    // (page numbers an item ahead, on their way while this one's rows are copied)
+    more = items.next(s, a, next, lane);
+    if (more) look_up();
     const int tpt = w.tpt[it.source];
     for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
       if (!wait_warp(s, a, &s.qempty[qr.at], qr.phase ^ 1, 3u)) return;
@@ -266,15 +278,22 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
   const uint32_t ts = tmem + (uint32_t)stream * 256u + ((uint32_t)(warp * 32) << 16);
   const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
   ItemReader items;
-  WeighItem it;
+  WeighItem next{};
   Ring<kRowTiles> r;
   Ring<2> sr;
-  while (items.next(s, a, it, lane)) {
-    const int k = stream * kKeys + row, j = it.key0 + k;
-    const bool active = stream < key_tiles(it), mine = active && k < it.nkeys;
-    // (on its way while the products are)
-    float* at = mine && it.tile0 == 0 ? weight_at(w, it, j) : nullptr;
+  const int k = stream * kKeys + row;
+  bool more = items.next(s, a, next, lane);
+  auto page_of = [&]() { return more && k < next.nkeys ? weight_page(w, next, next.key0 + k) : 0; };
+  int page = page_of();
+  while (more) {
+    const WeighItem it = next;
+    const int j = it.key0 + k;
+    const bool active = stream < key_tiles(it), mine = k < it.nkeys;
+    // (on its way while the products are; the next item's page number too)
+    float* at = mine && it.tile0 == 0 ? weight_at(w, it, j, page) : nullptr;
     const float before = weight_before(w, it, at, j);
+    more = items.next(s, a, next, lane);
+    page = page_of();
     float total = 0.f;
     const int tpt = w.tpt[it.source];
     for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
