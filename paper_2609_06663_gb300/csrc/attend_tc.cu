@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // (the injected stall: no tile ever comes)
       if (a.stall == 0) produce(s, a, m, lane, d);
     } else if (warp == 1 || warp == 3) {
-      if (lane == 0) {
+      if (elect_one()) {
         multiply(s, a, tmem, (uint32_t)warp >> 1);
         mma_commit(&s.drained);
       }

@@ -8,9 +8,10 @@
 // a thread's register over all the rows that see it, the keys are read once and the few
 // queries again for each item, from the L2.  All items' tiles in a row (the prefix's by
 // head, the own ones by head and sequence) are dealt to the CTAs in equal runs of
-// units: `lead` for an item's keys, `unit` for each of its tiles.  An item's first
-// CTA adds its sum to the weight; the others leave theirs, which a second kernel adds
-// in their order.
+// units: `lead` for an item's keys, `unit` for each of its tiles.  An item of more than
+// `whole` units may be cut: its first CTA adds its sum to the weight, the others leave theirs,
+// which a second kernel adds in their order.  A smaller one is its first unit's CTA's: it
+// takes less time than that kernel's launch.
 #pragma once
 
 #include "attend.cuh"
@@ -33,20 +34,24 @@ struct WeighArgs {
   ecokv_weights pw, w;    // of the prefix, of the slots
   const float* lse;
   float decay;
-  int span, tpt[2], unit[2], lead;
+  int span, span_log2, tpt[2], unit[2], lead, whole;
   float* next;            // [P][kWeighSpan] sums of the item that a CTA goes on with
   WeighItem* next_item;   // [P], tile0 = 0: none
 };
 
 // Row tiles of an item that so many tokens see (one at least, so that it is met).
 __device__ __forceinline__ int row_tiles(const WeighArgs& w, int source, int ntok) {
-  return max(div_up(ntok, w.tpt[source]), 1);
+  return ntok > w.tpt[source] ? div_up(ntok, w.tpt[source]) : 1;
+}
+// (numbers of 64 bits that nearly always have 31: the long division's code is not fetched)
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+  return ((x | y) >> 31) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
 }
 __device__ __forceinline__ int weigh_per(const WeighArgs& w, int source, int ntok) {
   return w.lead + row_tiles(w, source, ntok) * w.unit[source];
 }
 __device__ __forceinline__ long long weigh_units(const WeighArgs& w, int source, int keys, int ntok) {
-  return (long long)((keys + w.span - 1) / w.span) * weigh_per(w, source, ntok);
+  return (long long)((keys + w.span - 1) >> w.span_log2) * weigh_per(w, source, ntok);
 }
 
 // Tokens of the call that are of a sequence, from 0 on.
@@ -105,19 +110,22 @@ struct WeighWalk {
     }
     own = 0;
     if (a.has_cache) {
-#pragma unroll 1
-      for (int c = 0; c < a.batch; c += 32) {
-        chunk(w, c, report);
-        own += __shfl_sync(0xffffffffu, upto, 31);
+      chunk(w, 0, report);
+      own = n;
+#pragma unroll 4
+      for (int b = 32 + lane; b < a.batch; b += 32) {
+        const Seq q = load_seq(a, b, report);
+        own += weigh_units(w, 1, q.L, q.T);
       }
-      if (a.batch > 32) chunk(w, 0, false);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
     }
     before = 0;
     head = 0;
     left = 0;
     const long long total = prefix_total + a.h_kv * own;
     // (a tile's units at least: no CTA between an item's first and last is without a tile of it)
-    const long long run = max((total + a.P - 1) / a.P, (long long)max(w.unit[0], w.unit[1]));
+    const long long run = max(quotient(total + a.P - 1, a.P), (long long)max(w.unit[0], w.unit[1]));
     x = min(cta * run, total);
     end = min(x + run, total);
   }
@@ -149,8 +157,8 @@ struct WeighWalk {
       it.ntok = live;
       if (a.prefix.head_off == nullptr) {
         keys = a.prefix.rows;
-        const long long per = prefix_total / a.h_kv;
-        it.head = (int)(x / per);
+        const long long per = quotient(prefix_total, a.h_kv);
+        it.head = (int)quotient(x, per);
         y = x - it.head * per;
       } else {
         long long at = 0;
@@ -175,7 +183,7 @@ struct WeighWalk {
       it.base = keys;
     } else {
       y = x - prefix_total;
-      const int h = (int)(y / own);
+      const int h = (int)quotient(y, own);
       y -= h * own;
       if (h != head && b0 != 0) {
         before = 0;
@@ -200,7 +208,7 @@ struct WeighWalk {
       it.ntok = __shfl_sync(0xffffffffu, s.T, l);
       it.base = keys - it.ntok;
     }
-    const int per = weigh_per(w, it.source, it.ntok), i = (int)(y / per);
+    const int per = weigh_per(w, it.source, it.ntok), i = (int)quotient(y, per);
     it.key0 = i * w.span;
     it.nkeys = min(keys - it.key0, w.span);
     return part(w, it, (int)(y - (long long)i * per), keys - it.key0);
@@ -209,9 +217,10 @@ struct WeighWalk {
   // item and what lies behind it of its head and sequence have `keys` keys.
   __device__ __forceinline__ bool part(const WeighArgs& w, WeighItem& it, int y, int keys) {
     const int per = weigh_per(w, it.source, it.ntok), u = w.unit[it.source];
-    const int z = (int)min((long long)per, y + end - x);
+    const bool whole = per <= w.whole;
+    const int z = whole ? per : (int)min((long long)per, y + end - x);
     it.tile0 = (max(y - w.lead, 0) + u - 1) / u;
-    it.ntiles = (max(z - w.lead, 0) + u - 1) / u - it.tile0;
+    it.ntiles = whole && y > 0 ? 0 : (max(z - w.lead, 0) + u - 1) / u - it.tile0;
     x += z - y;
     left = z == per ? max(keys - w.span, 0) : 0;
     return z > y && keys > 0;  // (else nothing would move on)

@@ -118,13 +118,18 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
   w.lse = lse;
   w.decay = p->decay;
   w.span = tc ? kWeighSpan : 128;
+  w.span_log2 = tc ? 8 : 7;
+  static_assert(kWeighSpan == 1 << 8, "span_log2");
   w.tpt[0] = (tc ? 128 : 64) / a.g;
   // a sequence's own row tiles have room for twice the mean of its tokens: what is copied and
   // multiplied of a decode step's single rows is no more than they are
   const int mean = a.starts != nullptr ? div_up(a.tokens, a.batch) : 1;
   w.tpt[1] = a.starts != nullptr && 2 * mean < w.tpt[0] ? 2 * mean : a.starts != nullptr ? w.tpt[0] : 1;
-  for (int k = 0; k < 2; ++k) w.unit[k] = div_up(w.tpt[k] * a.g, 32);
-  w.lead = 8;
+  // (a unit: about 600 cycles of a CTA, an item of 256 keys with one row tile 5 of them, each row
+  // tile of 128 rows 4; on CUDA cores 16 rows of a tile, which take as long as the keys)
+  for (int k = 0; k < 2; ++k) w.unit[k] = div_up(w.tpt[k] * a.g, tc ? 32 : 16);
+  w.lead = tc ? 4 : 1;
+  w.whole = tc ? 24 : 5;
   const double items = div_up(a.cap, w.span), of_prefix = div_up(a.prefix.rows, w.span);
   const double most = w.lead + 4.0 * (p->tokens + 1);
   if (a.h_kv * (of_prefix + (double)p->batch * items) * most > 4e18) return ECOKV_ERR_UNSUPPORTED;
@@ -138,8 +143,10 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (a.prefix.rows == 0 && !a.has_cache) return ECOKV_OK;
   if ((tc ? launch_weigh_tc(w, s) : launch_weigh_simt(w, dtype, s)) != cudaSuccess) return ECOKV_ERR_CUDA;
-  // (items of one row tile are not cut)
-  const bool cut = (a.prefix.rows > 0 && a.tokens > w.tpt[0]) || (a.has_cache && a.starts != nullptr && a.tokens > w.tpt[1]);
+  // (the units of the largest items that there can be)
+  auto units = [&](int source, int ntok) { return w.lead + (double)w.unit[source] * div_up(ntok, w.tpt[source]); };
+  const bool cut = (a.prefix.rows > 0 && units(0, a.tokens) > w.whole) ||
+                   (a.has_cache && units(1, a.starts != nullptr ? a.tokens : 1) > w.whole);
   if (!cut) return ECOKV_OK;
   return launch_behind(weigh_join_kernel, (unsigned)a.P, kWeighSpan, 0, s, w) == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
 }

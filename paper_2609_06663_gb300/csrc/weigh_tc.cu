@@ -5,15 +5,16 @@
 // has rows, in sixteens), so that a thread has a key: it adds the exponentials of its
 // row of S^T, whose references lie in shared memory, in registers, without a shuffle and
 // without a maximum, the sums of exponentials being known.  An item's two key tiles stay in
-// shared memory while the row tiles pass by; each has a warpgroup of its own
-// ("stream") and two accumulators in tensor memory, so that the products run beside
-// the exponentials.
+// shared memory while the row tiles pass by; each has two accumulators in tensor memory, for
+// even and odd row tiles of all items, and each accumulator a warpgroup ("stream") of its
+// own, so that the products run beside the exponentials and four warps a scheduler hide
+// each other's latencies.  The sums of an item's even and odd tiles are added at its end.
 //
 // Bound by the keys' bytes where few rows see them (a decode step), by the exponentials
 // where many do: 128 x 128 of them take a CTA longer than their product.
 //
 // Warps: 0 copies (TMA; a lane a page), 1 the products, 2 the walk over the items, 3 the
-// rows' references, 4-7 and 8-11 the streams.
+// rows' references, 4-19 the streams: key tile, then parity.
 
 #include <atomic>
 
@@ -26,26 +27,29 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;
 constexpr int kKeyTiles = 4;  // key tiles in the ring
-constexpr int kRowTiles = 3;  // row tiles
+constexpr int kRowTiles = 3;  // row tiles (two: 53.7 us for 806 tokens over 6554 rows, three 46.9)
+constexpr int kRefs = 2;      // row tiles' references
 constexpr int kItems = 4;     // items ahead of their consumers
 constexpr uint32_t kHalf = kTileBytes / 2;  // 128 rows x 64 columns
 
 struct Smem {
   uint8_t k[kKeyTiles][kTileBytes];
   uint8_t q[kRowTiles][kTileBytes];
-  float ref[kRowTiles][128];
+  float ref[kRefs][128];
   uint64_t kfull[kKeyTiles], kempty[kKeyTiles];
-  uint64_t qfull[kRowTiles], qempty[kRowTiles], rfull[kRowTiles], rempty[kRowTiles];
-  uint64_t sfull[2][2], sempty[2][2];  // [stream][accumulator]
+  uint64_t qfull[kRowTiles], qempty[kRowTiles], rfull[kRefs], rempty[kRefs];
+  uint64_t sfull[2][2], sempty[2][2];  // [key tile][parity]
+  uint64_t mready[2][4], mdone[2][4];  // between the streams' warps of the same keys
+  float sum[2][128];                   // of the stream that has not had the item's first tile
   uint64_t ifull[kItems], iempty[kItems];
   uint64_t drained;
   WeighItem items[kItems];
   uint32_t tmem;
   volatile int abort;
 };
-static_assert(sizeof(Smem) + 1024 <= 232448, "one CTA's shared memory");
+static_assert(sizeof(Smem) <= 232448, "one CTA's shared memory");
 
 struct Maps {
   CUtensorMap q[2], pk, ck;
@@ -190,7 +194,9 @@ __device__ __forceinline__ void multiply(Smem& s, const WeighArgs& w, uint32_t t
   Ring<kItems> ir;
   Ring<kKeyTiles> kr;
   Ring<kRowTiles> qr;
-  Ring<2> sr[2];
+  uint32_t n = 0;         // row tiles so far
+  uint32_t phase = 0;     // bit 2 p + b: parity of the next phase of sempty[p][b]
+  const uint64_t k0 = smem_desc(smem_u32(s.k[0]), 16, 1024, 2), q0 = smem_desc(smem_u32(s.q[0]), 16, 1024, 2);
   while (true) {
     if (!wait_bar(s, a, &s.ifull[ir.at], ir.phase, 1u)) return;
     const WeighItem it = s.items[ir.at];
@@ -202,30 +208,30 @@ __device__ __forceinline__ void multiply(Smem& s, const WeighArgs& w, uint32_t t
 #pragma unroll
     for (int p = 0; p < 2; ++p)
       if (p < nk) slot[p] = kr.at, kr.step();
-    // (the phase of the slot that the ring has just passed)
-    for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
-      const uint32_t n = (uint32_t)max((rows_of(w, it, t) + 15) & ~15, 16);
+    for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t, ++n) {
+      const uint32_t cols = (uint32_t)max((rows_of(w, it, t) + 15) & ~15, 16), b = n & 1;
+      const uint32_t idesc = idesc_bf16(128, (int)cols, false, false);
       if (!wait_bar(s, a, &s.qfull[qr.at], qr.phase, 4u)) return;
-      const uint64_t qd = smem_desc(smem_u32(s.q[qr.at]), 16, 1024, 2);
+      const uint64_t qd = q0 + (uint64_t)(qr.at * (kTileBytes >> 4));
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         if (p >= nk) break;
         if (t == it.tile0) {
-          const uint32_t phase = slot[p] < kr.at ? kr.phase : kr.phase ^ 1;
-          if (!wait_bar(s, a, &s.kfull[slot[p]], phase, 5u)) return;
+          // (the ring may have passed its end since the slot)
+          const uint32_t full = slot[p] < kr.at ? kr.phase : kr.phase ^ 1;
+          if (!wait_bar(s, a, &s.kfull[slot[p]], full, 5u)) return;
         }
-        if (!wait_bar(s, a, &s.sempty[p][sr[p].at], sr[p].phase ^ 1, 6u)) return;
+        const uint32_t i = (uint32_t)p * 2 + b;
+        if (!wait_bar(s, a, &s.sempty[p][b], ((phase >> i) & 1) ^ 1, 6u)) return;
+        phase ^= 1u << i;
         tc_fence_after();
-        const uint64_t kd = smem_desc(smem_u32(s.k[slot[p]]), 16, 1024, 2);
-        const uint32_t to = tmem + (uint32_t)(p * 2 + sr[p].at) * 128u;
-        const uint32_t idesc = idesc_bf16(128, (int)n, false, false);
+        const uint64_t kd = k0 + (uint64_t)(slot[p] * (kTileBytes >> 4));
 #pragma unroll
         for (int k8 = 0; k8 < 8; ++k8) {
           const uint64_t d = (uint64_t)((k8 >> 2) * (kHalf >> 4) + (k8 & 3) * 2);
-          mma_bf16(to, kd + d, qd + d, idesc, k8 > 0 ? 1u : 0u);
+          mma_bf16(tmem + i * 128u, kd + d, qd + d, idesc, k8 > 0 ? 1u : 0u);
         }
-        mma_commit(&s.sfull[p][sr[p].at]);
-        sr[p].step();
+        mma_commit(&s.sfull[p][b]);
       }
       mma_commit(&s.qempty[qr.at]);
       qr.step();
@@ -236,73 +242,89 @@ __device__ __forceinline__ void multiply(Smem& s, const WeighArgs& w, uint32_t t
   }
 }
 
-// The rows' references, a tile ahead of their turn.
+// The rows' references: those of the next two tiles are on their way.
 __device__ __forceinline__ void refer(Smem& s, const WeighArgs& w, int lane) {
   const AttendArgs& a = w.a;
   ItemReader items;
   WeighItem it;
-  Ring<kRowTiles> r;
-  float next[4];
-  auto look_up = [&](int t) {
-    const int rows = rows_of(w, it, t), first = it.tok0 + t * w.tpt[it.source];
+  // this lane's four rows of a tile: where their numbers are from the tile's first one's
+  int64_t at[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = lane + 32 * i, k = row / a.g;
-      next[i] = row < rows ? w.lse[(int64_t)(first + k) * a.h_q + it.head * a.g + row - k * a.g] : -INFINITY;
-    }
-  };
+  for (int i = 0; i < 4; ++i) {
+    const int row = lane + 32 * i, k = row / a.g;
+    at[i] = (int64_t)k * a.h_q + row - k * a.g;
+  }
+  int t = 0;
   bool more = items.next(s, a, it, lane);
-  int t = it.tile0;
-  if (more) look_up(t);
-  while (more) {
-    float ref[4];
+  if (more) t = it.tile0;
+  auto look_up = [&](float (&to)[4]) {  // the next tile's; false: there is none
+    if (!more) return false;
+    const int rows = rows_of(w, it, t);
+    const float* from = w.lse + (int64_t)(it.tok0 + t * w.tpt[it.source]) * a.h_q + it.head * a.g;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ref[i] = next[i];
+    for (int i = 0; i < 4; ++i) to[i] = lane + 32 * i < rows ? from[at[i]] : -INFINITY;
     if (++t == it.tile0 + it.ntiles) {
       more = items.next(s, a, it, lane);
-      t = it.tile0;
+      if (more) t = it.tile0;
     }
-    if (more) look_up(t);
-    if (!wait_warp(s, a, &s.rempty[r.at], r.phase ^ 1, 7u)) return;
+    return true;
+  };
+  float even[4], odd[4];
+  bool has_even = look_up(even), has_odd = look_up(odd);
+  Ring<kRefs> r;
+  auto put = [&](float (&x)[4], bool& has) {
+    float ref[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s.ref[r.at][lane + 32 * i] = weigh_ref(ref[i]);
+    for (int i = 0; i < 4; ++i) ref[i] = weigh_ref(x[i]);
+    has = look_up(x);
+    if (!wait_warp(s, a, &s.rempty[r.at], r.phase ^ 1, 7u)) return false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s.ref[r.at][lane + 32 * i] = ref[i];
     __syncwarp();
     if (lane == 0) mbar_arrive(&s.rfull[r.at]);
     r.step();
+    return true;
+  };
+  while (has_even && put(even, has_even) && has_odd && put(odd, has_odd)) {
   }
 }
 
-__device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tmem, int stream) {
+__device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tmem, int tile, uint32_t parity) {
   const AttendArgs& a = w.a;
   const int lane = threadIdx.x & 31, row = threadIdx.x & 127, warp = row >> 5;
-  const uint32_t ts = tmem + (uint32_t)stream * 256u + ((uint32_t)(warp * 32) << 16);
+  const uint32_t ts = tmem + (uint32_t)(tile * 2 + parity) * 128u + ((uint32_t)(warp * 32) << 16);
   const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
+  const int k = tile * kKeys + row;
   ItemReader items;
   WeighItem next{};
-  Ring<kRowTiles> r;
-  Ring<2> sr;
-  const int k = stream * kKeys + row;
+  uint32_t n0 = 0, jobs = 0, merges = 0;  // row tiles before the item; this stream's products; items it has shared
   bool more = items.next(s, a, next, lane);
-  auto page_of = [&]() { return more && k < next.nkeys ? weight_page(w, next, next.key0 + k) : 0; };
-  int page = page_of();
+  auto page_of = [&](uint32_t n) {
+    return more && (n & 1) == parity && k < next.nkeys ? weight_page(w, next, next.key0 + k) : 0;
+  };
+  int page = page_of(0);
   while (more) {
     const WeighItem it = next;
     const int j = it.key0 + k;
-    const bool active = stream < key_tiles(it), mine = k < it.nkeys;
+    // (the stream of the item's first tile has its keys' weights)
+    const bool active = tile < key_tiles(it), mine = k < it.nkeys, first = (n0 & 1) == parity, both = it.ntiles > 1;
     // (on its way while the products are; the next item's page number too)
-    float* at = mine && it.tile0 == 0 ? weight_at(w, it, j, page) : nullptr;
+    float* at = mine && first && it.tile0 == 0 ? weight_at(w, it, j, page) : nullptr;
     const float before = weight_before(w, it, at, j);
     more = items.next(s, a, next, lane);
-    page = page_of();
+    page = page_of(n0 + (uint32_t)it.ntiles);
     float total = 0.f;
     const int tpt = w.tpt[it.source];
-    for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
+    for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t, ++n0) {
+      if ((n0 & 1) != parity) continue;
       const int rows = rows_of(w, it, t);
       // rows from this one on see the key
       const int from = it.source == 0 ? 0 : max((j - it.base - t * tpt) * a.g, 0);
-      if (!wait_warp(s, a, &s.rfull[r.at], r.phase, 8u)) return;
+      const uint32_t slot = n0 % kRefs;
+      if (!wait_warp(s, a, &s.rfull[slot], (n0 / kRefs) & 1, 8u)) return;
       if (active) {
-        if (!wait_warp(s, a, &s.sfull[stream][sr.at], sr.phase, 9u)) return;
+        if (!wait_warp(s, a, &s.sfull[tile][parity], jobs & 1, 9u)) return;
+        ++jobs;
         tc_fence_after();
         float2 l[4];
 #pragma unroll
@@ -310,7 +332,7 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
 #pragma unroll 1
         for (int b = 0; b < rows; b += 32) {
           uint32_t x[32];
-          tmem_ld_x32(ts + sr.at * 128u + b, x);
+          tmem_ld_x32(ts + b, x);
           tmem_wait_ld();
           tmem_landed(x);
           if (b + 32 > rows) {  // (columns without a row hold anything)
@@ -323,7 +345,7 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
             for (int c = 0; c < 32; ++c)
               if (b + c < from) x[c] = 0xff800000u;
           }
-          const float4* ref = reinterpret_cast<const float4*>(s.ref[r.at] + b);
+          const float4* ref = reinterpret_cast<const float4*>(s.ref[slot] + b);
 #pragma unroll
           for (int c = 0; c < 32; c += 4) {
             const float4 f = ref[c / 4];
@@ -336,24 +358,44 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
         }
         total += ((l[0].x + l[0].y) + (l[1].x + l[1].y)) + ((l[2].x + l[2].y) + (l[3].x + l[3].y));
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s.sempty[stream][sr.at]);
-        sr.step();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&s.rempty[r.at]);
-      r.step();
+      if (lane == 0) {
+        if (active) mbar_arrive(&s.sempty[tile][parity]);
+        mbar_arrive(&s.rempty[slot]);
+      }
+    }
+    if (active && both) {
+      // (warps of the same keys wait for each other only, each time in both directions, so
+      // that neither's wait meets another phase)
+      if (!first) {
+        s.sum[tile][row] = total;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.mready[tile][warp]);
+        if (!wait_warp(s, a, &s.mdone[tile][warp], merges & 1, 11u)) return;
+      } else {
+        if (!wait_warp(s, a, &s.mready[tile][warp], merges & 1, 11u)) return;
+        total += s.sum[tile][row];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.mdone[tile][warp]);
+      }
+      ++merges;
     }
     if (at != nullptr) *at = fmaf(w.decay, before, total);
-    if (mine && it.tile0 != 0) w.next[(int64_t)blockIdx.x * kWeighSpan + k] = total;
+    if (mine && first && it.tile0 != 0) w.next[(int64_t)blockIdx.x * kWeighSpan + k] = total;
   }
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
     weigh_tc_kernel(const __grid_constant__ Maps m, const __grid_constant__ WeighArgs w) {
-  extern __shared__ uint8_t smem_raw[];
-  Smem& s = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t smem_raw[];  // (as the swizzled tiles want; no room to round up)
+  Smem& s = *reinterpret_cast<Smem*>(smem_raw);
   const AttendArgs& a = w.a;
+  if ((smem_u32(smem_raw) & 1023u) != 0) {
+    grid_wait();
+    if (threadIdx.x == 0) note(a, ECOKV_ERR_CUDA, 0u);
+    return;
+  }
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < kKeyTiles; ++i) {
@@ -363,16 +405,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kRowTiles; ++i) {
       mbar_init(&s.qfull[i], 1);
       mbar_init(&s.qempty[i], 1);
+    }
+    for (int i = 0; i < kRefs; ++i) {
       mbar_init(&s.rfull[i], 1);
-      mbar_init(&s.rempty[i], 8);  // the streams' warps
+      mbar_init(&s.rempty[i], 8);  // the warps of a parity's streams
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&s.sfull[i >> 1][i & 1], 1);
       mbar_init(&s.sempty[i >> 1][i & 1], 4);
     }
+    for (int i = 0; i < 8; ++i) {
+      mbar_init(&s.mready[i >> 2][i & 3], 1);
+      mbar_init(&s.mdone[i >> 2][i & 3], 1);
+    }
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&s.ifull[i], 1);
-      mbar_init(&s.iempty[i], 11);  // the warps of the copies, products and references, and the streams
+      mbar_init(&s.iempty[i], 19);  // the warps of the copies, products and references, and the streams
     }
     mbar_init(&s.drained, 1);
     s.abort = 0;
@@ -391,12 +439,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = s.tmem;
   Issued d;
   if (warp >= 4) {
-    add_up(s, w, tmem, (warp >> 2) - 1);
+    add_up(s, w, tmem, (warp - 4) >> 3, ((warp - 4) >> 2) & 1);
   } else if (warp == 0) {
     // (the injected stall: no tile ever comes)
     if (a.stall == 0) produce(s, w, m, lane, d);
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (elect_one()) {
       multiply(s, w, tmem);
       mma_commit(&s.drained);
     }
@@ -471,7 +519,7 @@ cudaError_t launch_weigh_tc(const WeighArgs& w, cudaStream_t st) {
     const uint32_t box[4] = {64, (uint32_t)(c.page_size < kKeys ? c.page_size : kKeys), 1, 1};
     if (!map_of(&m.ck, c.k, 4, dims, strides, box)) return cudaErrorInvalidValue;
   }
-  const int smem = (int)sizeof(Smem) + 1024;
+  const int smem = (int)sizeof(Smem);
   if (!g_attr_set[dev].load()) {  // a racing thread repeats the idempotent setting
     e = cudaFuncSetAttribute(weigh_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;

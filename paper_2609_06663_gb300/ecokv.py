@@ -597,16 +597,20 @@ def _dtype(t, *others):
 _codes = {}  # torch dtype -> code
 
 
-_int32 = None
+_int32 = _int64 = _float32 = None
+
+
+def _types():
+    global _int32, _int64, _float32
+    import torch
+    _int32, _int64, _float32 = torch.int32, torch.int64, torch.float32
 
 
 def _ints(x, shape, what, dev):
-    global _int32
     if x is None:
         return None
     if _int32 is None:
-        import torch
-        _int32 = torch.int32
+        _types()
     if x.dtype is not _int32 or x.get_device() != dev or not x.is_contiguous() or (shape and x.shape != shape):
         of = f" of shape {shape}" if shape else ""
         raise ValueError(f"{what}: a contiguous int32 tensor{of} on cuda:{dev} is wanted")
@@ -729,7 +733,8 @@ class PagedCache(_Handle):
     lengths are read on the device by every call, and written in place between them."""
 
     def __init__(self, k_pages, v_pages, table, lengths):
-        _, dev = _dtype(k_pages, v_pages)
+        self.dtype, dev = _dtype(k_pages, v_pages)
+        self.device = dev
         s = _strides(k_pages)
         if k_pages.dim() != 4 or k_pages.shape[3] != HEAD_DIM or s[3] != 1:
             raise ValueError(f"pages [n_pages, h_kv, page_size, {HEAD_DIM}] with the last axis contiguous are wanted")
@@ -738,7 +743,7 @@ class PagedCache(_Handle):
         if table.dim() != 2 or tuple(lengths.shape) != (table.shape[0],):
             raise ValueError("table [batch, pages a sequence] and lengths [batch] are wanted")
         self.k_pages, self.v_pages, self.table, self.lengths = k_pages, v_pages, table, lengths
-        self.batch, self.h_kv = table.shape[0], k_pages.shape[1]
+        self.batch, self.h_kv, self.slots = table.shape[0], k_pages.shape[1], k_pages.shape[:3]
         self.c = ecokv_pages(k_pages.data_ptr(), v_pages.data_ptr(), s[0], s[1], s[2], k_pages.shape[0],
                              k_pages.shape[2], _ints(table, None, "table", dev), table.shape[1],
                              _ints(lengths, None, "lengths", dev))
@@ -755,7 +760,7 @@ class Prefix(_Handle):
             raise ValueError(f"prefix: [h_kv, rows, {HEAD_DIM}], or [rows, {HEAD_DIM}] with head_off, is wanted")
         if v.shape != k.shape or _strides(v) != s:
             raise ValueError("k and v have different shapes or strides")
-        self.k, self.v, self.head_off = k, v, head_off
+        self.k, self.v, self.head_off, self.slots = k, v, head_off, k.shape[:-1]
         self.h_kv = k.shape[0] if head_off is None else head_off.shape[0] - 1
         self.c = ecokv_prefix(k.data_ptr(), v.data_ptr(), s[0] if head_off is None else 0, s[-2], k.shape[-2],
                               _ints(head_off, None, "head_off", dev))
@@ -794,8 +799,8 @@ def alloc_attend_workspace(tokens, batch, h_q, h_kv, dtype, device="cuda"):
 
 
 def _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us, stream):
-    """The arguments of ecokv_attend but for its last three: parameters, dtype, tensors and out; the workspace; the
-    stream; out itself."""
+    """What ecokv_attend and ecokv_attend_tree are given: parameters, dtype, prefix, cache, starts, the workspace and
+    its bytes, the stream; and out."""
     if out is None:
         out = _like(q, stream)
     if prefix is None and cache is None:
@@ -811,41 +816,48 @@ def _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us, st
         _lse(lse, tokens, h_q, dev)
     if ws is None:
         ws = _made(stream, q, lambda: alloc_attend_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device))
-    _same_device(ws, dev)
+    ws, room = _workspace(ws, dev)
     p = ecokv_attend_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, qt, qh, ot, oh, flags, timeout_us)
     return p, dt, None if prefix is None else prefix.c, None if cache is None else cache.c, \
-        None if cache is None else _ints(starts, (batch + 1,), "starts", dev), ws, _on(stream, dev), out
+        None if cache is None else _ints(starts, (batch + 1,), "starts", dev), ws, room, _on(stream, dev), out
 
 
 def _lse(lse, tokens, h_q, dev):
-    if str(lse.dtype) != "torch.float32" or tuple(lse.shape) != (tokens, h_q) or not lse.is_contiguous() or \
-            lse.get_device() != dev:
+    if _float32 is None:
+        _types()
+    if lse.dtype is not _float32 or lse.shape != (tokens, h_q) or not lse.is_contiguous() or lse.get_device() != dev:
         raise ValueError(f"lse: a contiguous float32 [tokens, h_q] tensor on cuda:{dev} is wanted")
 
 
-def _same_device(ws, dev):
-    if ws is not None and ws.get_device() != dev:
+def _workspace(ws, dev):
+    """Its address and bytes."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev:
         raise ValueError(f"the workspace is on {ws.device}, the tensors on cuda:{dev}")
+    return ws.data_ptr(), ws.numel()
 
 
 def attend(q, prefix, cache, starts=None, scale=0.0, out=None, lse=None, ws=None, flags=0, timeout_us=0, stream=None):
     """Run ecokv_attend: q [tokens, h_q, 128] over prefix (a Prefix or None) and
     cache (a PagedCache or None); returns out [tokens, h_q, 128].  starts int32
     [batch + 1]: None = one token a sequence.  lse: float32 [tokens, h_q] to fill."""
-    p, dt, pre, pages, starts, ws, on, out = _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us,
-                                                     stream)
-    _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), pre, pages, starts, out.data_ptr(), _ptr(lse),
-                                        ws.data_ptr(), ws.numel(), on), "ecokv_attend")
+    p, dt, pre, pages, starts, ws, room, on, out = _attend(q, prefix, cache, starts, scale, out, lse, ws, flags,
+                                                           timeout_us, stream)
+    _check((_lib or lib()).ecokv_attend(p, dt, q.data_ptr(), pre, pages, starts, out.data_ptr(), _ptr(lse), ws, room,
+                                        on), "ecokv_attend")
     return out
 
 
 # ---------------------------------------------------------------- drafted tokens
 def _mask(mask, tokens, dev):
     """Words of a tree's mask."""
-    if str(mask.dtype) != "torch.int64" or mask.dim() != 2 or mask.shape[0] != tokens or not mask.is_contiguous() or \
-            mask.get_device() != dev:
+    if _int64 is None:
+        _types()
+    n = mask.shape
+    if mask.dtype is not _int64 or len(n) != 2 or n[0] != tokens or not mask.is_contiguous() or mask.get_device() != dev:
         raise ValueError(f"mask: a contiguous int64 [tokens, words] tensor on cuda:{dev} is wanted")
-    return mask.shape[1]
+    return n[1]
 
 
 def tree_mask(parents, starts=None, mask=None, words=None, ws=None, stream=None):
@@ -861,25 +873,23 @@ def tree_mask(parents, starts=None, mask=None, words=None, ws=None, stream=None)
     tokens = parents.numel()
     if mask is None:
         n = words or (min(max(1, -(-tokens // 64)), 64) if starts is not None else 1)
-        mask = _made(stream, parents, lambda: parents.new_empty((tokens, n), dtype=_torch().int64))
+        if _int64 is None:
+            _types()
+        mask = _made(stream, parents, lambda: parents.new_empty((tokens, n), dtype=_int64))
     n = _mask(mask, tokens, dev)
     if words is not None and n != words:
         raise ValueError(f"a mask of {n} words, {words} were asked for")
-    if starts is not None and (starts.dim() != 1 or starts.shape[0] < 2):
-        raise ValueError("starts [batch + 1] are wanted")
-    batch = tokens if starts is None else starts.shape[0] - 1
-    _same_device(ws, dev)
+    batch = tokens
+    if starts is not None:
+        batch = starts.numel() - 1
+        if batch < 1:
+            raise ValueError("starts [batch + 1] are wanted")
+    ws, room = _workspace(ws, dev)
     if tokens:
         _check((_lib or lib()).ecokv_tree_mask(_ints(parents, (tokens,), "parents", dev),
-                                               _ints(starts, None, "starts", dev), tokens, batch, mask.data_ptr(), n,
-                                               _ptr(ws), 0 if ws is None else ws.numel(), _on(stream, dev)),
-               "ecokv_tree_mask")
+                                               _ints(starts, (batch + 1,), "starts", dev), tokens, batch,
+                                               mask.data_ptr(), n, ws, room, _on(stream, dev)), "ecokv_tree_mask")
     return mask
-
-
-def _torch():
-    import torch
-    return torch
 
 
 def attend_tree(q, prefix, cache, mask, starts=None, scale=0.0, out=None, lse=None, ws=None, flags=0, timeout_us=0,
@@ -889,22 +899,26 @@ def attend_tree(q, prefix, cache, mask, starts=None, scale=0.0, out=None, lse=No
     (int64 [tokens, words], from tree_mask() or any other)."""
     if cache is None:
         raise ValueError("a cache is wanted")
-    p, dt, pre, pages, starts, ws, on, out = _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us,
-                                                     stream)
+    p, dt, pre, pages, starts, ws, room, on, out = _attend(q, prefix, cache, starts, scale, out, lse, ws, flags,
+                                                           timeout_us, stream)
     words = _mask(mask, p.tokens, q.get_device())
     _check((_lib or lib()).ecokv_attend_tree(p, dt, q.data_ptr(), pre, pages, starts, mask.data_ptr(), words,
-                                             out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(), on),
-           "ecokv_attend_tree")
+                                             out.data_ptr(), _ptr(lse), ws, room, on), "ecokv_attend_tree")
     return out
 
 
 def _weights(w, shape, what, dev):
     """Weights [n_pages, h_kv, page_size] of a cache, [h_kv, rows] or [rows] of a prefix."""
-    if str(w.dtype) != "torch.float32" or tuple(w.shape) != tuple(shape) or w.get_device() != dev:
+    if _float32 is None:
+        _types()
+    n = w.shape
+    if w.dtype is not _float32 or n != shape or w.get_device() != dev:
         raise ValueError(f"{what}: a float32 tensor of shape {tuple(shape)} on cuda:{dev} is wanted")
+    s = w.stride()
     # (a stride that is never taken counts as one)
-    s = tuple(x if n > 1 else 1 for n, x in zip(w.shape, w.stride()))
-    return ecokv_weights(w.data_ptr(), *((1,) * (3 - len(s)) + s))
+    if len(n) == 3:
+        return ecokv_weights(w.data_ptr(), s[0] if n[0] > 1 else 1, s[1] if n[1] > 1 else 1, s[2] if n[2] > 1 else 1)
+    return ecokv_weights(w.data_ptr(), 1, 1 if len(n) == 1 or n[0] <= 1 else s[0], s[-1] if n[-1] > 1 else 1)
 
 
 def commit(cache, accepted, counts, starts=None, weights=None, lengths_out=None, tokens=None, ws=None, stream=None):
@@ -913,21 +927,21 @@ def commit(cache, accepted, counts, starts=None, weights=None, lengths_out=None,
     [n_pages, h_kv, page_size] where given.  accepted int32 [batch, most], counts int32
     [batch]; starts as in attend_tree() (tokens: starts' last; by default no limit but
     theirs).  Returns the new lengths, lengths_out where given (the cache's own lengths too)."""
-    dt, dev = _dtype(cache.k_pages)
+    dt, dev = cache.dtype, cache.device
     batch = cache.batch
-    if accepted.dim() != 2 or accepted.shape[0] != batch or accepted.shape[1] < 1:
+    n = accepted.shape
+    if len(n) != 2 or n[0] != batch or n[1] < 1:
         raise ValueError("accepted [batch, most] is wanted")
     if lengths_out is None:
         lengths_out = _like(cache.lengths, stream)
     if tokens is None:
         tokens = batch if starts is None else 2 ** 31 - 1
-    _same_device(ws, dev)
+    ws, room = _workspace(ws, dev)
     _check((_lib or lib()).ecokv_commit(
-        dt, cache.c, cache.h_kv, _ints(accepted, None, "accepted", dev), accepted.shape[1],
-        _ints(counts, (batch,), "counts", dev), _ints(starts, (batch + 1,), "starts", dev), tokens, batch,
-        None if weights is None else _weights(weights, cache.k_pages.shape[:3], "weights", dev),
-        _ints(lengths_out, (batch,), "lengths_out", dev), _ptr(ws), 0 if ws is None else ws.numel(),
-        _on(stream, dev)), "ecokv_commit")
+        dt, cache.c, cache.h_kv, _ints(accepted, None, "accepted", dev), n[1], _ints(counts, (batch,), "counts", dev),
+        _ints(starts, (batch + 1,), "starts", dev), tokens, batch,
+        None if weights is None else _weights(weights, cache.slots, "weights", dev),
+        _ints(lengths_out, (batch,), "lengths_out", dev), ws, room, _on(stream, dev)), "ecokv_commit")
     return lengths_out
 
 
@@ -961,19 +975,19 @@ def weigh(q, lse, prefix, cache, prefix_weights=None, weights=None, starts=None,
     if prefix is not None:
         if prefix_weights is None:
             raise ValueError("prefix_weights are wanted")
-        pw = _weights(prefix_weights, prefix.k.shape[:-1], "prefix_weights", dev)
+        pw = _weights(prefix_weights, prefix.slots, "prefix_weights", dev)
     if cache is not None:
         if weights is None:
             raise ValueError("weights are wanted")
-        w = _weights(weights, cache.k_pages.shape[:3], "weights", dev)
+        w = _weights(weights, cache.slots, "weights", dev)
     if ws is None:
         ws = _made(stream, q, lambda: alloc_weigh_workspace(tokens, batch, h_q, h_kv, q.dtype, q.device))
-    _same_device(ws, dev)
+    ws, room = _workspace(ws, dev)
     p = ecokv_weigh_params(h_q, h_kv, HEAD_DIM, tokens, batch, scale, decay, qt, qh, flags, timeout_us)
     _check((_lib or lib()).ecokv_weigh(p, dt, q.data_ptr(), lse.data_ptr(), None if prefix is None else prefix.c,
                                        None if cache is None else cache.c,
                                        None if cache is None else _ints(starts, (batch + 1,), "starts", dev), pw, w,
-                                       ws.data_ptr(), ws.numel(), _on(stream, dev)), "ecokv_weigh")
+                                       ws, room, _on(stream, dev)), "ecokv_weigh")
     return prefix_weights, weights
 
 
@@ -986,22 +1000,24 @@ def prune(cache, weights, budget, limit=None, first=0, recent=0, to=None, to_wei
     are not moved; `weights` itself in the same cache).  Returns (new lengths, idx int32
     [batch, h_kv, limit]: the slots kept, then -1); lengths_out may be either cache's lengths."""
     limit = budget if limit is None else limit
-    dt, dev = _dtype(cache.k_pages, None if to is None else to.k_pages)
+    dt, dev = cache.dtype, cache.device
+    if to is not None:
+        _dtype(cache.k_pages, to.k_pages)
     batch, h_kv = cache.batch, cache.h_kv
     if to is not None and (to.batch != batch or to.h_kv != h_kv):
         raise ValueError("the caches do not fit")
     if limit < 1:
         raise ValueError("a limit of one slot at least is wanted")
-    w = _weights(weights, cache.k_pages.shape[:3], "weights", dev)
-    tw = None if to_weights is None else _weights(to_weights, (to or cache).k_pages.shape[:3], "to_weights", dev)
+    w = _weights(weights, cache.slots, "weights", dev)
+    tw = None if to_weights is None else _weights(to_weights, (to or cache).slots, "to_weights", dev)
     if lengths_out is None:
         lengths_out = _like(cache.lengths, stream)
     if idx is None:
         idx = _made(stream, cache.lengths, lambda: cache.lengths.new_empty((batch, h_kv, limit)))
-    _same_device(ws, dev)
+    ws, room = _workspace(ws, dev)
     p = ecokv_prune_params(h_kv, batch, budget, limit, first, recent)
     _check((_lib or lib()).ecokv_prune(p, dt, cache.c, w, None if to is None else to.c, tw,
                                        _ints(idx, (batch, h_kv, limit), "idx", dev),
-                                       _ints(lengths_out, (batch,), "lengths_out", dev), _ptr(ws),
-                                       0 if ws is None else ws.numel(), _on(stream, dev)), "ecokv_prune")
+                                       _ints(lengths_out, (batch,), "lengths_out", dev), ws, room,
+                                       _on(stream, dev)), "ecokv_prune")
     return lengths_out, idx
