@@ -381,6 +381,16 @@ static ecokv_status attend(const ecokv_attend_params* p, ecokv_dtype dtype, cons
   a.h_kv = p->h_kv;
   a.g = p->h_q / p->h_kv;
   a.tpt = (tc ? kTileRows : 64) / a.g;
+  // A tree on CUDA cores: rows in smaller tiles where there would be few of them, down to 16
+  // (16 rows of an item take a fifth of the time of 64: 8 trees of up to 13 drafts, 8 heads,
+  // 128 rows before them XX us and not 29.9)
+  if (!tc && mask != nullptr) {
+    int rows = 64;
+    while (rows > 16 && rows / 2 >= a.g &&
+           (double)a.h_kv * div_up(a.tokens, rows / a.g) * (tiles_of(a.prefix.rows) + 1) < 2.0 * attend_sms())
+      rows /= 2;
+    a.tpt = rows / a.g;
+  }
   a.span = tc ? 2 * a.tpt : a.tpt;
   a.parts = tc ? 2 : 1;
   a.lead = tc ? 1 : 0;

@@ -74,6 +74,19 @@ __device__ __forceinline__ int64_t key_offset(const AttendArgs& a, const Item& i
          (int64_t)(j & (a.cache.page_size - 1)) * a.cache.slot_stride;
 }
 
+// Bits of the keys of tile t that token k of the item (of a tree's own slots) sees: bit c of
+// word q is key 32 q + c.
+__device__ __forceinline__ void tree_bits(const AttendArgs& a, const Item& it, int k, int t, uint32_t (&bits)[4]) {
+  const int d = t * kKeys - it.lim0, w = d >> 5;
+  const uint32_t* row = a.mask + (int64_t)(it.tok0 + k) * a.words;
+  uint32_t lo = tree_word(a, row, w);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t hi = tree_word(a, row, w + q + 1);
+    bits[q] = __funnelshift_r(lo, hi, d & 31);
+    lo = hi;
+  }
+}
 // Whether token k of the item sees key j of its tile.
 template <bool kTree>
 __device__ __forceinline__ bool sees(const AttendArgs& a, const Item& it, int k, int j) {
@@ -265,6 +278,12 @@ __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const It
     if (t + 1 < it.tile0 + it.ntiles) look_up(t + 1);
     __syncthreads();
     const int nv = min(it.vis - t * kKeys, kKeys), nc = (nv + 15) >> 4;  // keys that are there, in sixteens
+    uint32_t see[R][4];
+    const bool drafts = kTree && it.source != 0 && (t + 1) * kKeys > it.lim0;
+    if (drafts) {  // (on their way while the scores are formed)
+#pragma unroll
+      for (int r = 0; r < R; ++r) tree_bits(a, it, min((ty * R + r) / a.g, it.ntok - 1), t, see[r]);
+    }
     float x[R][8];
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -294,7 +313,8 @@ __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const It
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         const int j = t * kKeys + tx + 16 * c;
-        const bool seen = kTree ? sees<true>(a, it, min((ty * R + r) / a.g, it.ntok - 1), j) : j < lim[r];
+        bool seen = kTree && it.source != 0 ? j < it.vis : j < lim[r];
+        if (drafts) seen = seen && (see[r][c >> 1] >> (tx + 16 * (c & 1)) & 1u) != 0u;
         x[r][c] = seen ? x[r][c] * a.scale_log2 : -INFINITY;
         mx = fmaxf(mx, x[r][c]);
       }

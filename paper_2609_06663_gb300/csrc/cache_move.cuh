@@ -17,8 +17,7 @@
 
 namespace ecokv {
 
-constexpr int kMoveThreads = 256;
-constexpr int kMoveRows = 8;  // rows whose pieces a thread has in flight
+constexpr int kMoveBytes = 32 * 1024;  // of a chunk of one CTA
 
 struct MoveArgs {
   ecokv_pages from, to;           // the same pages in one cache
@@ -26,7 +25,8 @@ struct MoveArgs {
   int from_shift, to_shift;
   int h_kv, batch;
   int ctas;                       // of a unit
-  int in_place;                   // these are a cluster
+  int cluster;                    // CTAs that wait for each other
+  int in_place;
   unsigned* status;               // may be NULL
 };
 
@@ -58,13 +58,16 @@ __device__ __forceinline__ int64_t offset_of(const ecokv_weights& w, Place p, in
 }
 
 // One CTA's share of the rows [i0, n) of unit (b, h, kv): row i from slot src(i) to slot dst0 +
-// i.  src: row number -> slot, the same in every CTA.  E: bytes an element.
-template <int E, typename Src>
+// i.  src: row number -> slot, the same in every CTA.  E: bytes an element.  All of the
+// cluster's CTAs call it with the same i0 and n.
+template <int E, int kThreads, typename Src>
 __device__ __forceinline__ void move_rows(const MoveArgs& a, int b, int h, int kv, int rank, int i0, int n, int dst0,
                                           Src src) {
   constexpr int kLanes = kD * E / 16;               // lanes a row
-  constexpr int kAtOnce = kMoveThreads / kLanes;    // rows a step of the CTA
-  constexpr int kChunk = kAtOnce * kMoveRows;
+  constexpr int kAtOnce = kThreads / kLanes;        // rows a step of the CTA
+  constexpr int kChunk = kMoveBytes / (kD * E);
+  constexpr int kMoveRows = kChunk / kAtOnce;       // rows whose pieces a thread has in flight
+  static_assert(kChunk <= kThreads, "a thread a row");
   // bytes from k or v, from and to; from < 0: the row stays.  (Three chunks': while a warp
   // looks the next up, another may still write the one before.)
   __shared__ longlong2 places[3][kChunk];
@@ -109,7 +112,7 @@ __device__ __forceinline__ void move_rows(const MoveArgs& a, int b, int h, int k
     const float w_now = w;
     float* const w_to = w_at;
     if (base + kChunk * a.ctas < n) look_up(base + kChunk * a.ctas, next);
-    if (a.in_place && a.ctas > 1) cooperative_groups::this_cluster().sync();
+    if (a.in_place && a.cluster > 1) cooperative_groups::this_cluster().sync();
     else __syncthreads();
 #pragma unroll
     for (int k = 0; k < kMoveRows; ++k) {
@@ -121,31 +124,24 @@ __device__ __forceinline__ void move_rows(const MoveArgs& a, int b, int h, int k
   }
 }
 
-// Launch `kernel` with a.ctas CTAs a unit, as clusters where they wait for each other.
+// Launch `kernel` in clusters of a.cluster CTAs.
 template <typename... A>
-cudaError_t launch_move(void (*kernel)(A...), const MoveArgs& a, cudaStream_t st, const A&... args) {
+cudaError_t launch_move(void (*kernel)(A...), const MoveArgs& a, unsigned grid, unsigned threads, size_t smem,
+                        cudaStream_t st, const A&... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(a.batch * a.h_kv * 2 * a.ctas));
-  cfg.blockDim = dim3(kMoveThreads);
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = a.in_place ? (unsigned)a.ctas : 1u;
+  attr[1].val.clusterDim.x = (unsigned)a.cluster;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
-// CTAs a unit of up to `rows` rows has: as many as it has chunks for, while all units'
-// CTAs together are no more than two an SM (152 SMs), a power of two up to a cluster's eight.
-inline int move_ctas(int64_t units, int64_t rows, ecokv_dtype dt) {
-  const int64_t chunk = (int64_t)kMoveThreads * 16 / (kD * (dt == ECOKV_F32 ? 4 : 2)) * kMoveRows;
-  int c = 1;
-  while (c < 8 && units * c < 152 && chunk * c < rows) c *= 2;
-  return c;
 }
 
 inline bool weights_ok(const ecokv_weights* w) {

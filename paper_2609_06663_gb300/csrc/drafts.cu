@@ -111,20 +111,22 @@ __device__ __forceinline__ Path read_path(const CommitArgs& a, int b) {
   return p;
 }
 
+constexpr int kThreads = 256;
+
 template <int E>
-__global__ void __launch_bounds__(kMoveThreads, 4) commit_kernel(const __grid_constant__ CommitArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) commit_kernel(const __grid_constant__ CommitArgs a) {
   ptx::grid_trigger();
   ptx::grid_wait();
-  const int unit = blockIdx.x / a.m.ctas, rank = blockIdx.x - unit * a.m.ctas;
+  const int unit = blockIdx.x;
   const int kv = unit & 1, h = (unit >> 1) % a.m.h_kv, b = (unit >> 1) / a.m.h_kv;
   const Path p = read_path(a, b);
   const int32_t* list = a.accepted + (int64_t)b * a.stride;
-  move_rows<E>(a.m, b, h, kv, rank, 0, p.n, p.base, [=](int i) { return p.base + list[i]; });
-  if (a.lengths_out != nullptr && h == 0 && kv == 0 && rank == 0 && threadIdx.x == 0) a.lengths_out[b] = p.base + p.n;
+  move_rows<E, kThreads>(a.m, b, h, kv, 0, 0, p.n, p.base, [=](int i) { return p.base + list[i]; });
+  if (a.lengths_out != nullptr && h == 0 && kv == 0 && threadIdx.x == 0) a.lengths_out[b] = p.base + p.n;
 }
 
 // The lengths alone, once nothing reads the old ones any more.
-__global__ void __launch_bounds__(kMoveThreads) commit_lengths_kernel(const __grid_constant__ CommitArgs a) {
+__global__ void __launch_bounds__(64) commit_lengths_kernel(const __grid_constant__ CommitArgs a) {
   ptx::grid_trigger();
   ptx::grid_wait();
   const Path p = read_path(a, blockIdx.x);
@@ -179,7 +181,7 @@ ecokv_status ecokv_commit(ecokv_dtype dtype, const ecokv_pages* cache, int32_t h
   a.m.batch = batch;
   a.m.in_place = 1;
   a.m.status = static_cast<unsigned*>(ws);
-  a.m.ctas = 1;
+  a.m.ctas = a.m.cluster = 1;
   a.accepted = accepted;
   a.counts = counts;
   a.starts = starts;
@@ -189,7 +191,9 @@ ecokv_status ecokv_commit(ecokv_dtype dtype, const ecokv_pages* cache, int32_t h
   const bool same = lengths_out == cache->lengths;
   a.lengths_out = same ? nullptr : lengths_out;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = dtype == ECOKV_F32 ? launch_move(commit_kernel<4>, a.m, s, a) : launch_move(commit_kernel<2>, a.m, s, a);
+  const unsigned grid = (unsigned)(2 * batch * h_kv);
+  cudaError_t e = dtype == ECOKV_F32 ? launch_move(commit_kernel<4>, a.m, grid, kThreads, 0, s, a)
+                                     : launch_move(commit_kernel<2>, a.m, grid, kThreads, 0, s, a);
   if (e == cudaSuccess && same) {
     a.lengths_out = lengths_out;
     e = launch_behind(commit_lengths_kernel, (unsigned)batch, 64, 0, s, a);

@@ -19,6 +19,7 @@
 namespace ecokv {
 
 constexpr int kWeighSpan = 256;  // most keys an item has
+constexpr int kMaxWeighCtas = 2 * kMaxAttendSms;
 
 struct WeighItem {
   int source, head, seq;  // as in Item

@@ -35,8 +35,8 @@ struct WeighLayout {
 WeighLayout weigh_layout() {
   WeighLayout L{};
   L.item = 256;  // the status word
-  L.next = L.item + ((kMaxAttendSms * sizeof(WeighItem) + 255) & ~(size_t)255);
-  L.total = L.next + (size_t)kMaxAttendSms * kWeighSpan * sizeof(float);
+  L.next = L.item + ((kMaxWeighCtas * sizeof(WeighItem) + 255) & ~(size_t)255);
+  L.total = L.next + (size_t)kMaxWeighCtas * kWeighSpan * sizeof(float);
   return L;
 }
 
@@ -124,6 +124,7 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
   // a sequence's own row tiles have room for twice the mean of its tokens: what is copied and
   // multiplied of a decode step's single rows is no more than they are
   const int mean = a.starts != nullptr ? div_up(a.tokens, a.batch) : 1;
+  if (!tc && a.tokens > w.tpt[0]) w.tpt[0] = div_up(a.tokens, div_up(a.tokens, w.tpt[0]));  // equal row tiles
   w.tpt[1] = a.starts != nullptr && 2 * mean < w.tpt[0] ? 2 * mean : a.starts != nullptr ? w.tpt[0] : 1;
   // (a unit: about 600 cycles of a CTA, an item of 256 keys with one row tile 5 of them, each row
   // tile of 128 rows 4; on CUDA cores 16 rows of a tile, which take as long as the keys)
@@ -135,7 +136,7 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
   if (a.h_kv * (of_prefix + (double)p->batch * items) * most > 4e18) return ECOKV_ERR_UNSUPPORTED;
   const WeighLayout L = weigh_layout();
   if (ws == nullptr || !aligned16(ws) || ws_bytes < L.total) return ECOKV_ERR_WORKSPACE;
-  a.P = attend_sms();
+  a.P = attend_sms() * (tc ? 1 : 2);
   char* base = static_cast<char*>(ws);
   a.status = reinterpret_cast<unsigned*>(base);
   w.next_item = reinterpret_cast<WeighItem*>(base + L.item);

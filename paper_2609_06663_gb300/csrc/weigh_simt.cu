@@ -8,7 +8,9 @@
 //
 // Items of more rows: keys and rows of a tile in shared memory as fp32; thread (ty, tx) of
 // 16 x 16 forms the scores of its four rows with the keys tx + 16 j and adds their
-// exponentials to the keys' sums, which sixteen threads join at the item's end.
+// exponentials to the keys' sums, which sixteen threads join at the item's end (three, two or
+// one row a thread where a tile has no more).  Two CTAs an SM, so that one's products run
+// beside the other's loads.
 
 #include <math.h>
 
@@ -34,7 +36,7 @@ struct Smem {
   WeighItem item;
   int more;
 };
-static_assert(sizeof(Smem) <= 232448, "one CTA's shared memory");
+static_assert(2 * (sizeof(Smem) + 1024) <= 233472, "two CTAs' shared memory");
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
@@ -117,9 +119,54 @@ __device__ __forceinline__ void item_few(const WeighArgs& w, Smem& s, const Weig
   if (half == 0 && k < it.nkeys) put(w, it, k, sum);
 }
 
+// The exponentials of a row tile's scores, added over its rows by sixteenth: R rows a thread.
+template <int R>
+__device__ __forceinline__ void add_rows(const WeighArgs& w, const Smem& s, const WeighItem& it, int t, int rows,
+                                         float (&total)[8]) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, nc = (it.nkeys + 15) >> 4;  // keys that are there, in sixteens
+  float x[R][8];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[r][c] = 0.f;
+#pragma unroll 1
+  for (int e = 0; e < kD; e += 4) {
+    float4 q4[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(&s.q[ty * R + r][e]);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      if (c >= nc) break;
+      const float4 k4 = *reinterpret_cast<const float4*>(&s.k[tx + 16 * c][e]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        x[r][c] = fmaf(q4[r].x, k4.x, x[r][c]);
+        x[r][c] = fmaf(q4[r].y, k4.y, x[r][c]);
+        x[r][c] = fmaf(q4[r].z, k4.z, x[r][c]);
+        x[r][c] = fmaf(q4[r].w, k4.w, x[r][c]);
+      }
+    }
+  }
+  float sum[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) sum[c] = 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = ty * R + r;
+    if (row < rows) {  // (what shared memory holds past them may be anything)
+      const float ref = s.ref[row];
+      const int seen = it.source == 0 ? it.nkeys : it.base + t * w.tpt[1] + row / w.a.g + 1 - it.key0;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (tx + 16 * c < seen) sum[c] += ptx::ex2(fmaf(x[r][c], w.a.scale_log2, ref));
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) total[c] += sum[c];
+}
+
 template <typename T>
 __device__ __forceinline__ void item_rows(const WeighArgs& w, Smem& s, const WeighItem& it) {
-  constexpr int R = kRows / 16;
   const AttendArgs& a = w.a;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31, warp = tid >> 5;
   const T* K = static_cast<const T*>(it.source == 0 ? a.prefix.k : a.cache.k);
@@ -140,52 +187,16 @@ __device__ __forceinline__ void item_rows(const WeighArgs& w, Smem& s, const Wei
   float total[8];
 #pragma unroll
   for (int c = 0; c < 8; ++c) total[c] = 0.f;
-  const int nc = (it.nkeys + 15) >> 4;  // keys that are there, in sixteens
 #pragma unroll 1
   for (int t = it.tile0; t < it.tile0 + it.ntiles; ++t) {
     const int rows = min(it.ntok - t * tpt, tpt) * a.g;
     __syncthreads();
     load_rows<T>(w, s, it, t, rows);
     __syncthreads();
-    float x[R][8];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int c = 0; c < 8; ++c) x[r][c] = 0.f;
-#pragma unroll 1
-    for (int e = 0; e < kD; e += 4) {
-      float4 q4[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(&s.q[ty * R + r][e]);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        if (c >= nc) break;
-        const float4 k4 = *reinterpret_cast<const float4*>(&s.k[tx + 16 * c][e]);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          x[r][c] = fmaf(q4[r].x, k4.x, x[r][c]);
-          x[r][c] = fmaf(q4[r].y, k4.y, x[r][c]);
-          x[r][c] = fmaf(q4[r].z, k4.z, x[r][c]);
-          x[r][c] = fmaf(q4[r].w, k4.w, x[r][c]);
-        }
-      }
-    }
-    float sum[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) sum[c] = 0.f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int row = ty * R + r;
-      if (row < rows) {  // (what shared memory holds past them may be anything)
-        const float ref = s.ref[row];
-        const int seen = it.source == 0 ? it.nkeys : it.base + t * tpt + row / a.g + 1 - it.key0;
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (tx + 16 * c < seen) sum[c] += ptx::ex2(fmaf(x[r][c], a.scale_log2, ref));
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < 8; ++c) total[c] += sum[c];
+    if (rows <= 16) add_rows<1>(w, s, it, t, rows, total);
+    else if (rows <= 32) add_rows<2>(w, s, it, t, rows, total);
+    else if (rows <= 48) add_rows<3>(w, s, it, t, rows, total);
+    else add_rows<4>(w, s, it, t, rows, total);
   }
   __syncthreads();
 #pragma unroll
@@ -200,7 +211,7 @@ __device__ __forceinline__ void item_rows(const WeighArgs& w, Smem& s, const Wei
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 1) weigh_simt_kernel(const __grid_constant__ WeighArgs w) {
+__global__ void __launch_bounds__(kThreads, 2) weigh_simt_kernel(const __grid_constant__ WeighArgs w) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Smem& s = *reinterpret_cast<Smem*>(smem_raw);
   const int lane = threadIdx.x & 31;
