@@ -233,7 +233,7 @@ typedef struct {
  *                 (a path from the root does)
  *   counts      : int32 [batch], 0 <= counts[b] <= T_b, stride
  *   weights     : of the cache, or NULL
- *   lengths_out : int32 [batch]; may be the cache's lengths, else it does not overlap them
+ *   lengths_out : int32 [batch]; may be the cache's lengths, else it overlaps no input
  * A sequence's pages with new tokens are its own.  A sequence with numbers out of
  * range or out of order keeps none of its drafts (as with counts[b] = 0), a row whose
  * page number is out of range is not moved, and each sets ECOKV_ERR_DEVICE_INDEX in the
@@ -281,17 +281,18 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
 /* ------------------------------------------------------------------ pruning
  * A sequence of more than `limit` slots keeps `budget` of them in each head: the
  * `first` first ones, the `recent` last ones and between them the ones of the
- * largest weights (of equal ones the lower slot; NaN counts below every number); its
- * other heads choose for themselves.  The rows kept, in their order, take slots 0 ..
+ * largest weights (of equal ones the lower slot; NaN counts below every number), each
+ * head for itself.  The rows kept, in their order, take slots 0 ..
  * of the same cache, or of another one.
  *   0 <= first, 0 <= recent, first + recent <= budget, 1 <= budget <= limit
  *   to          : NULL = the same cache; else one of the same dtype whose pages in use are no
  *                 pages in use of `cache`; its table has entries for the rows kept, its
  *                 lengths are not read.  Sequences of up to `limit` slots are copied whole.
- *   to_weights  : where the kept rows' weights go (may be `weights`, in the same
- *                 cache), NULL = they are not moved
+ *   to_weights  : where the kept rows' weights go (in the same cache: `weights` itself),
+ *                 NULL = they are not moved
  *   idx         : out, int32 [batch][h_kv][limit], the kept slots, then -1
- *   lengths_out : int32 [batch], min(budget or lengths[b]); may be the lengths of either cache
+ *   lengths_out : int32 [batch], budget or, up to limit, lengths[b]; may be the lengths of
+ *                 either cache, else it overlaps no input
  * Slots in use belong to one sequence each.  A slot whose page number is out of range has
  * weight -inf and its row is not moved; a length out of range is clamped; each sets
  * ECOKV_ERR_DEVICE_INDEX in the status word of ws (may be NULL, else at least 256

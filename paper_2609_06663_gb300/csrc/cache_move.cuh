@@ -148,10 +148,14 @@ inline bool weights_ok(const ecokv_weights* w) {
   return w->w != nullptr && ((uintptr_t)w->w & 3u) == 0 && w->page_stride > 0 && w->head_stride > 0 &&
          w->slot_stride > 0;
 }
+// Whether n int32 at x and m at y have none in common.
+inline bool apart(const void* x, int64_t n, const void* y, int64_t m) {
+  const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
+  return a + (uintptr_t)n * 4 <= b || b + (uintptr_t)m * 4 <= a;
+}
 // lengths_out is the lengths, or apart from them.
 inline bool lengths_ok(const int32_t* lengths, const int32_t* out, int32_t batch) {
-  const uintptr_t x = (uintptr_t)lengths, y = (uintptr_t)out, n = (uintptr_t)batch * 4;
-  return out != nullptr && (y & 3u) == 0 && (x == y || x + n <= y || y + n <= x);
+  return out != nullptr && ((uintptr_t)out & 3u) == 0 && (out == lengths || apart(lengths, batch, out, batch));
 }
 
 }  // namespace ecokv

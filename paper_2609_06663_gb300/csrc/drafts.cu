@@ -168,7 +168,9 @@ ecokv_status ecokv_commit(ecokv_dtype dtype, const ecokv_pages* cache, int32_t h
   const ecokv_status st = check_pages(cache, batch, dtype);
   if (st != ECOKV_OK) return st;
   if (!accepted || !counts || ((uintptr_t)accepted & 3u) || ((uintptr_t)counts & 3u) || ((uintptr_t)starts & 3u) ||
-      (starts == nullptr && tokens != batch) || !lengths_ok(cache->lengths, lengths_out, batch))
+      (starts == nullptr && tokens != batch) || !lengths_ok(cache->lengths, lengths_out, batch) ||
+      !apart(counts, batch, lengths_out, batch) || !apart(accepted, (int64_t)batch * stride, lengths_out, batch) ||
+      (starts != nullptr && !apart(starts, (int64_t)batch + 1, lengths_out, batch)))
     return ECOKV_ERR_INVALID_ARG;
   if (weights != nullptr && !weights_ok(weights)) return ECOKV_ERR_INVALID_ARG;
   if ((int64_t)batch * h_kv > 1 << 29) return ECOKV_ERR_UNSUPPORTED;

@@ -271,8 +271,16 @@ extern "C" ecokv_status ecokv_prune(const ecokv_prune_params* p, ecokv_dtype dty
   if (st != ECOKV_OK) return st;
   if (weights == nullptr || !weights_ok(weights) || (to_weights != nullptr && !weights_ok(to_weights)))
     return ECOKV_ERR_INVALID_ARG;
-  if (!idx || ((uintptr_t)idx & 3u) || !lengths_ok(cache->lengths, lengths_out, p->batch)) return ECOKV_ERR_INVALID_ARG;
+  // (in the same cache rows that stay in place are not touched, nor are their weights)
+  if (to == nullptr && to_weights != nullptr &&
+      (to_weights->w != weights->w || to_weights->page_stride != weights->page_stride ||
+       to_weights->head_stride != weights->head_stride || to_weights->slot_stride != weights->slot_stride))
+    return ECOKV_ERR_INVALID_ARG;
   if ((int64_t)p->batch * p->h_kv > 1 << 29) return ECOKV_ERR_UNSUPPORTED;
+  if (!idx || ((uintptr_t)idx & 3u) || !lengths_ok(cache->lengths, lengths_out, p->batch) ||
+      !apart(idx, (int64_t)p->batch * p->h_kv * p->limit, lengths_out, p->batch) ||
+      !apart(idx, (int64_t)p->batch * p->h_kv * p->limit, cache->lengths, p->batch))
+    return ECOKV_ERR_INVALID_ARG;
   if (ws != nullptr && (!aligned16(ws) || ws_bytes < 256)) return ECOKV_ERR_WORKSPACE;
   PruneArgs a{};
   a.m.from = *cache;

@@ -733,8 +733,8 @@ class PagedCache(_Handle):
     lengths are read on the device by every call, and written in place between them."""
 
     def __init__(self, k_pages, v_pages, table, lengths):
-        self.dtype, dev = _dtype(k_pages, v_pages)
-        self.device = dev
+        self.code, dev = _dtype(k_pages, v_pages)
+        self.dev = dev
         s = _strides(k_pages)
         if k_pages.dim() != 4 or k_pages.shape[3] != HEAD_DIM or s[3] != 1:
             raise ValueError(f"pages [n_pages, h_kv, page_size, {HEAD_DIM}] with the last axis contiguous are wanted")
@@ -927,7 +927,7 @@ def commit(cache, accepted, counts, starts=None, weights=None, lengths_out=None,
     [n_pages, h_kv, page_size] where given.  accepted int32 [batch, most], counts int32
     [batch]; starts as in attend_tree() (tokens: starts' last; by default no limit but
     theirs).  Returns the new lengths, lengths_out where given (the cache's own lengths too)."""
-    dt, dev = cache.dtype, cache.device
+    dt, dev = cache.code, cache.dev
     batch = cache.batch
     n = accepted.shape
     if len(n) != 2 or n[0] != batch or n[1] < 1:
@@ -997,10 +997,10 @@ def prune(cache, weights, budget, limit=None, first=0, recent=0, to=None, to_wei
     `budget` of them in each head, the `first` first, the `recent` last and between
     them those of the largest weights [n_pages, h_kv, page_size].  They take slots 0 .. of
     the same cache, or of `to` (a PagedCache), their weights of to_weights (None: they
-    are not moved; `weights` itself in the same cache).  Returns (new lengths, idx int32
+    are not moved; in the same cache `weights` itself).  Returns (new lengths, idx int32
     [batch, h_kv, limit]: the slots kept, then -1); lengths_out may be either cache's lengths."""
     limit = budget if limit is None else limit
-    dt, dev = cache.dtype, cache.device
+    dt, dev = cache.code, cache.dev
     if to is not None:
         _dtype(cache.k_pages, to.k_pages)
     batch, h_kv = cache.batch, cache.h_kv

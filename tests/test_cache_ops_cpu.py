@@ -69,7 +69,11 @@ def test_commit_refuses_arguments():
     assert call(dt=2) == 1 and call(h_kv=0) == 1 and call(acc=None) == 1 and call(stride=0) == 1
     assert call(counts=FAKE + 1) == 1 and call(starts=FAKE + 2) == 1 and call(tokens=3) == 1 and call(tokens=-1) == 1
     assert call(batch=0, tokens=0) == 1 and call(out=None) == 1 and call(out=FAKE + 4) == 1 and call(c=None) == 1
-    assert call(ws=FAKE, n=255) == 3 and call(h_kv=1 << 28) == 2 or call(h_kv=(1 << 28) + 1) == 2
+    assert call(ws=FAKE, n=255) == 3 and call(h_kv=(1 << 28) + 1) == 2
+    # the lengths are written while others read the lists: they lie apart (but for the cache's own)
+    far = 1 << 24
+    assert call(counts=far) == 1 and call(counts=far + 4) == 1 and call(acc=far - 28) == 1 and call(starts=far - 8) == 1
+    assert call(counts=far + 8, acc=far - 32, starts=far - 12, ws=FAKE, n=0) == 3
     for kw in BAD_WEIGHTS:
         assert call(w=weights(**kw)) == 1
     for kw, code in BAD_PAGES:
@@ -129,11 +133,16 @@ def test_prune_refuses_parameters(kw, code):
 
 
 def test_prune_refuses_arguments():
-    def call(dt=1, c=pages(), w=weights(), to=None, tw=None, idx=FAKE, out=1 << 24, ws=None, n=0):
+    def call(dt=1, c=pages(), w=weights(), to=None, tw=None, idx=1 << 26, out=1 << 24, ws=None, n=0):
         return E.ecokv_prune(prune_params(), dt, c, w, to, tw, idx, out, ws, n)
-    assert call(dt=2) == 1 and call(w=None) == 1 and call(idx=None) == 1 and call(idx=FAKE + 1) == 1
+    assert call(dt=2) == 1 and call(w=None) == 1 and call(idx=None) == 1 and call(idx=(1 << 26) + 1) == 1
     assert call(out=None) == 1 and call(out=FAKE + 4) == 1 and call(out=FAKE + 2) == 1 and call(c=None) == 1
     assert call(ws=FAKE, n=255) == 3
+    # in the same cache weights move within their tensor
+    assert call(tw=weights(w=FAKE + 4)) == 1 and call(tw=weights(page_stride=128)) == 1
+    assert call(tw=weights(), ws=FAKE, n=0) == 3 and call(to=pages(), tw=weights(w=FAKE + 4), ws=FAKE, n=0) == 3
+    # the slots' list apart from both lengths
+    assert call(idx=(1 << 24) + 4) == 1 and call(idx=FAKE - 4) == 1
     for kw in BAD_WEIGHTS:
         assert call(w=weights(**kw)) == 1 and call(tw=weights(**kw)) == 1
     for kw, code in BAD_PAGES:
