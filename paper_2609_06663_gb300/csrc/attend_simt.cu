@@ -229,6 +229,29 @@ __device__ __forceinline__ void item_few(const AttendArgs& a, Smem& s, const Ite
   }
 }
 
+// Scores of the rows ty R .. with the keys tx + 16 c, c < C (those that are not there are zeros).
+// A step's loads come ahead of its products.
+template <int R, int C>
+__device__ __forceinline__ void form_scores(const Smem& s, int tx, int ty, float (&x)[R][8]) {
+#pragma unroll 1
+  for (int e = 0; e < kD; e += 4) {
+    float4 q4[R], k4[C];
+#pragma unroll
+    for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(&s.q[ty * R + r][e]);
+#pragma unroll
+    for (int c = 0; c < C; ++c) k4[c] = *reinterpret_cast<const float4*>(&s.k[tx + 16 * c][e]);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        x[r][c] = fmaf(q4[r].x, k4[c].x, x[r][c]);
+        x[r][c] = fmaf(q4[r].y, k4[c].y, x[r][c]);
+        x[r][c] = fmaf(q4[r].z, k4[c].z, x[r][c]);
+        x[r][c] = fmaf(q4[r].w, k4[c].w, x[r][c]);
+      }
+  }
+}
+
 template <typename T, bool kTree>
 __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const Item& it) {
   constexpr int R = kRows / 16;
@@ -289,24 +312,9 @@ __device__ __forceinline__ void item_rows(const AttendArgs& a, Smem& s, const It
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int c = 0; c < 8; ++c) x[r][c] = 0.f;
-#pragma unroll 1
-    for (int e = 0; e < kD; e += 4) {
-      float4 q4[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(&s.q[ty * R + r][e]);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        if (c >= nc) break;
-        const float4 k4 = *reinterpret_cast<const float4*>(&s.k[tx + 16 * c][e]);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          x[r][c] = fmaf(q4[r].x, k4.x, x[r][c]);
-          x[r][c] = fmaf(q4[r].y, k4.y, x[r][c]);
-          x[r][c] = fmaf(q4[r].z, k4.z, x[r][c]);
-          x[r][c] = fmaf(q4[r].w, k4.w, x[r][c]);
-        }
-      }
-    }
+    if (nc > 4) form_scores<R, 8>(s, tx, ty, x);
+    else if (nc > 1) form_scores<R, 4>(s, tx, ty, x);
+    else form_scores<R, 1>(s, tx, ty, x);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float mx = -INFINITY;

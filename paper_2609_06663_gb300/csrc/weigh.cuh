@@ -35,7 +35,7 @@ struct WeighArgs {
   ecokv_weights pw, w;    // of the prefix, of the slots
   const float* lse;
   float decay;
-  int span, span_log2, tpt[2], unit[2], lead, whole;
+  int span, span_log2, tpt[2], unit[2], lead, whole, least;
   float* next;            // [P][kWeighSpan] sums of the item that a CTA goes on with
   WeighItem* next_item;   // [P], tile0 = 0: none
 };
@@ -125,8 +125,7 @@ struct WeighWalk {
     head = 0;
     left = 0;
     const long long total = prefix_total + a.h_kv * own;
-    // (a tile's units at least: no CTA between an item's first and last is without a tile of it)
-    const long long run = max(quotient(total + a.P - 1, a.P), (long long)max(w.unit[0], w.unit[1]));
+    const long long run = max(quotient(total + a.P - 1, a.P), (long long)w.least);
     x = min(cta * run, total);
     end = min(x + run, total);
   }

@@ -22,9 +22,18 @@ __global__ void __launch_bounds__(kWeighSpan) weigh_join_kernel(const __grid_con
   };
   if (c > 0 && same(w.next_item[c - 1])) return;
   const int k = threadIdx.x;
+  // (the last CTA of the item, 32 looked at at once, then independent loads)
+  int last = c;
+  for (int o = c + 1; o < w.a.P; o += 32) {
+    const int i = o + (k & 31);
+    const unsigned m = __ballot_sync(0xffffffffu, i < w.a.P && same(w.next_item[min(i, w.a.P - 1)]));
+    last += m == ~0u ? 32 : __ffs(~m) - 1;
+    if (m != ~0u) break;
+  }
+  float sum = 0.f;
+#pragma unroll 8
+  for (int o = c; o <= last; ++o) sum += w.next[(int64_t)o * kWeighSpan + k];
   if (k >= it.nkeys) return;
-  float sum = w.next[(int64_t)c * kWeighSpan + k];
-  for (int o = c + 1; o < w.a.P && same(w.next_item[o]); ++o) sum += w.next[(int64_t)o * kWeighSpan + k];
   float* at = weight_at(w, it, it.key0 + k);
   if (at != nullptr) *at += sum;
 }
@@ -127,10 +136,16 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
   if (!tc && a.tokens > w.tpt[0]) w.tpt[0] = div_up(a.tokens, div_up(a.tokens, w.tpt[0]));  // equal row tiles
   w.tpt[1] = a.starts != nullptr && 2 * mean < w.tpt[0] ? 2 * mean : a.starts != nullptr ? w.tpt[0] : 1;
   // (a unit: about 600 cycles of a CTA, an item of 256 keys with one row tile 5 of them, each row
-  // tile of 128 rows 4; on CUDA cores 16 rows of a tile, which take as long as the keys)
-  for (int k = 0; k < 2; ++k) w.unit[k] = div_up(w.tpt[k] * a.g, tc ? 32 : 16);
-  w.lead = tc ? 4 : 1;
-  w.whole = tc ? 24 : 5;
+  // tile of 128 rows 4; on CUDA cores: about 1700, 128 keys two of them and a tile of 64 rows 22)
+  for (int k = 0; k < 2; ++k) w.unit[k] = div_up((a.tokens < w.tpt[k] ? a.tokens : w.tpt[k]) * a.g, tc ? 32 : 3);
+  w.lead = tc ? 4 : 2;
+  w.whole = 24;
+  // (the units of the largest items that there can be)
+  auto units = [&](int source, int ntok) { return w.lead + (double)w.unit[source] * div_up(ntok, w.tpt[source]); };
+  const bool cut = (a.prefix.rows > 0 && units(0, a.tokens) > w.whole) ||
+                   (a.has_cache && units(1, a.starts != nullptr ? a.tokens : 1) > w.whole);
+  // (a cut item's tile at least: no CTA between its first and last is without a tile of it)
+  w.least = cut ? (w.unit[0] > w.unit[1] ? w.unit[0] : w.unit[1]) : 1;
   const double items = div_up(a.cap, w.span), of_prefix = div_up(a.prefix.rows, w.span);
   const double most = w.lead + 4.0 * (p->tokens + 1);
   if (a.h_kv * (of_prefix + (double)p->batch * items) * most > 4e18) return ECOKV_ERR_UNSUPPORTED;
@@ -144,10 +159,6 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (a.prefix.rows == 0 && !a.has_cache) return ECOKV_OK;
   if ((tc ? launch_weigh_tc(w, s) : launch_weigh_simt(w, dtype, s)) != cudaSuccess) return ECOKV_ERR_CUDA;
-  // (the units of the largest items that there can be)
-  auto units = [&](int source, int ntok) { return w.lead + (double)w.unit[source] * div_up(ntok, w.tpt[source]); };
-  const bool cut = (a.prefix.rows > 0 && units(0, a.tokens) > w.whole) ||
-                   (a.has_cache && units(1, a.starts != nullptr ? a.tokens : 1) > w.whole);
   if (!cut) return ECOKV_OK;
   return launch_behind(weigh_join_kernel, (unsigned)a.P, kWeighSpan, 0, s, w) == cudaSuccess ? ECOKV_OK : ECOKV_ERR_CUDA;
 }

@@ -119,37 +119,38 @@ __device__ __forceinline__ void item_few(const WeighArgs& w, Smem& s, const Weig
   if (half == 0 && k < it.nkeys) put(w, it, k, sum);
 }
 
-// The exponentials of a row tile's scores, added over its rows by sixteenth: R rows a thread.
-template <int R>
+// The exponentials of a row tile's scores, added over its rows by sixteenth: R rows a thread and
+// C keys (16 C of the tile; those that are not there are zeros).  A step's loads come ahead of
+// its products: between them they took three times as long.
+template <int R, int C>
 __device__ __forceinline__ void add_rows(const WeighArgs& w, const Smem& s, const WeighItem& it, int t, int rows,
                                          float (&total)[8]) {
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, nc = (it.nkeys + 15) >> 4;  // keys that are there, in sixteens
-  float x[R][8];
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  float x[R][C];
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
-    for (int c = 0; c < 8; ++c) x[r][c] = 0.f;
+    for (int c = 0; c < C; ++c) x[r][c] = 0.f;
 #pragma unroll 1
   for (int e = 0; e < kD; e += 4) {
-    float4 q4[R];
+    float4 q4[R], k4[C];
 #pragma unroll
     for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(&s.q[ty * R + r][e]);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      if (c >= nc) break;
-      const float4 k4 = *reinterpret_cast<const float4*>(&s.k[tx + 16 * c][e]);
+    for (int c = 0; c < C; ++c) k4[c] = *reinterpret_cast<const float4*>(&s.k[tx + 16 * c][e]);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        x[r][c] = fmaf(q4[r].x, k4.x, x[r][c]);
-        x[r][c] = fmaf(q4[r].y, k4.y, x[r][c]);
-        x[r][c] = fmaf(q4[r].z, k4.z, x[r][c]);
-        x[r][c] = fmaf(q4[r].w, k4.w, x[r][c]);
+        x[r][c] = fmaf(q4[r].x, k4[c].x, x[r][c]);
+        x[r][c] = fmaf(q4[r].y, k4[c].y, x[r][c]);
+        x[r][c] = fmaf(q4[r].z, k4[c].z, x[r][c]);
+        x[r][c] = fmaf(q4[r].w, k4[c].w, x[r][c]);
       }
-    }
   }
-  float sum[8];
+  float sum[C];
 #pragma unroll
-  for (int c = 0; c < 8; ++c) sum[c] = 0.f;
+  for (int c = 0; c < C; ++c) sum[c] = 0.f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = ty * R + r;
@@ -157,12 +158,19 @@ __device__ __forceinline__ void add_rows(const WeighArgs& w, const Smem& s, cons
       const float ref = s.ref[row];
       const int seen = it.source == 0 ? it.nkeys : it.base + t * w.tpt[1] + row / w.a.g + 1 - it.key0;
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
+      for (int c = 0; c < C; ++c)
         if (tx + 16 * c < seen) sum[c] += ptx::ex2(fmaf(x[r][c], w.a.scale_log2, ref));
     }
   }
 #pragma unroll
-  for (int c = 0; c < 8; ++c) total[c] += sum[c];
+  for (int c = 0; c < C; ++c) total[c] += sum[c];
+}
+template <int R>
+__device__ __forceinline__ void add_rows(const WeighArgs& w, const Smem& s, const WeighItem& it, int t, int rows,
+                                         float (&total)[8]) {
+  if (it.nkeys > 64) add_rows<R, 8>(w, s, it, t, rows, total);
+  else if (it.nkeys > 16) add_rows<R, 4>(w, s, it, t, rows, total);
+  else add_rows<R, 1>(w, s, it, t, rows, total);
 }
 
 template <typename T>

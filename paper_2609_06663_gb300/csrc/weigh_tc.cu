@@ -330,11 +330,17 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
 #pragma unroll
         for (int q = 0; q < 4; ++q) l[q] = make_float2(0.f, 0.f);
 #pragma unroll 1
-        for (int b = 0; b < rows; b += 32) {
+        for (int b = 0;; b += 32) {
           uint32_t x[32];
           tmem_ld_x32(ts + b, x);
           tmem_wait_ld();
           tmem_landed(x);
+          const bool last = b + 32 >= rows;
+          if (last) {  // the accumulator is read: the next product runs beside these columns
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sempty[tile][parity]);
+          }
           if (b + 32 > rows) {  // (columns without a row hold anything)
 #pragma unroll
             for (int c = 0; c < 32; ++c)
@@ -355,15 +361,12 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
             add_pair(l[((c >> 1) + 1) & 3].x, l[((c >> 1) + 1) & 3].y, ex2(__uint_as_float(x[c + 2])),
                      ex2(__uint_as_float(x[c + 3])));
           }
+          if (last) break;
         }
         total += ((l[0].x + l[0].y) + (l[1].x + l[1].y)) + ((l[2].x + l[2].y) + (l[3].x + l[3].y));
-        tc_fence_before();
       }
       __syncwarp();
-      if (lane == 0) {
-        if (active) mbar_arrive(&s.sempty[tile][parity]);
-        mbar_arrive(&s.rempty[slot]);
-      }
+      if (lane == 0) mbar_arrive(&s.rempty[slot]);
     }
     if (active && both) {
       // (warps of the same keys wait for each other only, each time in both directions, so
