@@ -155,7 +155,7 @@ constexpr int kAhead = 32 / kJoinWarps;  // sums whose loads a warp has in fligh
 
 // One warp `per` rows of a (token, KV head).
 template <typename T>
-__global__ void __launch_bounds__(32 * kJoinWarps)
+__global__ void __launch_bounds__(32 * kJoinWarps, 8)
     attend_join_heads_kernel(const __grid_constant__ AttendArgs a, int per, int split) {
   // (the next call's first kernel is scheduled behind this one)
   ptx::grid_trigger();
@@ -186,7 +186,17 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
       }
       const float w = next_weight(M, L, acc, ml);
       const int n = min(32, l.n - e0);
-      // (four sums' loads at once: 768 drafts of 28 heads 70.5 -> 67.4 us, in the same order)
+      // (in one order; past two sums the loads of four at once: 768 drafts of 28 heads 68.3 us,
+      // 70.5 one after another.  Eight CTAs an SM: without that bound 3000 tokens of 32 heads,
+      // of few sums a row, take 167 us and not 162.5.)
+      if (n <= 2) {
+#pragma unroll 2
+        for (int k = 0; k < n; ++k) {
+          const float* ok = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)o, k));
+          add_part(acc, __shfl_sync(0xffffffffu, w, k), *reinterpret_cast<const float4*>(ok + 4 * lane));
+        }
+        continue;
+      }
 #pragma unroll 1
       for (int k0 = 0; k0 < n; k0 += 4) {
         float4 v[4];

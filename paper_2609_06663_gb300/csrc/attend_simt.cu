@@ -16,7 +16,7 @@
 //
 // Items of more rows, in groups of 64: a CTA of 256 threads holds an item's queries, a
 // tile of 128 keys and its values in shared memory as fp32 (82 tokens of 8 sequences, 28
-// heads over 4, 1369 rows and up to 300 of their own: 93 us, 19 TFLOP/s).  Thread (ty, tx)
+// heads over 4, 1369 rows and up to 300 of their own: 70.6 us, 25 TFLOP/s).  Thread (ty, tx)
 // of 16 x 16 forms the scores of its rows ty R .. ty R + R - 1 with the keys tx + 16 j, a
 // row's maximum and sum are four shuffles away, and the same thread then sums columns
 // 4 tx .. and 64 + 4 tx .. of its rows' outputs over the tile, which stay in registers
