@@ -272,7 +272,9 @@ size_t ecokv_weigh_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, in
  * A call of no tokens changes nothing.
  * Page numbers, lengths and offsets out of range: as for ecokv_attend; a slot without a
  * page has no weight.  ECOKV_ERR_UNSUPPORTED: d, h_q / h_kv as for ecokv_attend, and
- * more work than 62 bits count. */
+ * more work than 31 bits count, which it is not while
+ *   h_kv (k(rows) (32 + n) + k(page_size * table_stride) (40 batch + n + 48)) < 2^31,
+ * n = tokens h_q / h_kv, k(keys) = ceil(keys / 128). */
 ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const void* q, const float* lse,
                          const ecokv_prefix* prefix, const ecokv_pages* cache, const int32_t* starts,
                          const ecokv_weights* prefix_weights, const ecokv_weights* weights, void* ws, size_t ws_bytes,

@@ -408,7 +408,7 @@ static ecokv_status attend(const ecokv_attend_params* p, ecokv_dtype dtype, cons
   if (!tc && mask != nullptr) {
     int rows = 64;
     while (rows > 16 && rows / 2 >= a.g &&
-           (double)a.h_kv * div_up(a.tokens, rows / a.g) * (tiles_of(a.prefix.rows) + 1) < 2.0 * attend_sms())
+           (double)a.h_kv * ((a.tokens - 1) / (rows / a.g) + 1) * (tiles_of(a.prefix.rows) + 1) < 2.0 * attend_sms())
       rows /= 2;
     a.tpt = rows / a.g;
   }

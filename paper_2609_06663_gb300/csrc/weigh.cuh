@@ -42,17 +42,14 @@ struct WeighArgs {
 
 // Row tiles of an item that so many tokens see (one at least, so that it is met).
 __device__ __forceinline__ int row_tiles(const WeighArgs& w, int source, int ntok) {
-  return ntok > w.tpt[source] ? div_up(ntok, w.tpt[source]) : 1;
-}
-// (numbers of 64 bits that nearly always have 31: the long division's code is not fetched)
-__device__ __forceinline__ long long quotient(long long x, long long y) {
-  return ((x | y) >> 31) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
+  return ntok > w.tpt[source] ? (ntok - 1) / w.tpt[source] + 1 : 1;
 }
 __device__ __forceinline__ int weigh_per(const WeighArgs& w, int source, int ntok) {
   return w.lead + row_tiles(w, source, ntok) * w.unit[source];
 }
-__device__ __forceinline__ long long weigh_units(const WeighArgs& w, int source, int keys, int ntok) {
-  return (long long)((keys + w.span - 1) >> w.span_log2) * weigh_per(w, source, ntok);
+// (31 bits hold it, as the host has checked for any of the call's sequences)
+__device__ __forceinline__ int weigh_units(const WeighArgs& w, int source, int keys, int ntok) {
+  return ((keys + w.span - 1) >> w.span_log2) * weigh_per(w, source, ntok);
 }
 
 // Tokens of the call that are of a sequence, from 0 on.
@@ -63,22 +60,14 @@ __device__ __forceinline__ int live_tokens(const AttendArgs& a) {
 // A warp's walk over its CTA's run of units, item by item.  Every lane holds the same
 // state but for the 32 sequences (or heads) at hand, one a lane.
 struct WeighWalk {
-  long long x, end, prefix_total, own;
+  int x, end, prefix_total, own;
   int live, lane;
   int b0, head;
-  int left;          // keys of the head and sequence behind the item before, if that was met to its end
-  long long before;  // units of the sequences before b0
+  int left;    // keys of the head and sequence behind the item before, if that was met to its end
+  int before;  // units of the sequences before b0
   Seq s;
-  long long n, upto;
+  int n, upto;
 
-  static __device__ __forceinline__ long long scan(long long v, int lane) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += u;
-    }
-    return v;
-  }
   __device__ __forceinline__ void chunk(const WeighArgs& w, int from, bool report) {
     b0 = from;
     s = Seq{0, 0, 0};
@@ -87,7 +76,7 @@ struct WeighWalk {
       s = load_seq(w.a, b0 + lane, report);
       n = weigh_units(w, 1, s.L, s.T);
     }
-    upto = scan(n, lane);
+    upto = Walk::scan(n, lane);  // (may wrap where begin() drops the sequences)
   }
 
   // All of the warp's lanes; `report`: note what is out of range.
@@ -102,32 +91,38 @@ struct WeighWalk {
       } else {
 #pragma unroll 1
         for (int h0 = 0; h0 < a.h_kv; h0 += 32) {
-          int row0;
-          long long v = 0;
+          int row0, v = 0;
           if (h0 + lane < a.h_kv) v = weigh_units(w, 0, prefix_rows(a, h0 + lane, row0, report), live);
-          prefix_total += __shfl_sync(0xffffffffu, scan(v, lane), 31);
+          prefix_total += (int)__reduce_add_sync(0xffffffffu, (unsigned)v);
         }
       }
     }
     own = 0;
     if (a.has_cache) {
       chunk(w, 0, report);
-      own = n;
+      long long sum = n;
 #pragma unroll 4
       for (int b = 32 + lane; b < a.batch; b += 32) {
         const Seq q = load_seq(a, b, report);
-        own += weigh_units(w, 1, q.L, q.T);
+        sum += weigh_units(w, 1, q.L, q.T);
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
+      // (in 64 bits: starts that overlap may have every sequence hold all of the tokens)
+      const unsigned most = (unsigned)min(sum, 0x7fffffffll);
+      sum = __reduce_add_sync(0xffffffffu, most & 0xffffu) +
+            ((long long)__reduce_add_sync(0xffffffffu, most >> 16) << 16);
+      if (sum * a.h_kv > 0x7fffffff - prefix_total) {
+        if (report && lane == 0) note(a, ECOKV_ERR_DEVICE_INDEX, (unsigned)a.batch);
+        sum = 0;
+      }
+      own = (int)sum;
     }
     before = 0;
     head = 0;
     left = 0;
-    const long long total = prefix_total + a.h_kv * own;
-    const long long run = max(quotient(total + a.P - 1, a.P), (long long)w.least);
-    x = min(cta * run, total);
-    end = min(x + run, total);
+    const int total = prefix_total + a.h_kv * own;
+    const int run = max((int)(((unsigned)total + (unsigned)a.P - 1u) / (unsigned)a.P), w.least);
+    x = (int)min((unsigned)cta * (unsigned)run, (unsigned)total);
+    end = (int)min((unsigned)x + (unsigned)run, (unsigned)total);
   }
 
   // The next item (the same in every lane); false: none left.
@@ -142,8 +137,7 @@ struct WeighWalk {
   // The part of an item from unit x on, which may be less than its first tile (ntiles <= 0).
   __device__ __forceinline__ bool at(const WeighArgs& w, WeighItem& it) {
     const AttendArgs& a = w.a;
-    long long y;
-    int keys;
+    int y, keys;
     if (left > 0) {  // the item behind the one before
       it.key0 += w.span;
       it.nkeys = min(left, w.span);
@@ -157,18 +151,18 @@ struct WeighWalk {
       it.ntok = live;
       if (a.prefix.head_off == nullptr) {
         keys = a.prefix.rows;
-        const long long per = quotient(prefix_total, a.h_kv);
-        it.head = (int)quotient(x, per);
+        const int per = prefix_total / a.h_kv;
+        it.head = x / per;
         y = x - it.head * per;
       } else {
-        long long at = 0;
+        int at = 0;
 #pragma unroll 1
         for (int h0 = 0;; h0 += 32) {
           if (h0 >= a.h_kv) return false;  // (only when the offsets change under the kernel; so below)
           int r0 = 0, rows = 0;
           if (h0 + lane < a.h_kv) rows = prefix_rows(a, h0 + lane, r0, false);
-          const long long v = weigh_units(w, 0, rows, live), up = scan(v, lane);
-          const long long all = __shfl_sync(0xffffffffu, up, 31);
+          const int v = weigh_units(w, 0, rows, live), up = Walk::scan(v, lane);
+          const int all = __shfl_sync(0xffffffffu, up, 31);
           if (x < at + all) {
             const int l = __ffs(__ballot_sync(0xffffffffu, x < at + up)) - 1;
             it.head = h0 + l;
@@ -183,14 +177,14 @@ struct WeighWalk {
       it.base = keys;
     } else {
       y = x - prefix_total;
-      const int h = (int)quotient(y, own);
+      const int h = y / own;
       y -= h * own;
       if (h != head && b0 != 0) {
         before = 0;
         chunk(w, 0, false);
       }
       head = h;
-      long long all;
+      int all;
 #pragma unroll 1
       while (y >= before + (all = __shfl_sync(0xffffffffu, upto, 31))) {
         before += all;
@@ -208,17 +202,17 @@ struct WeighWalk {
       it.ntok = __shfl_sync(0xffffffffu, s.T, l);
       it.base = keys - it.ntok;
     }
-    const int per = weigh_per(w, it.source, it.ntok), i = (int)quotient(y, per);
+    const int per = weigh_per(w, it.source, it.ntok), i = y / per;
     it.key0 = i * w.span;
     it.nkeys = min(keys - it.key0, w.span);
-    return part(w, it, (int)(y - (long long)i * per), keys - it.key0);
+    return part(w, it, y - i * per, keys - it.key0);
   }
   // The tiles of an item whose first unit lies within this CTA's part of it, y .. z - 1; the
   // item and what lies behind it of its head and sequence have `keys` keys.
   __device__ __forceinline__ bool part(const WeighArgs& w, WeighItem& it, int y, int keys) {
     const int per = weigh_per(w, it.source, it.ntok), u = w.unit[it.source];
     const bool whole = per <= w.whole;
-    const int z = whole ? per : (int)min((long long)per, y + end - x);
+    const int z = whole ? per : min(per, y + end - x);
     it.tile0 = (max(y - w.lead, 0) + u - 1) / u;
     it.ntiles = whole && y > 0 ? 0 : (max(z - w.lead, 0) + u - 1) / u - it.tile0;
     x += z - y;

@@ -132,23 +132,27 @@ ecokv_status ecokv_weigh(const ecokv_weigh_params* p, ecokv_dtype dtype, const v
   w.tpt[0] = (tc ? 128 : 64) / a.g;
   // a sequence's own row tiles have room for twice the mean of its tokens: what is copied and
   // multiplied of a decode step's single rows is no more than they are
-  const int mean = a.starts != nullptr ? div_up(a.tokens, a.batch) : 1;
-  if (!tc && a.tokens > w.tpt[0]) w.tpt[0] = div_up(a.tokens, div_up(a.tokens, w.tpt[0]));  // equal row tiles
-  w.tpt[1] = a.starts != nullptr && 2 * mean < w.tpt[0] ? 2 * mean : a.starts != nullptr ? w.tpt[0] : 1;
+  const int mean = a.starts != nullptr ? (a.tokens - 1) / a.batch + 1 : 1;
+  auto tiles = [](int ntok, int tpt) { return (ntok - 1) / tpt + 1; };  // (ntok + tpt may not be an int)
+  if (!tc && a.tokens > w.tpt[0]) w.tpt[0] = tiles(a.tokens, tiles(a.tokens, w.tpt[0]));  // equal ones
+  w.tpt[1] = a.starts != nullptr && mean < (w.tpt[0] + 1) / 2 ? 2 * mean : a.starts != nullptr ? w.tpt[0] : 1;
   // (a unit: about 600 cycles of a CTA, an item of 256 keys with one row tile 5 of them, each row
   // tile of 128 rows 4; on CUDA cores: about 1700, 128 keys two of them and a tile of 64 rows 22)
   for (int k = 0; k < 2; ++k) w.unit[k] = div_up((a.tokens < w.tpt[k] ? a.tokens : w.tpt[k]) * a.g, tc ? 32 : 3);
   w.lead = tc ? 4 : 2;
   w.whole = 24;
   // (the units of the largest items that there can be)
-  auto units = [&](int source, int ntok) { return w.lead + (double)w.unit[source] * div_up(ntok, w.tpt[source]); };
+  auto units = [&](int source, int ntok) { return w.lead + (double)w.unit[source] * tiles(ntok, w.tpt[source]); };
   const bool cut = (a.prefix.rows > 0 && units(0, a.tokens) > w.whole) ||
                    (a.has_cache && units(1, a.starts != nullptr ? a.tokens : 1) > w.whole);
   // (a cut item's tile at least: no CTA between its first and last is without a tile of it)
   w.least = cut ? (w.unit[0] > w.unit[1] ? w.unit[0] : w.unit[1]) : 1;
+  // Units of all items, counted in 31 bits by the kernels: as many as there can be of the sequences'
+  // slots.  (A sequence's tokens make a row tile more than their share.)
   const double items = div_up(a.cap, w.span), of_prefix = div_up(a.prefix.rows, w.span);
-  const double most = w.lead + 4.0 * (p->tokens + 1);
-  if (a.h_kv * (of_prefix + (double)p->batch * items) * most > 4e18) return ECOKV_ERR_UNSUPPORTED;
+  const double row_tiles = tiles(a.tokens, w.tpt[1]) + (double)a.batch;
+  const double own = items * (a.batch * (double)w.lead + row_tiles * w.unit[1]);
+  if (a.h_kv * (of_prefix * units(0, a.tokens) + own) > 0x7fffffff) return ECOKV_ERR_UNSUPPORTED;
   const WeighLayout L = weigh_layout();
   if (ws == nullptr || !aligned16(ws) || ws_bytes < L.total) return ECOKV_ERR_WORKSPACE;
   a.P = attend_sms() * (tc ? 1 : 2);

@@ -4,14 +4,14 @@
 // Items that up to 32 rows see (a decode step): each warp has sixteen keys in
 // registers, lanes 2k and 2k + 1 the halves of key k, and goes over the rows, whose dot
 // products need one shuffle and whose weights no other thread's.  Bound by the chain of
-// loads before the first of them (8 sequences of up to three tokens, 8 heads: 10.9 us; one
-// sequence, one token 6.2).
+// loads before the first of them (8 sequences of up to three tokens, 8 heads: 10.7 us; one
+// sequence, one token 5.9).
 //
 // Items of more rows: keys and rows of a tile in shared memory as fp32; thread (ty, tx) of
 // 16 x 16 forms the scores of its four rows with the keys tx + 16 j and adds their
 // exponentials to the keys' sums, which sixteen threads join at the item's end (three, two or
 // one row a thread where a tile has no more).  Two CTAs an SM, so that one's products run
-// beside the other's loads (12 single tokens of 28 heads over 12010 rows: 54.5 us, 19
+// beside the other's loads (12 single tokens of 28 heads over 12010 rows: 53.7 us, 19
 // TFLOP/s, 78.8 with one; bound by the reads of shared memory).
 
 #include <math.h>

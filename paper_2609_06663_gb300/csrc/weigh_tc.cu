@@ -11,8 +11,8 @@
 // each other's latencies.  The sums of an item's even and odd tiles are added at its end.
 //
 // Bound by the keys' bytes where few rows see them (64 sequences of up to 4097 slots and a
-// token each, 28 heads over 4: 32.9 us, 4.6 TB/s over the call, of which 8 are the walk's
-// start and the launch).  Where many do (806 tokens over 6554 rows: 47.9 us, 800 TFLOP/s) a
+// token each, 28 heads over 4: 31.5 us, 4.8 TB/s over the call, of which 8 are the walk's
+// start and the launch).  Where many do (806 tokens over 6554 rows: 47.4 us, 807 TFLOP/s) a
 // stream's 128 columns take 3100 cycles, its wait for their product 600, and a CTA's four
 // streams share a unit for exponentials that 2048 would do and a tensor pipe that 2200
 // would: without exponentials it takes 44 us, with half of each product 45, with half of

@@ -119,6 +119,27 @@ def test_weigh_refuses_arguments():
         assert call(pre=prefix(**kw)) == code
 
 
+@pytest.mark.parametrize("dtype,flags", [(1, 0), (1, E.ECOKV_FLAG_FORCE_SIMT), (0, 0)])
+@pytest.mark.parametrize("group", [1, 7, 8, 64])
+@pytest.mark.parametrize("tokens,page,cols,rows", [(100000, 4096, 256, 0), (4096, 4096, 4096, 0), (10, 8, 1, 0),
+                                                   (10000, 16, 8192, 131072), (1 << 20, 16, 4, 1 << 24)])
+def test_weigh_size_limit(tokens, page, cols, rows, group, dtype, flags):
+    """Taken up to the header's bound, refused far past it (no workspace is given: nothing is launched)."""
+    h_kv, n, k = 2, tokens * group, lambda keys: -(-keys // 128)
+    room = (2 ** 31 - 1) // h_kv - k(rows) * (32 + n)
+    most = (room // k(page * cols) - n - 48) // 40
+    c = pages(page_size=page, table_stride=cols, page_stride=h_kv * page * 128, head_stride=page * 128)
+
+    def call(batch):
+        p = weigh_params(h_q=h_kv * group, h_kv=h_kv, tokens=tokens, batch=batch, flags=flags)
+        return E.ecokv_weigh(p, dtype, FAKE, FAKE, prefix(rows=rows, head_stride=max(rows, 1) * 128), c, FAKE, weights(),
+                             weights(), FAKE, 0)
+    if most >= 1:
+        assert call(min(most, 2 ** 31 - 1)) == 3
+    if cols > 1:
+        assert call(2 ** 31 - 1) == 2
+
+
 def prune_params(**kw):
     d = dict(h_kv=4, batch=2, budget=20, limit=30, first=4, recent=8)
     d.update(kw)
