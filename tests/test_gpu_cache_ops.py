@@ -363,6 +363,21 @@ def test_weights_of_an_attention_add_up_to_its_rows(dt, flags):
     assert bool(((total - 6 * b.tokens).abs() <= 6 * b.tokens * (2 * (140 * 60 + 40) + 1000) * U).all())
 
 
+@pytest.mark.parametrize("dt,flags", [("bf16", 0), ("bf16", SIMT), ("f32", 0)])
+def test_weigh_from_nothing(dt, flags):
+    """decay = 0: what the weights were is not read."""
+    b = Batch(5, 2, [3, 1, 40], [30, 12, 100], 16, dt)
+    heads, pre = make_prefix(gen(1), [300, 300], dt, False)
+    q = (2 * torch.randn(b.tokens, 12, D, generator=gen(9))).to(TYPES[dt]).cuda()
+    lse = torch.full((b.tokens, 12), 8.0, device="cuda")
+    got = [E.weigh(q, lse, pre, b.cache, torch.full((2, 300), x, device="cuda"), torch.full(b.k.shape[:3], x, device="cuda"),
+                   b.starts.cuda(), decay=0.0, flags=flags) for x in (0.0, math.nan)]
+    assert torch.equal(got[0][0], got[1][0])
+    for s, n in enumerate(b.lens):
+        p, r = places(b, s, range(n))
+        assert torch.equal(got[0][1].cpu()[p, :, r], got[1][1].cpu()[p, :, r])
+
+
 def test_weigh_without_a_cache_or_a_prefix():
     for dt in ("bf16", "f32"):
         T = TYPES[dt]
