@@ -247,7 +247,7 @@ ecokv_status ecokv_commit(ecokv_dtype dtype, const ecokv_pages* cache, int32_t h
 typedef struct {
   int32_t h_q, h_kv, d, tokens, batch;  /* as in ecokv_attend_params */
   float scale;
-  float decay;                          /* of the weights so far, finite, >= 0 (0: they are not read) */
+  float decay;                          /* of the weights so far, finite, >= 0 (0: they do not count) */
   int64_t q_token, q_head;
   uint32_t flags;                       /* as in ecokv_attend_params */
   uint32_t timeout_us;

@@ -242,10 +242,13 @@ __device__ __forceinline__ float* weight_at(const WeighArgs& w, const WeighItem&
 __device__ __forceinline__ float* weight_at(const WeighArgs& w, const WeighItem& it, int j) {
   return weight_at(w, it, j, weight_page(w, it, j));
 }
-// The weight that the item's sum is added to: a new token's own slot starts at 0, and so does
-// every key where nothing of what was before counts (it may be anything).
-__device__ __forceinline__ float weight_before(const WeighArgs& w, const WeighItem& it, const float* at, int j) {
-  return at == nullptr || w.decay == 0.f || (it.source != 0 && j >= it.base) ? 0.f : *at;
+// The weight that the item's sum is added to: a new token's own slot starts at 0.
+__device__ __forceinline__ float weight_before(const WeighItem& it, const float* at, int j) {
+  return at == nullptr || (it.source != 0 && j >= it.base) ? 0.f : *at;
+}
+// (what was before may be anything where nothing of it counts)
+__device__ __forceinline__ float weight_after(const WeighArgs& w, float before, float sum) {
+  return w.decay == 0.f ? sum : fmaf(w.decay, before, sum);
 }
 // What a row's scores (in log2 units) are taken relative to, negated: rows that saw no key
 // give nothing.

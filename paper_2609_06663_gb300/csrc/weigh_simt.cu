@@ -83,7 +83,7 @@ __device__ __forceinline__ void put(const WeighArgs& w, const WeighItem& it, int
   }
   const int j = it.key0 + k;
   float* at = weight_at(w, it, j);
-  if (at != nullptr) *at = fmaf(w.decay, weight_before(w, it, at, j), sum);
+  if (at != nullptr) *at = weight_after(w, weight_before(it, at, j), sum);
 }
 
 template <typename T>

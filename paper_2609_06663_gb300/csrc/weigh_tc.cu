@@ -11,8 +11,8 @@
 // each other's latencies.  The sums of an item's even and odd tiles are added at its end.
 //
 // Bound by the keys' bytes where few rows see them (64 sequences of up to 4097 slots and a
-// token each, 28 heads over 4: 31.5 us, 4.8 TB/s over the call, of which 8 are the walk's
-// start and the launch).  Where many do (806 tokens over 6554 rows: 47.4 us, 807 TFLOP/s) a
+// token each, 28 heads over 4: 30.5 us, 5.0 TB/s over the call, of which 8 are the walk's
+// start and the launch).  Where many do (806 tokens over 6554 rows: 46.4 us, 824 TFLOP/s) a
 // stream's 128 columns take 3100 cycles, its wait for their product 600, and a CTA's four
 // streams share a unit for exponentials that 2048 would do and a tensor pipe that 2200
 // would: without exponentials it takes 44 us, with half of each product 45, with half of
@@ -315,7 +315,7 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
     const bool active = tile < key_tiles(it), mine = k < it.nkeys, first = (n0 & 1) == parity, both = it.ntiles > 1;
     // (on its way while the products are; the next item's page number too)
     float* at = mine && first && it.tile0 == 0 ? weight_at(w, it, j, page) : nullptr;
-    const float before = weight_before(w, it, at, j);
+    const float before = weight_before(it, at, j);
     more = items.next(s, a, next, lane);
     page = page_of(n0 + (uint32_t)it.ntiles);
     float total = 0.f;
@@ -331,9 +331,7 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
         if (!wait_warp(s, a, &s.sfull[tile][parity], jobs & 1, 9u)) return;
         ++jobs;
         tc_fence_after();
-        float2 l[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) l[q] = make_float2(0.f, 0.f);
+        float2 l = make_float2(0.f, 0.f);  // (more of them cost registers: two 47.0 us, four 47.9)
 #pragma unroll 1
         for (int b = 0;; b += 32) {
           uint32_t x[32];
@@ -362,13 +360,12 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
             const float4 f = ref[c / 4];
             fma_pair(x[c], x[c + 1], scale2, f.x, f.y);
             fma_pair(x[c + 2], x[c + 3], scale2, f.z, f.w);
-            add_pair(l[(c >> 1) & 3].x, l[(c >> 1) & 3].y, ex2(__uint_as_float(x[c])), ex2(__uint_as_float(x[c + 1])));
-            add_pair(l[((c >> 1) + 1) & 3].x, l[((c >> 1) + 1) & 3].y, ex2(__uint_as_float(x[c + 2])),
-                     ex2(__uint_as_float(x[c + 3])));
+            add_pair(l.x, l.y, ex2(__uint_as_float(x[c])), ex2(__uint_as_float(x[c + 1])));
+            add_pair(l.x, l.y, ex2(__uint_as_float(x[c + 2])), ex2(__uint_as_float(x[c + 3])));
           }
           if (last) break;
         }
-        total += ((l[0].x + l[0].y) + (l[1].x + l[1].y)) + ((l[2].x + l[2].y) + (l[3].x + l[3].y));
+        total += l.x + l.y;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.rempty[slot]);
@@ -389,7 +386,7 @@ __device__ __forceinline__ void add_up(Smem& s, const WeighArgs& w, uint32_t tme
       }
       ++merges;
     }
-    if (at != nullptr) *at = fmaf(w.decay, before, total);
+    if (at != nullptr) *at = weight_after(w, before, total);
     if (mine && first && it.tile0 != 0) w.next[(int64_t)blockIdx.x * kWeighSpan + k] = total;
   }
 }

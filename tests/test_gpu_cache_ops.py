@@ -365,7 +365,7 @@ def test_weights_of_an_attention_add_up_to_its_rows(dt, flags):
 
 @pytest.mark.parametrize("dt,flags", [("bf16", 0), ("bf16", SIMT), ("f32", 0)])
 def test_weigh_from_nothing(dt, flags):
-    """decay = 0: what the weights were is not read."""
+    """decay = 0: what the weights were does not count."""
     b = Batch(5, 2, [3, 1, 40], [30, 12, 100], 16, dt)
     heads, pre = make_prefix(gen(1), [300, 300], dt, False)
     q = (2 * torch.randn(b.tokens, 12, D, generator=gen(9))).to(TYPES[dt]).cuda()
