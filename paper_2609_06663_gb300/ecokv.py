@@ -795,13 +795,7 @@ def alloc_attend_workspace(tokens, batch, h_q, h_kv, dtype, device="cuda"):
     n = ecokv_attend_workspace_size(tokens, batch, h_q, h_kv, ECOKV_F32 if dtype == torch.float32 else ECOKV_BF16)
     if n == 0:
         raise EcokvError(ECOKV_ERR_INVALID_ARG, "ecokv_attend_workspace_size")
-    return _cleared(torch.empty(n, dtype=torch.uint8, device=device))
-
-
-def _cleared(ws):
-    """A workspace whose status word is clear; the calls read nothing else that they have not written."""
-    ws[:256].zero_()
-    return ws
+    return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
 def _attend(q, prefix, cache, starts, scale, out, lse, ws, flags, timeout_us, stream):
@@ -958,7 +952,7 @@ def alloc_weigh_workspace(tokens, batch, h_q, h_kv, dtype, device="cuda"):
     n = ecokv_weigh_workspace_size(tokens, batch, h_q, h_kv, ECOKV_F32 if dtype == torch.float32 else ECOKV_BF16)
     if n == 0:
         raise EcokvError(ECOKV_ERR_INVALID_ARG, "ecokv_weigh_workspace_size")
-    return _cleared(torch.empty(n, dtype=torch.uint8, device=device))
+    return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
 def weigh(q, lse, prefix, cache, prefix_weights=None, weights=None, starts=None, scale=0.0, decay=1.0, ws=None,
