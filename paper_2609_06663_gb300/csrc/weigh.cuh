@@ -65,6 +65,7 @@ struct WeighWalk {
   int b0, head;
   int left;    // keys of the head and sequence behind the item before, if that was met to its end
   int before;  // units of the sequences before b0
+  WeighItem it;  // the one at hand, from which the next one of its head and sequence follows
   Seq s;
   int n, upto;
 
@@ -125,23 +126,26 @@ struct WeighWalk {
     end = (int)min((unsigned)x + (unsigned)run, (unsigned)total);
   }
 
-  // The next item (the same in every lane); false: none left.
-  __device__ __forceinline__ bool next(const WeighArgs& w, WeighItem& it) {
+  // The next item (the same in every lane); false: none left, and `to` as it was.
+  __device__ __forceinline__ bool next(const WeighArgs& w, WeighItem& to) {
 #pragma unroll 1
     while (x < end) {
-      if (!at(w, it)) return false;
-      if (it.ntiles > 0) return true;
+      if (!at(w)) return false;
+      if (it.ntiles > 0) {
+        to = it;
+        return true;
+      }
     }
     return false;
   }
   // The part of an item from unit x on, which may be less than its first tile (ntiles <= 0).
-  __device__ __forceinline__ bool at(const WeighArgs& w, WeighItem& it) {
+  __device__ __forceinline__ bool at(const WeighArgs& w) {
     const AttendArgs& a = w.a;
     int y, keys;
     if (left > 0) {  // the item behind the one before
       it.key0 += w.span;
       it.nkeys = min(left, w.span);
-      return part(w, it, 0, left);
+      return part(w, 0, left);
     }
     if (x < prefix_total) {
       it.source = 0;
@@ -205,11 +209,11 @@ struct WeighWalk {
     const int per = weigh_per(w, it.source, it.ntok), i = y / per;
     it.key0 = i * w.span;
     it.nkeys = min(keys - it.key0, w.span);
-    return part(w, it, y - i * per, keys - it.key0);
+    return part(w, y - i * per, keys - it.key0);
   }
   // The tiles of an item whose first unit lies within this CTA's part of it, y .. z - 1; the
   // item and what lies behind it of its head and sequence have `keys` keys.
-  __device__ __forceinline__ bool part(const WeighArgs& w, WeighItem& it, int y, int keys) {
+  __device__ __forceinline__ bool part(const WeighArgs& w, int y, int keys) {
     const int per = weigh_per(w, it.source, it.ntok), u = w.unit[it.source];
     const bool whole = per <= w.whole;
     const int z = whole ? per : min(per, y + end - x);

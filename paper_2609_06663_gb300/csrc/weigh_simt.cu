@@ -232,9 +232,8 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_simt_kernel(const __grid_co
   while (true) {
     __syncthreads();
     if (threadIdx.x < 32) {
-      WeighItem it;
+      WeighItem it{};
       const bool more = walk.next(w, it);
-      if (!more) it.tile0 = 0;
       if (lane == 0) {
         s.item = it;
         s.more = more ? 1 : 0;

@@ -460,9 +460,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     walk.begin(w, blockIdx.x, lane, blockIdx.x == 0);
     Ring<kItems> r;
     for (bool first = true;; first = false) {
-      WeighItem it;
+      WeighItem it{};
       const bool more = walk.next(w, it);
-      if (!more) it.ntiles = it.tile0 = 0;
       if (first && lane == 0) w.next_item[blockIdx.x] = it;
       if (!wait_warp(s, a, &s.iempty[r.at], r.phase ^ 1, 10u)) break;
       if (lane == 0) {
