@@ -269,7 +269,9 @@ size_t ecokv_weigh_workspace_size(int32_t tokens, int32_t batch, int32_t h_q, in
  *                                      from lengths[b] on are left as they were
  * Slots in use belong to one sequence each.  Sums are fp32 and in a fixed order: the
  * result is deterministic.  q, lse and the keys in use must be finite (lse: or -inf).
- * A call of no tokens changes nothing.
+ * A call of no tokens changes nothing.  One that ends with ECOKV_ERR_TIMEOUT in the status
+ * word has weighed some keys, others by a part of their rows or not at all: the weights
+ * are lost.
  * Page numbers, lengths and offsets out of range: as for ecokv_attend; a slot without a
  * page has no weight.  ECOKV_ERR_UNSUPPORTED: d, h_q / h_kv as for ecokv_attend, and
  * more work than 31 bits count, which it is not while

@@ -484,6 +484,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (d.q > i) drain_bar(&s.qfull[i], ((d.q - 1 - i) / kRowTiles) & 1);
   }
   __syncthreads();
+  // (a CTA that gave up leaves no sum: what lies there may be another call's)
+  if (s.abort != 0 && tid < kWeighSpan) w.next[(int64_t)blockIdx.x * kWeighSpan + tid] = 0.f;
   grid_trigger();
   if (warp == 3) {
     tc_fence_after();

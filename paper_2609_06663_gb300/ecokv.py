@@ -961,7 +961,8 @@ def weigh(q, lse, prefix, cache, prefix_weights=None, weights=None, starts=None,
     prefix and cache (either may be None), from the lse that attend() has left, is added to
     prefix_weights (float32, of the shape of the prefix's k without its last axis) and to
     weights [n_pages, h_kv, page_size], which are multiplied by decay first (0: whatever they
-    are).  starts int32 [batch + 1]: None = one token a sequence.  Returns (prefix_weights, weights)."""
+    are).  starts int32 [batch + 1]: None = one token a sequence.  Returns (prefix_weights, weights);
+    they are lost where the workspace's status is ECOKV_ERR_TIMEOUT."""
     if prefix is None and cache is None:
         raise ValueError("a prefix or a cache is wanted")
     dt, dev = _dtype(q, None if prefix is None else prefix.k, None if cache is None else cache.k_pages)
