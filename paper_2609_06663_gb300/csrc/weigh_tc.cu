@@ -398,7 +398,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const AttendArgs& a = w.a;
   if ((smem_u32(smem_raw) & 1023u) != 0) {
     grid_wait();
-    if (threadIdx.x == 0) note(a, ECOKV_ERR_CUDA, 0u);
+    if (threadIdx.x == 0) {
+      note(a, ECOKV_ERR_CUDA, 0u);
+      w.next_item[blockIdx.x] = WeighItem{};  // (nothing to join)
+    }
     return;
   }
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
