@@ -218,14 +218,15 @@ struct Walk {
     head = 0;
     const int total = prefix_total + a.h_kv * own;
     // (at least a tile's units: no CTA between the first and the last of an item is without a tile of it)
-    const int run = max(div_up(total, a.P), tile_units(a, a.span));
+    // (in 32 bits without a sign: a run behind the last unit may begin past 31 bits)
+    const int run = max((int)(((unsigned)total + (unsigned)a.P - 1u) / (unsigned)a.P), tile_units(a, a.span));
     if (lead && lane == 0) {
       a.plan[PLAN_RUN] = run;
       a.plan[PLAN_PREFIX] = prefix_total;
       a.plan[PLAN_OWN] = own;
     }
-    x = min(cta * run, total);
-    end = min(x + run, total);
+    x = (int)min((unsigned)cta * (unsigned)run, (unsigned)total);
+    end = (int)min((unsigned)x + (unsigned)run, (unsigned)total);
   }
 
   // The next item (the same in every lane); false: none left.

@@ -19,7 +19,7 @@ def walk(tmp_path_factory):
     if shutil.which("g++") is None or not os.path.exists(CUDA):
         pytest.skip("no host compiler or CUDA headers")
     exe = str(tmp_path_factory.mktemp("walk") / "walk_host")
-    subprocess.run(["g++", "-O1", "-std=c++17", "-Wno-attributes", "-I", CUDA, "-I", os.path.join(ROOT, "include"), "-I",
+    subprocess.run(["g++", "-O1", "-fwrapv", "-std=c++17", "-Wno-attributes", "-I", CUDA, "-I", os.path.join(ROOT, "include"), "-I",
                     os.path.join(ROOT, "paper_2609_06663_gb300", "csrc"), os.path.join(HERE, "walk_host.cpp"), "-o", exe],
                    check=True)
 
@@ -182,3 +182,17 @@ def test_attend_walk_of_random_calls(walk, tc):
             offsets = [0] + sorted(rng.randint(0, rows) for _ in range(h_kv - 1)) + [rows]
         check_attend(walk, rng.choice([1, 3, 20, 152]), h_kv, rng.choice([1, 4, 7, 64]), new, lens, rows, offsets, tc, single,
                      tree=rng.random() < 0.5)
+
+
+def test_attend_walk_of_as_much_work_as_is_taken(walk):
+    """A prefix whose units are one less than 31 bits hold: every CTA has its equal run of them."""
+    P, h_kv, groups, tiles = 152, 7, 3069, 99962
+    total = h_kv * groups * tiles
+    assert total == 2 ** 31 - 2
+    run = div_up(total, P)
+    for cta in (0, 1, 77, 150, 151):
+        got, _ = check_attend(walk, P, h_kv, 1, [64 * groups], [], tiles * TILE, None, False, ctas=(cta, cta))
+        assert sum(it[-1] for it in got[cta]) == min(run, total - cta * run), cta
+        first, unit = got[cta][0], cta * run
+        head, unit = divmod(unit, groups * tiles)
+        assert first[1] == head and first[3] == unit // tiles * 64 and first[-2] == unit % tiles
