@@ -407,8 +407,13 @@ static ecokv_status attend(const ecokv_attend_params* p, ecokv_dtype dtype, cons
   // 128 rows before them 16.7 us and not 29.9)
   if (!tc && mask != nullptr) {
     int rows = 64;
-    while (rows > 16 && rows / 2 >= a.g &&
-           (double)a.h_kv * ((a.tokens - 1) / (rows / a.g) + 1) * (tiles_of(a.prefix.rows) + 1) < 2.0 * attend_sms())
+    auto tiles = [&](int n) { return (double)((a.tokens - 1) / (n / a.g) + 1); };
+    // (and no smaller than what is counted in 31 bits, below: the limit is that of 64 rows)
+    auto counted = [&](int n) {
+      return a.h_kv * (tiles(n) * tiles_of(a.prefix.rows) + (tiles(n) + a.batch) * tiles_of(a.cap)) <= 0x7fffffff;
+    };
+    while (rows > 16 && rows / 2 >= a.g && a.h_kv * tiles(rows) * (tiles_of(a.prefix.rows) + 1) < 2.0 * attend_sms() &&
+           counted(rows / 2))
       rows /= 2;
     a.tpt = rows / a.g;
   }

@@ -178,3 +178,20 @@ def test_helpers_want_cuda_tensors():
         E.attend_tree(torch.zeros(2, 4, 128), None, None, torch.zeros(2, 1, dtype=torch.int64))
     with pytest.raises(ValueError):
         E.weigh(torch.zeros(2, 4, 128), torch.zeros(2, 4), None, None)
+
+
+@pytest.mark.parametrize("dtype,flags", [(1, 0), (1, E.ECOKV_FLAG_FORCE_SIMT), (0, 0)])
+@pytest.mark.parametrize("group", [1, 2, 7, 32, 64])
+@pytest.mark.parametrize("tokens,page,cols,rows", [(2560, 4096, 4096, 0), (40, 4096, 4096, 0), (1, 4096, 4096, 1000),
+                                                   (300, 16, 8192, 100)])
+def test_attend_tree_size_limit(tokens, page, cols, rows, group, dtype, flags):
+    """The header's count of work, whichever tiles the call is cut in (no workspace is given: nothing is launched)."""
+    tc = dtype == 1 and not flags
+    n = -(-tokens // (2 * (128 // group) if tc else 64 // group))
+    u = lambda keys: (2 * -(-keys // 128) + 4 if tc else -(-keys // 128)) if keys else 0  # noqa: E731
+    most = (2 ** 31 - 1 - n * u(rows)) // u(page * cols) - n
+    for batch, code in ((most, 3), (most + 1, 2)):
+        p = params(h_q=group, h_kv=1, tokens=tokens, batch=batch, flags=flags)
+        c = pages(page_size=page, table_stride=cols, page_stride=page * 128, head_stride=page * 128)
+        pre = prefix(rows=rows, head_stride=max(rows, 1) * 128)
+        assert E.ecokv_attend_tree(p, dtype, FAKE, pre, c, FAKE, FAKE, 1, FAKE, None, FAKE, 0) == code, batch
