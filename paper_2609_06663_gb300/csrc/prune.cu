@@ -304,12 +304,13 @@ extern "C" ecokv_status ecokv_prune(const ecokv_prune_params* p, ecokv_dtype dty
   a.cap = cache->page_size * cache->table_stride;
   a.cached = a.cap < kMostCached ? a.cap : kMostCached;
   const int64_t units = (int64_t)p->batch * p->h_kv, rows = to != nullptr ? p->limit : p->budget;
-  // two CTAs a unit, and more while all of them together are no more than two an SM (152 SMs) and
-  // have a chunk each, up to a cluster's eight
+  // two CTAs a unit, and more while all of them together are no more than two an SM and have a chunk
+  // each, up to a cluster's eight
+  const int64_t sms = attend_sms();
   const int64_t chunk = kMoveBytes / (kD * (dtype == ECOKV_F32 ? 4 : 2));
   a.m.ctas = 1;
-  while (a.m.ctas < 4 && units * 2 * a.m.ctas < 152 && chunk * a.m.ctas < rows) a.m.ctas *= 2;
-  const bool choose = units * 2 * a.m.ctas <= 2 * 152;
+  while (a.m.ctas < 4 && units * 2 * a.m.ctas < sms && chunk * a.m.ctas < rows) a.m.ctas *= 2;
+  const bool choose = units * 2 * a.m.ctas <= 2 * sms;
   a.m.cluster = choose ? 2 * a.m.ctas : 1;
   const bool same = lengths_out == cache->lengths;
   a.lengths_out = same ? nullptr : lengths_out;
