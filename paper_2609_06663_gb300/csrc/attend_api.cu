@@ -402,20 +402,17 @@ static ecokv_status attend(const ecokv_attend_params* p, ecokv_dtype dtype, cons
   a.h_kv = p->h_kv;
   a.g = p->h_q / p->h_kv;
   a.tpt = (tc ? kTileRows : 64) / a.g;
-  // A tree on CUDA cores: rows in smaller tiles where there would be few of them, down to 16
-  // (16 rows of an item take a fifth of the time of 64: 8 trees of up to 13 drafts, 8 heads,
-  // 128 rows before them 16.7 us and not 29.9)
-  if (!tc && mask != nullptr) {
-    int rows = 64;
-    auto tiles = [&](int n) { return (double)((a.tokens - 1) / (n / a.g) + 1); };
-    // (and no smaller than what is counted in 31 bits, below: the limit is that of 64 rows)
-    auto counted = [&](int n) {
-      return a.h_kv * (tiles(n) * tiles_of(a.prefix.rows) + (tiles(n) + a.batch) * tiles_of(a.cap)) <= 0x7fffffff;
-    };
-    while (rows > 16 && rows / 2 >= a.g && a.h_kv * tiles(rows) * (tiles_of(a.prefix.rows) + 1) < 2.0 * attend_sms() &&
-           counted(rows / 2))
-      rows /= 2;
-    a.tpt = rows / a.g;
+  // A tree on CUDA cores: row tiles of 16 where even those are few, one or two a CTA (two take the time
+  // of one of 64, whose rows cost less each: 8 trees of up to 13 drafts, 8 heads, 128 rows before
+  // them and up to 200 slots 16.5 us, 24.4 in 64s; one of 64 drafts over 4000 slots 68.6 and 41.6.
+  // Of 70 batches of 1 to 32 trees this takes 1.02 times the better of the two, 64 rows
+  // always 1.05, 16 always 1.45).  A table with room for more than is in use counts in full, and
+  // a call is then cut in 64s.
+  if (!tc && mask != nullptr && a.g <= 16) {
+    const int few = 16 / a.g;
+    const double groups = (a.tokens - 1) / few + 1, each = (a.tokens - 1) / a.batch / few + 1;
+    if (a.h_kv * (groups * tiles_of(a.prefix.rows) + a.batch * each * tiles_of(a.cap)) <= 1.5 * attend_sms())
+      a.tpt = few;
   }
   a.span = tc ? 2 * a.tpt : a.tpt;
   a.parts = tc ? 2 : 1;
