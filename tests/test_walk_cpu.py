@@ -196,3 +196,23 @@ def test_attend_walk_of_as_much_work_as_is_taken(walk):
         first, unit = got[cta][0], cta * run
         head, unit = divmod(unit, groups * tiles)
         assert first[1] == head and first[3] == unit // tiles * 64 and first[-2] == unit % tiles
+
+
+def test_weigh_walk_of_as_much_work_as_is_taken(walk):
+    P, h_kv, spans, tiles = 152, 8, 65536, 1022  # (a tile is 4 units, an item's keys 4)
+    per, total = 4 + 4 * tiles, h_kv * spans * (4 + 4 * tiles)
+    assert 2 ** 31 - per * h_kv * spans <= total < 2 ** 31
+    run = div_up(total, P)
+    for cta in (0, 75, 151):
+        got, status = walk("weigh", [P, cta, cta, h_kv, 128 * tiles, 1, 256 * spans, 1 << 20, 0, 0, 0, 8, 128, 128, 4, 4, 4, 24, 4])
+        x, end = cta * run, min((cta + 1) * run, total)
+        want = []
+        while x < end:
+            item, y = divmod(x, per)
+            z = min(per, y + end - x)
+            t0, t1 = (div_up(max(v - 4, 0), 4) for v in (y, z))
+            if t1 > t0:
+                head, k = divmod(item, spans)
+                want.append((0, head, 0, k * 256, 256, 0, 128 * tiles, 256 * spans, 0, t0, t1 - t0))
+            x += z - y
+        assert status == 0 and got[cta] == want
