@@ -104,8 +104,8 @@ __device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b, bool report)
 }
 // Units of a tile of an item of so many tokens; those an item has before its first
 // tile's (one row tile: 1, two: 4, their sums being up to 128 KB; at 1 for both 16
-// sequences of 61 tokens over 6554 rows take 144 us, so 91; at 4 for both 61 single
-// tokens of 32 heads over 1095 rows 71, so 45); all of an item's.
+// sequences of 61 tokens over 6554 rows take 137 us, so 95; at 4 for both 61 single
+// tokens of 32 heads over 1095 rows 67, so 42); all of an item's.
 __host__ __device__ inline int tile_units(const AttendArgs& a, int ntok) { return ntok > a.tpt ? 2 : 1; }
 __host__ __device__ inline int lead_units(const AttendArgs& a, int ntok) { return ntok > a.tpt ? 4 * a.lead : a.lead; }
 __host__ __device__ inline int item_units(const AttendArgs& a, int tiles, int ntok) {

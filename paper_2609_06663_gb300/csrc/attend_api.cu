@@ -187,8 +187,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 8)
       const float w = next_weight(M, L, acc, ml);
       const int n = min(32, l.n - e0);
       // (in one order; past two sums the loads of four at once: 768 drafts of 28 heads 68.3 us,
-      // 70.5 one after another.  Eight CTAs an SM: without that bound 3000 tokens of 32 heads,
-      // of few sums a row, take 167 us and not 162.5.)
+      // 70.5 one after another.  Eight CTAs an SM, 64 registers a thread and 28 bytes of it
+      // spilled: without that bound 3000 tokens of 32 heads, of few sums a row, take 167 us and
+      // not 162.5.)
       if (n <= 2) {
 #pragma unroll 2
         for (int k = 0; k < n; ++k) {

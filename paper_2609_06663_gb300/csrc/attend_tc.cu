@@ -298,7 +298,7 @@ __device__ __forceinline__ void soften(Smem& s, const AttendArgs& a, uint32_t tm
         // of a tile's scores in registers and unrolled: the batch of 16 over 3277 rows
         // 16.2 us, 1952 items of a tile each 59.0; in two rolled passes, one for the
         // maximum, 15.1 and 50.2; so 15.0 and 49.1, 16 questions of 61 tokens over 6554
-        // rows 109.8 and not 116.6; with what came after it 14.7, 45.6 and 107)
+        // rows 109.8 and not 116.6; with what came after it 14.7, 42.3 and 91.6)
         const int seen = lim - from;
 #pragma unroll 1
         for (int b = 0; b < nc; ++b) {

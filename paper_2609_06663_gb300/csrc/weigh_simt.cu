@@ -5,7 +5,7 @@
 // registers, lanes 2k and 2k + 1 the halves of key k, and goes over the rows, whose dot
 // products need one shuffle and whose weights no other thread's.  Bound by the chain of
 // loads before the first of them (8 sequences of up to three tokens, 8 heads: 10.7 us; one
-// sequence, one token 5.9).
+// sequence, one token 5.5).
 //
 // Items of more rows: keys and rows of a tile in shared memory as fp32; thread (ty, tx) of
 // 16 x 16 forms the scores of its four rows with the keys tx + 16 j and adds their

@@ -11,9 +11,10 @@
 // each other's latencies.  The sums of an item's even and odd tiles are added at its end.
 //
 // Bound by the keys' bytes where few rows see them (64 sequences of up to 4097 slots and a
-// token each, 28 heads over 4: 30.5 us, 5.0 TB/s over the call, of which 8 are the walk's
-// start and the launch).  Where many do (806 tokens over 6554 rows: 46.4 us, 824 TFLOP/s) a
-// stream's 128 columns take 3100 cycles, its wait for their product 600, and a CTA's four
+// token each, 28 heads over 4: 31.0 us, 4.9 TB/s over the call, of which 8 are the walk's
+// start and the launch).  Where many do (806 tokens over 6554 rows: 45.5 us, 841 TFLOP/s) a
+// stream takes 5100 cycles a row tile: 3240 for its 128 columns, 380 waiting for their
+// references, 260 for the product, 120 for the other stream's sum.  A CTA's four
 // streams share a unit for exponentials that 2048 would do and a tensor pipe that 2200
 // would: without exponentials it takes 44 us, with half of each product 45, with half of
 // the columns 36.
